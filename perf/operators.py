@@ -187,6 +187,10 @@ def prepare(case, seed):
     s = _case_inputs(case, seed)
     kind, B, Hkv = s["kind"], s["B"], s["Hkv"]
     if kind == "prefill":
+        if own:
+            from paper_2405_04532_amd import api
+            need = api.attention_prefill_workspace_bytes(s["q"].shape[0], s["k"].shape[0], B, s["H"], Hkv, s["window"], s["sinks"])
+            s["workspace"] = api.new_workspace(need, "cuda")
         return s
     if own:
         from paper_2405_04532_amd import api
@@ -357,7 +361,8 @@ def run(s):
         if kind == "decode":
             return dict(out=api.kv4_paged_attention_decode(s["q"], s["pool"], s["table"], s["lens"], s["Hkv"], window=s["window"],
                                                            sinks=s["sinks"], out=s["out"], workspace=s["workspace"]))
-        return dict(out=api.attention_prefill(s["q"], s["k"], s["v"], s["cu_q"], s["cu_k"], window=s["window"], sinks=s["sinks"]))
+        return dict(out=api.attention_prefill(s["q"], s["k"], s["v"], s["cu_q"], s["cu_k"], window=s["window"], sinks=s["sinks"],
+                                              workspace=s["workspace"]))
     if kind == "append":
         q, k = _plain_append(s)
         kc, vc = _plain_read(s["pool"], s["table"], s["cu"], s["starts"], q.shape[0])
