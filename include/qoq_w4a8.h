@@ -263,6 +263,65 @@ int qoq_kv4_unpack(const void* cache, int64_t B, int64_t Hkv, int64_t S_max, int
                    void* k_scale_fp16, void* k_zero_fp16, uint8_t* v_codes, void* v_scale_fp16, void* v_zero_fp16,
                    void* stream);
 
+/* ---- The KV4 cache in pages, and what a layer runs around it -------------------------------------------------
+ * A pool holds `pages` pages of 64 tokens, qoq_kv4_pool_bytes(pages, Hkv, D) bytes of device memory owned by the
+ * caller; a page keeps all KV heads of its tokens, coded as in the contiguous cache above.  A block table [B, width] of
+ * INT32 names the page of each 64 tokens of a sequence, position t lying in entry t / 64.  An entry outside [0, pages)
+ * is no page: what would be written there is dropped, what would be read there is not seen.  Entries behind a
+ * sequence's length, and in front of its window but for the sinks, are not used, so their pages may be given away.
+ *
+ * A ragged batch of B sequences is described by cu [B + 1] INT32, device, ascending: sequence b owns the rows cu[b] ..
+ * cu[b + 1] - 1 of tensors of M rows.  Rows outside cu[0] .. cu[B] - 1 belong to none: outputs are left as they were there.
+ * Values of cu outside [0, M] are taken as the nearest bound or their rows left out; nothing outside the M rows is touched.
+ * Tensors of heads are [M, heads, 128] FP16 with contiguous heads; their strides from token to token are given in elements (a
+ * multiple of 8, at least heads * 128, at most 4194304), so that they may be slices of a fused QKV projection.
+ *
+ * qoq_qk_rope_kv4_append: for every row, of sequence b and position p = starts[b] + row - cu[b]
+ *     y = x gamma / sqrt(mean(x^2) + eps)          per head, where q_gamma / k_gamma [128] FP16 are given (else y = x)
+ *     (a, b) -> (a cos - b sin, b cos + a sin)      the pairs (i, i + rot/2) of y's first `rot` elements, or (2i, 2i + 1)
+ *                                                   with `interleaved`; cos = angles[p][i], sin = angles[p][rot/2 + i]
+ *   evaluated in FP64 and rounded once to FP16: q_out, k_out; k_out and v are quantized exactly as qoq_kv4_append does and
+ *   written into the pages of their positions (positions outside [0, 64 width) are dropped).
+ *   angles    [angle_rows, rot] FP32; rot = 0 with NULL: no rotation; else a multiple of 16 up to 128.  Positions outside
+ *             [0, angle_rows) take the nearest row.
+ *   starts    [B] INT32, or NULL: zeros.
+ *   q, q_out  may be NULL together (keys and values only); q_out may be q itself, k_out may be k itself or NULL.
+ *   Positions of one call that lie in the same place of the same page (a page named twice) are written in no order.
+ * qoq_kv4_paged_gather: k_out, v_out [M, Hkv, 128] FP16 contiguous: row cu[b] + i is the dequantized token starts[b] + i of
+ *   sequence b, (code - z) s rounded once; zeros where it lies on no page.  For a prompt that goes on behind cached tokens.
+ * qoq_kv4_paged_attention_decode: qoq_kv4_attention_decode over pages, q [B, H, 128] with a stride, out [B, H, 128] contiguous; of
+ *   the seq_lens[b] tokens (clamped to [0, 64 width]) those t with  t >= seq_lens[b] - window  or  t < sinks  are seen; window = 0:
+ *   all.  A query that sees nothing gives a zero row.
+ *   workspace  NULL, or at least qoq_kv4_paged_attention_workspace_bytes(...) bytes (0: none is needed), 16-byte aligned, zero-filled
+ *              once with qoq_gemm_workspace_prepare, as for qoq_w4a8_gemm, whose workspace may be the same one: calls of both kinds
+ *              and any shapes may take turns in it on one stream; calls that overlap in time need workspaces of their own.
+ *              Without one, a sequence is not shared by several workgroups.  The sums are the same ones in every call on the
+ *              same inputs, whichever workgroup ends last.
+ * qoq_attention_prefill: causal attention over FP16 keys and values; a sequence's Tq queries (cu_q, M rows) are the last of its Tk
+ *   tokens (cu_k, Mk rows): query i has position p = Tk - Tq + i and sees t <= p with  t > p - window  or  t < sinks  (window = 0: all);
+ *     out[i, h] = softmax_t(q[i, h] . k[t, h / r] / sqrt(128)) v[t, h / r],  r = H / Hkv <= 64
+ *   FP32 softmax and sums, weights rounded to FP16 for the second product, one rounding at the end.  A query that sees nothing gives a
+ *   zero row.  Infinities and NaN in keys and values reach the queries that see them, and no others.
+ *   out [M, H, 128] FP16 contiguous; workspace as above, of qoq_attention_prefill_workspace_bytes(...) bytes.
+ * Limits: D = 128; B <= 1048576, Hkv <= 1024, M and Mk <= 16777216, width <= 262144, pages <= 2^31 - 1, window and sinks >= 0; in decode
+ * H / Hkv <= 16.  Errors as above. */
+size_t qoq_kv4_pool_bytes(int64_t pages, int64_t Hkv, int64_t D);
+int qoq_qk_rope_kv4_append(const void* q_fp16, int64_t q_stride, const void* k_fp16, int64_t k_stride, const void* v_fp16, int64_t v_stride,
+                           const void* q_gamma_fp16, const void* k_gamma_fp16, double eps, const float* angles, int64_t angle_rows,
+                           int64_t rot, int interleaved, const int32_t* cu, const int32_t* starts, int64_t M, int64_t B, int64_t H,
+                           int64_t Hkv, int64_t D, void* pool, int64_t pages, const int32_t* block_table, int64_t width, void* q_out_fp16,
+                           int64_t q_out_stride, void* k_out_fp16, int64_t k_out_stride, void* stream);
+int qoq_kv4_paged_gather(const void* pool, int64_t pages, const int32_t* block_table, int64_t width, const int32_t* cu, const int32_t* starts,
+                         int64_t M, int64_t B, int64_t Hkv, int64_t D, void* k_out_fp16, void* v_out_fp16, void* stream);
+size_t qoq_kv4_paged_attention_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t width, int64_t window, int64_t sinks);
+int qoq_kv4_paged_attention_decode(const void* q_fp16, int64_t q_stride, const void* pool, int64_t pages, const int32_t* block_table,
+                                   int64_t width, const int32_t* seq_lens, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t window,
+                                   int64_t sinks, void* out_fp16, void* workspace, size_t workspace_bytes, void* stream);
+size_t qoq_attention_prefill_workspace_bytes(int64_t M, int64_t Mk, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t window, int64_t sinks);
+int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp16, int64_t k_stride, const void* v_fp16, int64_t v_stride,
+                          const int32_t* cu_q, const int32_t* cu_k, int64_t M, int64_t Mk, int64_t B, int64_t H, int64_t Hkv, int64_t D,
+                          int64_t window, int64_t sinks, void* out_fp16, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Test/tuning hook: force the GEMM launch configuration instead of the built-in heuristic.
  * tile_m: 0 = auto; 16, 32, 64 = streaming kernel with that many tokens per tile; 65 = 64 tokens,
  * two adjacent blocks per workgroup in lockstep (N % 128 == 0; else as 64); 66 = four blocks in lockstep

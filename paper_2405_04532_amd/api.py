@@ -88,6 +88,19 @@ _SIGNATURES = {
     "qoq_kv4_unpack": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
                                       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                       ctypes.c_void_p, ctypes.c_void_p]),
+    "qoq_kv4_pool_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 3),
+    "qoq_qk_rope_kv4_append": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_double,
+                                             ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_int, ctypes.c_void_p,
+                                             ctypes.c_void_p] + [ctypes.c_int64] * 5 + [ctypes.c_void_p, ctypes.c_int64] * 4 +
+                               [ctypes.c_void_p]),
+    "qoq_kv4_paged_gather": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64] * 2 + [ctypes.c_void_p] * 2 + [ctypes.c_int64] * 4 +
+                             [ctypes.c_void_p] * 3),
+    "qoq_kv4_paged_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 7),
+    "qoq_kv4_paged_attention_decode": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_void_p] + [ctypes.c_int64] * 6 +
+                                       [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "qoq_attention_prefill_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 8),
+    "qoq_attention_prefill": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_void_p] * 2 + [ctypes.c_int64] * 8 +
+                              [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
 }
 
 EXPORTS = tuple(_SIGNATURES)
@@ -322,6 +335,73 @@ def kv4_unpack(cache, B, Hkv, S_max, D=128):
     _check(lib().qoq_kv4_unpack(_ptr(cache), B, Hkv, S_max, D, _ptr(kc), _ptr(ks), _ptr(kz), _ptr(vc), _ptr(vs), _ptr(vz),
                                 _stream(dev)))
     return kc, ks, kz, vc, vs, vz
+
+
+# ---------------------------------------------------------------------------------------
+# The KV4 cache in pages of a pool, and attention over prompts
+# ---------------------------------------------------------------------------------------
+KV4_PAGE = 64                     # tokens of a page
+
+
+def kv4_pool_bytes(pages, Hkv, D=128):
+    return int(lib().qoq_kv4_pool_bytes(pages, Hkv, D))
+
+
+def kv4_new_pool(pages, Hkv, device, D=128):
+    """An empty (zero-filled) pool of `pages` pages of 64 tokens, all KV heads of a token in one page."""
+    n = kv4_pool_bytes(pages, Hkv, D)
+    if n == 0:
+        raise QoqError(QOQ_ERR_SHAPE, "unsupported KV4 pool shape")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def rope_angles(positions, rot=128, theta=10000.0, device="cpu"):
+    """FP32 table [positions, rot] of the rotation: cosines, then sines, of p theta^(-2 i / rot), evaluated in FP64."""
+    inv = float(theta) ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
+    a = torch.arange(positions, dtype=torch.float64)[:, None] * inv
+    return torch.cat((a.cos(), a.sin()), dim=1).to(torch.float32).to(device)
+
+
+def qk_rope_kv4_append(q, k, v, pool, block_table, cu, starts, angles, q_gamma=None, k_gamma=None, eps=1e-6, interleaved=False,
+                       q_out=None, k_out=None, want_k=False):
+    """New tokens of a ragged batch: norms of q [M, H, 128] and k [M, Hkv, 128] per head (with gammas), rotation by `angles`
+    (rope_angles; None: no rotation), keys and values quantized into the pages of their positions; returns (q, k) as they are after
+    that, k only if asked for (want_k or k_out).  Token rows may be strided (slices of a QKV projection); q_out may be q, k_out
+    k.  cu [B + 1] INT32: rows of each sequence, starts [B] INT32 (None: zeros): the position of its first row; q may be None."""
+    return (_native or _load_native()).qk_rope_kv4_append(q, k, v, pool, block_table, cu, starts, angles, q_gamma, k_gamma, eps, interleaved,
+                                                          q_out, k_out, want_k)
+
+
+def kv4_paged_append(pool, k, v, block_table, cu, starts=None):
+    """Quantize k, v [M, Hkv, 128] FP16 as they are into the pages of their positions."""
+    qk_rope_kv4_append(None, k, v, pool, block_table, cu, starts, None)
+
+
+def kv4_paged_gather(pool, block_table, cu, starts, rows, Hkv, k_out=None, v_out=None):
+    """Tokens starts[b] .. starts[b] + cu[b + 1] - cu[b] - 1 of each sequence as FP16 keys and values [rows, Hkv, 128]."""
+    return (_native or _load_native()).kv4_paged_gather(pool, block_table, cu, starts, rows, Hkv, k_out, v_out)
+
+
+def kv4_paged_attention_workspace_bytes(B, H, Hkv, width, window=0, sinks=0, D=128):
+    return int(lib().qoq_kv4_paged_attention_workspace_bytes(B, H, Hkv, D, width, window, sinks))
+
+
+def kv4_paged_attention_decode(q, pool, block_table, seq_lens, Hkv, window=0, sinks=0, out=None, workspace=None):
+    """kv4_attention_decode over the pages that block_table [B, width] names: of the first seq_lens[b] tokens the last `window`
+    (0: all) and the first `sinks`.  With a `workspace` (new_workspace of kv4_paged_attention_workspace_bytes) several
+    workgroups may share a sequence."""
+    return (_native or _load_native()).kv4_paged_attention_decode(q, pool, block_table, seq_lens, Hkv, window, sinks, out, workspace)
+
+
+def attention_prefill_workspace_bytes(M, Mk, B, H, Hkv, window=0, sinks=0, D=128):
+    return int(lib().qoq_attention_prefill_workspace_bytes(M, Mk, B, H, Hkv, D, window, sinks))
+
+
+def attention_prefill(q, k, v, cu_q, cu_k, window=0, sinks=0, out=None, workspace=None):
+    """Causal attention of q [M, H, 128] over k, v [Mk, Hkv, 128], ragged by cu_q and cu_k [B + 1] INT32; a sequence's queries are
+    the last of its tokens.  A query sees the last `window` tokens up to its own (0: all) and the first `sinks`.  With a
+    `workspace` (new_workspace of attention_prefill_workspace_bytes) several workgroups may share the keys of few queries."""
+    return (_native or _load_native()).attention_prefill(q, k, v, cu_q, cu_k, window, sinks, out, workspace)
 
 
 # ---------------------------------------------------------------------------------------

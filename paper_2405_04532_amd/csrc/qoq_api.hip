@@ -427,6 +427,128 @@ int qoq_kv4_unpack(const void* cache, int64_t B, int64_t Hkv, int64_t S_max, int
                                   v_scale_fp16, v_zero_fp16, static_cast<hipStream_t>(stream)) == hipSuccess ? QOQ_OK : QOQ_ERR_HIP;
 }
 
+// ---- paged cache and prompt attention ---------------------------------------------------------------------
+static bool paged_ok(int64_t B, int64_t Hkv, int64_t D, int64_t pages, int64_t width)
+{
+    return D == 128 && B >= 0 && B <= (1 << 20) && Hkv > 0 && Hkv <= 1024 && pages > 0 && pages < (int64_t)1 << 31 && width > 0 && width <= (1 << 18);
+}
+static bool rows_ok(int64_t M) { return M >= 0 && M <= (1 << 24); }
+static bool stride_ok(int64_t stride, int64_t heads) { return stride >= heads * 128 && stride % 8 == 0 && stride <= (1 << 22); }
+static bool window_ok(int64_t window, int64_t sinks) { return window >= 0 && sinks >= 0; }
+// no sequence is longer
+static int64_t at_most(int64_t v) { return v < (1 << 24) ? v : 1 << 24; }
+
+size_t qoq_kv4_pool_bytes(int64_t pages, int64_t Hkv, int64_t D)
+{
+    return paged_ok(0, Hkv, D, pages, 1) ? (size_t)(pages * qoq::kv4_page_bytes(Hkv)) : 0;
+}
+
+int qoq_qk_rope_kv4_append(const void* q_fp16, int64_t q_stride, const void* k_fp16, int64_t k_stride, const void* v_fp16, int64_t v_stride,
+                           const void* q_gamma_fp16, const void* k_gamma_fp16, double eps, const float* angles, int64_t angle_rows,
+                           int64_t rot, int interleaved, const int32_t* cu, const int32_t* starts, int64_t M, int64_t B, int64_t H,
+                           int64_t Hkv, int64_t D, void* pool, int64_t pages, const int32_t* block_table, int64_t width, void* q_out_fp16,
+                           int64_t q_out_stride, void* k_out_fp16, int64_t k_out_stride, void* stream)
+{
+    if (!paged_ok(B, Hkv, D, pages, width) || !rows_ok(M) || !(eps >= 0.0) || std::isinf(eps)) return QOQ_ERR_SHAPE;
+    if (rot < 0 || rot > 128 || rot % 16 != 0 || (rot && (angle_rows <= 0 || angle_rows >= (int64_t)1 << 31))) return QOQ_ERR_SHAPE;
+    if (!stride_ok(k_stride, Hkv) || !stride_ok(v_stride, Hkv) || (k_out_fp16 && !stride_ok(k_out_stride, Hkv))) return QOQ_ERR_SHAPE;
+    if (q_fp16 && (H <= 0 || H > 16384 || !stride_ok(q_stride, H) || !stride_ok(q_out_stride, H))) return QOQ_ERR_SHAPE;
+    if (B == 0 || M == 0) return QOQ_OK;
+    if (!k_fp16 || !v_fp16 || !cu || !pool || !block_table || !q_fp16 != !q_out_fp16 || (rot && !angles)) return QOQ_ERR_NULL;
+    if (!aligned16(q_fp16) || !aligned16(k_fp16) || !aligned16(v_fp16) || !aligned16(q_gamma_fp16) || !aligned16(k_gamma_fp16) ||
+        !aligned16(angles) || !aligned16(pool) || !aligned16(q_out_fp16) || !aligned16(k_out_fp16) || !aligned4(cu) || !aligned4(starts) ||
+        !aligned4(block_table))
+        return QOQ_ERR_ALIGN;
+    if (!arch_ok()) return QOQ_ERR_ARCH;
+    qoq::RopeAppend a{};
+    a.q = q_fp16; a.k = k_fp16; a.v = v_fp16;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+    a.q_gamma = q_gamma_fp16; a.k_gamma = k_gamma_fp16; a.eps = eps;
+    a.angles = angles; a.angle_rows = rot ? angle_rows : 0; a.rot = rot; a.interleaved = interleaved != 0;
+    a.cu = cu; a.starts = starts;
+    a.M = M; a.B = B; a.H = q_fp16 ? H : 0; a.Hkv = Hkv;
+    a.pool = static_cast<uint8_t*>(pool); a.pages = pages; a.table = block_table; a.width = width;
+    a.q_out = q_out_fp16; a.k_out = k_out_fp16; a.q_out_stride = q_out_stride; a.k_out_stride = k_out_stride;
+    return qoq::launch_rope_append(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QOQ_OK : QOQ_ERR_HIP;
+}
+
+int qoq_kv4_paged_gather(const void* pool, int64_t pages, const int32_t* block_table, int64_t width, const int32_t* cu, const int32_t* starts,
+                         int64_t M, int64_t B, int64_t Hkv, int64_t D, void* k_out_fp16, void* v_out_fp16, void* stream)
+{
+    if (!paged_ok(B, Hkv, D, pages, width) || !rows_ok(M)) return QOQ_ERR_SHAPE;
+    if (B == 0 || M == 0) return QOQ_OK;
+    if (!pool || !block_table || !cu || !k_out_fp16 || !v_out_fp16) return QOQ_ERR_NULL;
+    if (!aligned16(pool) || !aligned16(k_out_fp16) || !aligned16(v_out_fp16) || !aligned4(block_table) || !aligned4(cu) || !aligned4(starts))
+        return QOQ_ERR_ALIGN;
+    if (!arch_ok()) return QOQ_ERR_ARCH;
+    return qoq::launch_paged_gather(static_cast<const uint8_t*>(pool), pages, block_table, width, cu, starts, M, B, Hkv, k_out_fp16, v_out_fp16,
+                                    static_cast<hipStream_t>(stream)) == hipSuccess ? QOQ_OK : QOQ_ERR_HIP;
+}
+
+static bool paged_decode_ok(int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t width, int64_t window, int64_t sinks)
+{
+    return paged_ok(B, Hkv, D, 1, width) && H > 0 && H % Hkv == 0 && H / Hkv <= 16 && window_ok(window, sinks) && B * Hkv < (int64_t)1 << 31;
+}
+
+size_t qoq_kv4_paged_attention_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t width, int64_t window, int64_t sinks)
+{
+    if (!paged_decode_ok(B, H, Hkv, D, width, window, sinks)) return 0;
+    return qoq::paged_decode_workspace_bytes(B, H, Hkv, width, at_most(window), at_most(sinks));
+}
+
+int qoq_kv4_paged_attention_decode(const void* q_fp16, int64_t q_stride, const void* pool, int64_t pages, const int32_t* block_table,
+                                   int64_t width, const int32_t* seq_lens, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t window,
+                                   int64_t sinks, void* out_fp16, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!paged_ok(B, Hkv, D, pages, width) || !paged_decode_ok(B, H, Hkv, D, width, window, sinks) || !stride_ok(q_stride, H)) return QOQ_ERR_SHAPE;
+    if (B == 0) return QOQ_OK;
+    if (!q_fp16 || !pool || !block_table || !seq_lens || !out_fp16) return QOQ_ERR_NULL;
+    if (!aligned16(q_fp16) || !aligned16(pool) || !aligned16(out_fp16) || !aligned16(workspace) || !aligned4(block_table) || !aligned4(seq_lens))
+        return QOQ_ERR_ALIGN;
+    window = at_most(window), sinks = at_most(sinks);
+    const size_t need = qoq::paged_decode_workspace_bytes(B, H, Hkv, width, window, sinks);
+    if (workspace && workspace_bytes < need) return QOQ_ERR_WORKSPACE;
+    if (!arch_ok()) return QOQ_ERR_ARCH;
+    return qoq::launch_paged_decode(q_fp16, q_stride, static_cast<const uint8_t*>(pool), pages, block_table, width, seq_lens, B, H, Hkv, window, sinks,
+                                    out_fp16, need ? workspace : nullptr, static_cast<hipStream_t>(stream)) == hipSuccess ? QOQ_OK : QOQ_ERR_HIP;
+}
+
+static bool prefill_ok(int64_t M, int64_t Mk, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t window, int64_t sinks)
+{
+    return paged_ok(B, Hkv, D, 1, 1) && rows_ok(M) && rows_ok(Mk) && H > 0 && H % Hkv == 0 && H / Hkv <= 64 && window_ok(window, sinks);
+}
+
+size_t qoq_attention_prefill_workspace_bytes(int64_t M, int64_t Mk, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t window, int64_t sinks)
+{
+    if (!prefill_ok(M, Mk, B, H, Hkv, D, window, sinks)) return 0;
+    return qoq::prefill_workspace_bytes(M, Mk, B, H, Hkv, at_most(window), at_most(sinks));
+}
+
+int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp16, int64_t k_stride, const void* v_fp16, int64_t v_stride,
+                          const int32_t* cu_q, const int32_t* cu_k, int64_t M, int64_t Mk, int64_t B, int64_t H, int64_t Hkv, int64_t D,
+                          int64_t window, int64_t sinks, void* out_fp16, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!prefill_ok(M, Mk, B, H, Hkv, D, window, sinks) || !stride_ok(q_stride, H) || !stride_ok(k_stride, Hkv) || !stride_ok(v_stride, Hkv))
+        return QOQ_ERR_SHAPE;
+    if (B == 0 || M == 0) return QOQ_OK;
+    if (!q_fp16 || !cu_q || !cu_k || !out_fp16 || (Mk && (!k_fp16 || !v_fp16))) return QOQ_ERR_NULL;
+    if (!aligned16(q_fp16) || !aligned16(k_fp16) || !aligned16(v_fp16) || !aligned16(out_fp16) || !aligned16(workspace) || !aligned4(cu_q) ||
+        !aligned4(cu_k))
+        return QOQ_ERR_ALIGN;
+    window = at_most(window), sinks = at_most(sinks);
+    const size_t need = qoq::prefill_workspace_bytes(M, Mk, B, H, Hkv, window, sinks);
+    if (workspace && workspace_bytes < need) return QOQ_ERR_WORKSPACE;
+    if (!arch_ok()) return QOQ_ERR_ARCH;
+    qoq::Prefill a{};
+    a.q = q_fp16; a.k = k_fp16; a.v = v_fp16;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+    a.cu_q = cu_q; a.cu_k = cu_k;
+    a.M = M; a.Mk = Mk; a.B = B; a.H = H; a.Hkv = Hkv; a.window = window; a.sinks = sinks;
+    a.out = out_fp16;
+    a.workspace = need ? workspace : nullptr;
+    return qoq::launch_prefill(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QOQ_OK : QOQ_ERR_HIP;
+}
+
 int qoq_w4a8_gemm(const int8_t* qx, const void* sx_fp16, const int32_t* rowsum, const void* packed, int64_t M,
                   int64_t N, int64_t K, int mode, void* out_fp16, void* workspace, size_t workspace_bytes,
                   void* stream)

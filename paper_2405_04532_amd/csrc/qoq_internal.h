@@ -78,6 +78,45 @@ hipError_t launch_kv4_decode(const void* q, const uint8_t* cache, const int32_t*
                              int64_t S_max, void* out, void* workspace, size_t workspace_bytes, hipStream_t s);
 size_t kv4_decode_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t S_max);
 
+// qoq_kv4_paged.hip: the same cache in pages of a pool.
+struct RopeAppend {
+    const void *q, *k, *v;               // FP16 rows of H, Hkv, Hkv heads; q may be null
+    int64_t q_stride, k_stride, v_stride;
+    const void *q_gamma, *k_gamma;       // FP16 [128], or null
+    double eps;
+    const float* angles;                 // [angle_rows, rot], or null with rot = 0
+    int64_t angle_rows, rot;
+    int interleaved;
+    const int32_t *cu, *starts;          // starts may be null
+    int64_t M, B, H, Hkv;
+    uint8_t* pool;
+    int64_t pages;
+    const int32_t* table;
+    int64_t width;
+    void *q_out, *k_out;                 // k_out may be null
+    int64_t q_out_stride, k_out_stride;
+};
+int64_t kv4_page_bytes(int64_t Hkv);
+hipError_t launch_rope_append(const RopeAppend& a, hipStream_t s);
+hipError_t launch_paged_gather(const uint8_t* pool, int64_t pages, const int32_t* table, int64_t width, const int32_t* cu,
+                               const int32_t* starts, int64_t M, int64_t B, int64_t Hkv, void* k_out, void* v_out, hipStream_t s);
+size_t paged_decode_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t width, int64_t window, int64_t sinks);
+hipError_t launch_paged_decode(const void* q, int64_t q_stride, const uint8_t* pool, int64_t pages, const int32_t* table, int64_t width,
+                               const int32_t* seq_lens, int64_t B, int64_t H, int64_t Hkv, int64_t window, int64_t sinks, void* out,
+                               void* workspace, hipStream_t s);
+
+// qoq_prefill.hip: causal attention over ragged prompts.
+struct Prefill {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    const int32_t *cu_q, *cu_k;
+    int64_t M, Mk, B, H, Hkv, window, sinks;
+    void* out;
+    void* workspace;
+};
+size_t prefill_workspace_bytes(int64_t M, int64_t Mk, int64_t B, int64_t H, int64_t Hkv, int64_t window, int64_t sinks);
+hipError_t launch_prefill(const Prefill& a, hipStream_t s);
+
 // Launch configuration the library picks for a problem (also sizes the workspace).
 struct GemmTuning { int tile_m, split_k; };  // 0 = let the heuristic decide
 // eight_waves = false: a plan without those kernels, whose k-slices take more workspace, and without 48-token tiles in place of

@@ -1,0 +1,707 @@
+// The 4-bit KV cache in pages of a pool: norm, rotation and quantization of new tokens, tokens back as FP16, decode attention.
+//
+// Pool.  `pages` pages of 64 tokens; a page holds, for each KV head, the 8704 bytes that the contiguous cache holds per 64
+// tokens (qoq_kv4.hip): codes of the keys, their scales and zeros, codes of the values, theirs.  A block table [B, width] names
+// the page of each 64 tokens of a sequence; an entry outside 0 .. pages - 1 is no page: nothing is read or written there.
+#include <algorithm>
+#include <type_traits>
+
+#include "qoq_gemm_common.h"
+#include "qoq_kv4_common.h"
+#include "qoq_ragged.h"
+#include "qoq_workspace.h"
+
+namespace qoq {
+namespace {
+
+// ------------------------------------------------------------------------------------------
+// Norm, rotation and quantization of new tokens.  One pass over queries, keys and values: a row of 16 lanes holds one head of one
+// token, 8 elements (16 bytes) a lane, so that a head's sum of squares, the other half of a rotated pair, and the quantizer's range
+// are exchanges inside the row.
+//   y = x gamma r,  r = 1 / sqrt(mean(x^2) + eps)   (with gamma);   pairs (a, b) -> (a cos - b sin, b cos + a sin)
+// x gamma is exact in FP32 (two 11-bit numbers), its product with the FP32 cosine exact in FP64, whose multiply-add runs at
+// FP32's rate here, so everything behind x gamma is FP64 and the result the FP64 evaluation rounded once to FP16.
+// ------------------------------------------------------------------------------------------
+struct AppendArgs {
+    const __half *q, *k, *v;                     // token rows, their strides in elements
+    int64_t q_stride, k_stride, v_stride;
+    const __half *q_gamma, *k_gamma;             // [128] or null
+    double eps;
+    const float* angles;                         // [angle_rows, rot]: cosines, sines
+    int angle_rows, rot, interleaved;
+    const int32_t *cu, *starts;                  // starts may be null
+    int M, B, H, Hkv;
+    uint8_t* pool;
+    uint32_t pages;
+    const int32_t* table;
+    int width;
+    __half *q_out, *k_out;                       // k_out may be null
+    int64_t q_out_stride, k_out_stride;
+    uint32_t kv_items, q_items, q_groups, q_heads;      // waves for keys and values, for queries; groups of q_heads heads per four rows
+};
+
+// a number as FP16, rounded once: through FP32 unless that could be a midpoint of two FP16 numbers (its last 12 bits are then zero)
+__device__ __forceinline__ uint4 halves_of(const double (&y)[8])
+{
+    float f[8];
+    uint32_t least = 0xFFFu;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        f[e] = (float)y[e];
+        least = min(least, (uint32_t)__float_as_int(f[e]) & 0xFFFu);
+    }
+    uint32_t o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = __builtin_bit_cast(uint32_t, (h2){(_Float16)f[2 * e], (_Float16)f[2 * e + 1]});
+    if (least == 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (((uint32_t)__float_as_int(f[e]) & 0xFFFu) == 0 && (__float_as_int(f[e]) & 0x7F800000) != 0x7F800000) {
+                const uint32_t h = double_to_half_rne(y[e]);
+                o[e >> 1] = (e & 1) ? (o[e >> 1] & 0xFFFFu) | (h << 16) : (o[e >> 1] & 0xFFFF0000u) | h;
+            }
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+__device__ __forceinline__ double row_sum16(double v)
+{
+#pragma unroll
+    for (int o = 8; o; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// What the lanes of one token's heads share: the angles' cosines and sines for a lane's elements
+struct Turn {
+    float c[8], s[8];                            // 8 pairs (half pairs) or 4 (neighbours: c[0..3], s[0..3])
+    int partner;                                 // lane that holds the other half of the pairs
+    bool turned, first;                          // this lane's elements are rotated; they are the first of their pairs
+};
+
+__device__ __forceinline__ void load_turn(Turn& t, const AppendArgs& p, int64_t pos, int lane)
+{
+    const int w = lane & 15, half = p.rot / 2;
+    t.turned = 8 * w < p.rot;
+    t.first = 8 * w < half;
+    t.partner = lane;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { t.c[e] = 1.f; t.s[e] = 0.f; }
+    if (!t.turned) return;
+    const int64_t row = pos < 0 ? 0 : pos < p.angle_rows ? pos : p.angle_rows - 1;
+    const float* at = p.angles + row * p.rot;
+    if (p.interleaved) {
+        const float4 c = reinterpret_cast<const float4*>(at)[w], s = reinterpret_cast<const float4*>(at + half)[w];
+        t.c[0] = c.x; t.c[1] = c.y; t.c[2] = c.z; t.c[3] = c.w;
+        t.s[0] = s.x; t.s[1] = s.y; t.s[2] = s.z; t.s[3] = s.w;
+    } else {
+        t.partner = t.first ? lane + p.rot / 16 : lane - p.rot / 16;
+        const int i = t.first ? 8 * w : 8 * w - half;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float4 c = reinterpret_cast<const float4*>(at + i)[e], s = reinterpret_cast<const float4*>(at + half + i)[e];
+            t.c[4 * e] = c.x; t.c[4 * e + 1] = c.y; t.c[4 * e + 2] = c.z; t.c[4 * e + 3] = c.w;
+            t.s[4 * e] = s.x; t.s[4 * e + 1] = s.y; t.s[4 * e + 2] = s.z; t.s[4 * e + 3] = s.w;
+        }
+    }
+}
+
+// one head of a token: every lane of the row takes part
+__device__ __forceinline__ uint4 turn_head(const uint4& raw, const Turn& t, const __half* gamma, const AppendArgs& p, int lane)
+{
+    if (!gamma && p.rot == 0) return raw;
+    const int w = lane & 15;
+    const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
+    float x[8];                                                            // x gamma
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)half_of(rw[e >> 1] >> (16 * (e & 1)));
+    double r = 1.0;
+    if (gamma) {
+        double sum = 0.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fma((double)x[e], (double)x[e], sum);
+        r = 1.0 / sqrt(row_sum16(sum) * (1.0 / kD) + p.eps);
+        const uint4 g4 = reinterpret_cast<const uint4*>(gamma)[w];
+        const uint32_t g[4] = {g4.x, g4.y, g4.z, g4.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= (float)half_of(g[e >> 1] >> (16 * (e & 1)));
+    }
+    double y[8];
+    if (p.interleaved) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const double a = x[2 * e], b = x[2 * e + 1], c = t.c[e], s = t.s[e];
+            y[2 * e] = fma(a, c, -(b * s));
+            y[2 * e + 1] = fma(b, c, a * s);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const double other = (double)__shfl(x[e], t.partner, 64) * (double)t.s[e];
+            y[e] = fma((double)x[e], (double)t.c[e], t.first ? -other : other);
+        }
+    }
+    if (gamma)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] *= r;
+    if (!gamma && !t.turned) return raw;                                   // (its bits, whatever they are)
+    return halves_of(y);
+}
+
+__global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs p)
+{
+    __shared__ uint4 s_block[4][16];                                       // per wave: the value codes of its quad
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = lane >> 4, w = lane & 15;
+    uint32_t item = blockIdx.x * 4 + (uint32_t)wave;
+    Turn turn;
+    if (item < p.kv_items) {
+        // keys and values: an aligned quad of token positions of one sequence, one KV head
+        const uint32_t slot = item / (uint32_t)p.Hkv;
+        const int h = (int)(item - slot * (uint32_t)p.Hkv);
+        const int b = count_before(p.B, lane, [&](int i) { return (uint32_t)(p.cu[i] >> 2) + 2u * (uint32_t)i <= slot; });
+        if (b >= p.B) return;
+        const int64_t row0 = p.cu[b], T = (int64_t)p.cu[b + 1] - row0, p0 = p.starts ? p.starts[b] : 0;
+        const int64_t j = (int64_t)slot - ((row0 >> 2) + 2 * (int64_t)b);
+        const int64_t pos = ((p0 >> 2) + j) * 4 + g, t = pos - p0, row = row0 + t;
+        const bool there = t >= 0 && t < T && row >= 0 && row < p.M;       // a token of the call
+        if (__builtin_amdgcn_ballot_w64(there) == 0) return;
+        const bool held = there && pos >= 0 && pos < (int64_t)p.width * kPageTokens;
+        const uint32_t id = held ? (uint32_t)p.table[(int64_t)b * p.width + pos / kPageTokens] : ~0u;
+        const bool valid = held && id < p.pages;
+        const int64_t at = there ? row : row0 > 0 && row0 < p.M ? row0 : 0;
+        const uint4 rk = reinterpret_cast<const uint4*>(p.k + at * p.k_stride + h * kD)[w];
+        const uint4 rv = reinterpret_cast<const uint4*>(p.v + at * p.v_stride + h * kD)[w];
+        load_turn(turn, p, pos, lane);
+        const uint4 k = turn_head(rk, turn, p.k_gamma, p, lane);
+        if (p.k_out && there) reinterpret_cast<uint4*>(p.k_out + row * p.k_out_stride + h * kD)[w] = k;
+        const uint64_t written = __builtin_amdgcn_ballot_w64(valid);
+        if (written == 0) return;
+        uint8_t* page = p.pool + ((int64_t)(valid ? id : 0) * p.Hkv + h) * kPageBytes;
+        const int tin = (int)(pos & (kPageTokens - 1));
+        write_token<false>(k, page, tin, w, lane, written == ~0ull, valid, s_block[wave]);
+        write_token<true>(rv, page, tin, w, lane, written == ~0ull, valid, s_block[wave]);
+        return;
+    }
+    // queries: four rows, a group of heads
+    item -= p.kv_items;
+    if (item >= p.q_items) return;
+    const uint32_t quad = item / p.q_groups, group = item - quad * p.q_groups;
+    int b = 0;
+    if (p.B <= 64) {
+        const int end = lane < p.B ? p.cu[lane + 1] : INT32_MAX;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = __popcll(__builtin_amdgcn_ballot_w64(end <= (int)(4 * quad + i)));
+            b = g == i ? c : b;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = count_before(p.B, lane, [&](int x) { return p.cu[x] <= (int)(4 * quad + i); });
+            b = g == i ? c : b;
+        }
+    }
+    const int64_t row = 4 * (int64_t)quad + g;
+    const int64_t row0 = b < p.B ? p.cu[b] : 0;
+    const bool there = b < p.B && row >= row0 && row < p.M;
+    const int64_t pos = (there && p.starts ? p.starts[b] : 0) + row - row0;
+    load_turn(turn, p, there ? pos : 0, lane);
+    const int64_t at = there ? row : 0;
+    const int h0 = (int)(group * p.q_heads), h1 = min(h0 + (int)p.q_heads, p.H);
+    const uint4* src = reinterpret_cast<const uint4*>(p.q + at * p.q_stride) + w;
+    uint4* dst = reinterpret_cast<uint4*>(p.q_out + at * p.q_out_stride) + w;
+    uint4 next = src[h0 * (kD / 8)];
+    for (int h = h0; h < h1; ++h) {
+        const uint4 raw = next;
+        next = src[min(h + 1, h1 - 1) * (kD / 8)];
+        const uint4 y = turn_head(raw, turn, p.q_gamma, p, lane);
+        if (there) dst[h * (kD / 8)] = y;
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// Tokens of the cache back as FP16, (code - z) s rounded once: one wave per aligned 16 positions of a sequence and KV head.
+// ------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint2 values_of(uint32_t c4, float z, float s)     // four codes in the low 16 bits
+{
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = ((float)((c4 >> (4 * j)) & 15u) + z) * s;
+    return make_uint2(__builtin_bit_cast(uint32_t, (h2){(_Float16)x[0], (_Float16)x[1]}), __builtin_bit_cast(uint32_t, (h2){(_Float16)x[2], (_Float16)x[3]}));
+}
+
+__global__ __launch_bounds__(256) void paged_gather_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ table,
+                                                           const int32_t* __restrict__ cu, const int32_t* __restrict__ starts,
+                                                           __half* __restrict__ k_out, __half* __restrict__ v_out, uint32_t pages, int width,
+                                                           int M, int B, int Hkv, uint32_t items)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = lane >> 4, w = lane & 15;
+    const uint32_t item = blockIdx.x * 4 + (uint32_t)wave;
+    if (item >= items) return;
+    const uint32_t slot = item / (uint32_t)Hkv;
+    const int h = (int)(item - slot * (uint32_t)Hkv);
+    const int b = count_before(B, lane, [&](int i) { return (uint32_t)(cu[i] >> 4) + 2u * (uint32_t)i <= slot; });
+    if (b >= B) return;
+    const int64_t row0 = cu[b], T = (int64_t)cu[b + 1] - row0, p0 = starts ? starts[b] : 0;
+    const int64_t j = (int64_t)slot - ((row0 >> 4) + 2 * (int64_t)b);
+    const int64_t pos0 = ((p0 >> 4) + j) * 16;                             // floor(p0 / 16) also for negative p0
+    if (pos0 >= p0 + T || pos0 + 16 <= p0) return;
+    const bool held = pos0 >= 0 && pos0 < (int64_t)width * kPageTokens;
+    const uint32_t id = held ? (uint32_t)table[(int64_t)b * width + pos0 / kPageTokens] : ~0u;
+    const bool on = id < pages;                                            // else zeros
+    const uint8_t* page = pool + ((int64_t)(on ? id : 0) * Hkv + h) * kPageBytes;
+    const int tin = (int)(pos0 & (kPageTokens - 1));
+    uint32_t kw[4], kp[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                                          // token 4 i + g, elements 8 w ..
+        kw[i] = on ? reinterpret_cast<const uint32_t*>(page + (tin + 4 * i + g) * (kD / 2))[w] : 0u;
+        kp[i] = on ? reinterpret_cast<const uint32_t*>(page + kCodeBytes)[tin + 4 * i + g] : 0xE4000000u;
+    }
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    const uint4 vc = on ? reinterpret_cast<const uint4*>(page + kHalfPage + tin * (kD / 2))[lane] : none;
+    const uint4 vp = on ? reinterpret_cast<const uint4*>(page + kHalfPage + kCodeBytes + tin * 4)[g]
+                        : make_uint4(0xE4000000u, 0xE4000000u, 0xE4000000u, 0xE4000000u);
+    auto there = [&](int64_t t) { return t >= 0 && t < T && row0 + t >= 0 && row0 + t < M; };
+    auto zero_of = [](uint32_t prm) { return (float)half_of(prm >> 16) + 1024.0f; };      // -z
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t t = pos0 + 4 * i + g - p0;
+        const float z = zero_of(kp[i]), s = (float)half_of(kp[i]);
+        // element 8w + 2j in nibble j of the low half, 8w + 2j + 1 of the high half
+        uint32_t lo = 0, hi = 0;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            lo |= ((kw[i] >> (4 * x)) & 15u) << (8 * x) | ((kw[i] >> (16 + 4 * x)) & 15u) << (8 * x + 4);
+            hi |= ((kw[i] >> (8 + 4 * x)) & 15u) << (8 * x) | ((kw[i] >> (24 + 4 * x)) & 15u) << (8 * x + 4);
+        }
+        const uint2 a = values_of(lo, z, s), c = values_of(hi, z, s);
+        if (there(t)) reinterpret_cast<uint4*>(k_out + ((row0 + t) * Hkv + h) * kD)[w] = make_uint4(a.x, a.y, c.x, c.y);
+    }
+    const uint32_t vw[4] = {vc.x, vc.y, vc.z, vc.w}, prm[4] = {vp.x, vp.y, vp.z, vp.w};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {                                          // token 4 g + x: dword 2u + (x >> 1), half x & 1
+        const int64_t t = pos0 + 4 * g + x - p0;
+        const float z = zero_of(prm[x]), s = (float)half_of(prm[x]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)                                        // elements 4 (w + 16 u) ..
+            if (there(t))
+                reinterpret_cast<uint2*>(v_out + ((row0 + t) * Hkv + h) * kD)[w + 16 * u] = values_of(vw[2 * u + (x >> 1)] >> (16 * (x & 1)), z, s);
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// Decode attention over pages.  The arithmetic of a chunk of 32 tokens is that of the contiguous cache's kernel (qoq_kv4.hip): both
+// products on the matrix cores, codes unpacked in registers, softmax in place.
+//
+// What a sequence's query sees is a list of chunks: those of the sinks, then those of the window (without a window all of them).
+// `ns` workgroups stand by for each (sequence, KV head); nwg of them attend, as many as give each wave at least `deal` chunks, and
+// their waves take the chunks in turn.  Unnormalised sums, maxima and weight sums meet in the workspace; the last workgroup to
+// arrive adds them up, in the order of the workgroups whichever arrives when, and leaves the counter at zero.
+// ------------------------------------------------------------------------------------------
+constexpr int kPartial = kD + 2;                         // floats per head: 128 sums, the maximum, the weight sum
+constexpr int kChunk = 32;                               // tokens per chunk: two tiles of 16 (divides the page)
+constexpr int kWaves = 4;
+constexpr int kMaxSplits = 32;
+
+struct DecodeArgs {
+    const __half* q;
+    const uint8_t* pool;
+    const int32_t* table;
+    const int32_t* seq_lens;
+    __half* out;
+    int* counters;
+    float* parts;
+    int64_t q_stride;
+    uint32_t pages;
+    int width, Hkv, R, ns, deal, window, sinks;
+};
+
+template <int PK, bool NT>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(PK == 1 ? 2 : 3))) void paged_decode_kernel(DecodeArgs p)
+{
+    extern __shared__ float s_part[];                    // [wave][column][kPartial]
+    __shared__ int s_last;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r16 = lane & 15, kb = lane >> 4;
+    const int R = p.R, head = PK == 2 ? r16 & 7 : r16;
+    const bool second = PK == 2 && r16 >= 8;
+    const uint32_t bh = blockIdx.x, b = bh / (uint32_t)p.Hkv, hk = bh - b * (uint32_t)p.Hkv;
+    const int split = blockIdx.y;
+
+    // what is seen: tokens below `first_end`, and from `lo` to L
+    const int L = min(max(p.seq_lens[b], 0), p.width * kPageTokens);
+    const int lo = p.window ? max(L - p.window, 0) : 0, sinks = p.sinks;
+    const int chunks = (L + kChunk - 1) / kChunk;
+    const int n_first = min((sinks + kChunk - 1) / kChunk, chunks);        // chunks of the sinks
+    const int gap = max(lo / kChunk - n_first, 0);                         // chunks behind them that nothing sees
+    const int n = chunks - gap;                                            // the list: i < n_first ? i : i + gap
+    const int nwg = min(p.ns, max(1, (n + kWaves * p.deal - 1) / (kWaves * p.deal)));
+    if (split >= nwg) return;
+    __half* out_bh = p.out + (size_t)bh * R * kD;
+    if (n == 0) {
+        for (int x = threadIdx.x; x < R * kD; x += 64 * kWaves) out_bh[x] = __float2half_rn(0.f);
+        return;
+    }
+    const int stride = nwg * kWaves, i0 = split * kWaves + wave;
+    const int n_iter = i0 < n ? (n - i0 + stride - 1) / stride : 0;
+    const int32_t* pages_of = p.table + (int64_t)b * p.width;
+
+    struct Chunk {
+        uint4 kc[2];        // keys: token r16 of the tile, elements 32 kb ..
+        uint4 vc[2];        // values: this lane's 16 bytes of the tile
+        uint32_t kz[2];     // (s, z) of token r16 (zero point for unpacking)
+        uint4 ks[2 / PK];   // (s, z) of tokens 4 kb .. 4 kb + 3 (scales of the scores this lane keeps)
+        uint4 vp[2];        // (s, z) of tokens 4 kb .. 4 kb + 3 of the values
+    };
+    const uint32_t off_kc = (uint32_t)(r16 * (kD / 2) + kb * 16), off_kz = (uint32_t)(kCodeBytes + r16 * 4);
+    const uint32_t off_ks = (uint32_t)(kCodeBytes + kb * 16 + (second ? 64 : 0)), off_vc = (uint32_t)(kHalfPage + lane * 16);
+    const uint32_t off_vp = (uint32_t)(kHalfPage + kCodeBytes + kb * 16);
+    auto code_words = [](const uint8_t* at) __attribute__((always_inline)) {
+        const uint4* x = reinterpret_cast<const uint4*>(at);
+        return NT ? load_nontemporal(x) : *x;
+    };
+    auto chunk_of = [&](int it) __attribute__((always_inline)) {           // of the wave's it-th turn; past its last one, the last of the list
+        const int i = min(i0 + it * stride, n - 1);
+        return __builtin_amdgcn_readfirstlane(i < n_first ? i : i + gap);
+    };
+    auto page_of = [&](int it) __attribute__((always_inline)) { return (uint32_t)pages_of[chunk_of(it) >> 1]; };
+    auto load_chunk = [&](Chunk& c, int chunk, uint32_t id) __attribute__((always_inline)) {
+        const uint32_t held = id < p.pages ? id : 0;                       // (no page: any, and nothing of it counts)
+        const uint8_t* page = p.pool + ((int64_t)held * p.Hkv + hk) * kPageBytes;
+        const int tin = (chunk & 1) * kChunk;
+        const uint8_t* codes = page + tin * (kD / 2);
+        const uint8_t* prm = page + tin * 4;
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            c.kc[tt] = code_words(codes + tt * 1024 + off_kc);
+            c.kz[tt] = *reinterpret_cast<const uint32_t*>(prm + tt * 64 + off_kz);
+            if (tt < 2 / PK) c.ks[tt] = *reinterpret_cast<const uint4*>(prm + tt * 64 + off_ks);
+        }
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            c.vc[tt] = code_words(codes + tt * 1024 + off_vc);
+            c.vp[tt] = *reinterpret_cast<const uint4*>(prm + tt * 64 + off_vp);
+        }
+    };
+    Chunk A, Bf;
+    uint32_t id_a = page_of(0), id_b = page_of(1);
+    load_chunk(A, chunk_of(0), id_a);
+
+    // B operand of S = K q^T: column = head (both halves of the columns with PK = 2; heads >= R: zero), k-block kb = elements 32 kb ..
+    h2 qv[16];
+    {
+        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_stride + ((int)hk * R + min(head, R - 1)) * kD + kb * 32);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint4 t = src[e];
+            const uint32_t u[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) qv[4 * e + x] = __builtin_bit_cast(h2, head < R ? u[x] : 0u);
+        }
+    }
+
+    float m = -1e30f, l = 0.f;                           // of this lane's column, over the tokens it has seen
+    f4 acc[8];                                           // acc[4u + j][x]: element d = 16 kb + 4x + 64u + j of the column
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = (f4){0.f, 0.f, 0.f, 0.f};
+    const float kScale = 1.4426950408889634f * 0.08838834764831845f;      // log2(e) / sqrt(128)
+    const h2 k960 = {(_Float16)960.0f, (_Float16)960.0f};
+
+    // One chunk of arithmetic.  MASKED: not all of its tokens are seen; the parameters of those that are not are whatever the
+    // cache holds and must not enter the arithmetic.
+    auto process_as = [&](const Chunk& cur, int chunk, bool held, auto masked_tag) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(masked_tag)::value;
+        constexpr int NS = 2 / PK;
+        const int own = chunk * kChunk + (second ? 16 : 0) + 4 * kb;       // first token of the lane's (first) score vector
+        const int end = held ? L : 0, end_first = held ? sinks : 0;
+        auto seen = [&](int t) { return t < end && (t >= lo || t < end_first); };
+        f4 d[2];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            uint32_t kz = cur.kz[tt];
+            if (MASKED) kz = seen(chunk * kChunk + tt * 16 + r16) ? kz : 0xE4000000u;   // -(1024 + 0)
+            const h2 c = __builtin_bit_cast(h2, __builtin_amdgcn_perm(kz, kz, 0x07060706u));   // high half in both halves
+            const h2 c16 = c + k960;
+            const uint32_t kw[4] = {cur.kc[tt].x, cur.kc[tt].y, cur.kc[tt].z, cur.kc[tt].w};
+            d[tt] = (f4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                h2 kh[4];
+                unpack4(kw[w], c, c16, kh);              // kh[j] = elements 8w + 2j, 8w + 2j + 1 of this lane's 32
+                d[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(kh[0], kh[1], kh[2], kh[3]),
+                                                               join(qv[4 * w], qv[4 * w + 1], qv[4 * w + 2], qv[4 * w + 3]), d[tt], 0, 0, 0);
+            }
+        }
+        f4 sc[NS];                                       // [x] = token own + x (+ 16 for the second vector)
+        if (PK == 2) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) sc[0][x] = second ? d[1][x] : d[0][x];
+        } else {
+#pragma unroll
+            for (int tt = 0; tt < NS; ++tt) sc[tt] = d[tt];
+        }
+        float m_new = m;
+#pragma unroll
+        for (int tt = 0; tt < NS; ++tt) {
+            const uint32_t sw[4] = {cur.ks[tt].x, cur.ks[tt].y, cur.ks[tt].z, cur.ks[tt].w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                sc[tt][x] *= (float)half_of(sw[x]) * kScale;
+                if (MASKED) sc[tt][x] = seen(own + tt * 16 + x) ? sc[tt][x] : -1e30f;
+                m_new = fmaxf(m_new, sc[tt][x]);
+            }
+        }
+        m_new = fmaxf(m_new, __shfl_xor(m_new, 16, 64));  // the four k-blocks of a column agree on the maximum
+        m_new = fmaxf(m_new, __shfl_xor(m_new, 32, 64));
+        if (__builtin_amdgcn_ballot_w64(m_new != m) != 0) {                  // rare once a few chunks have been seen
+            const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= alpha;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] *= alpha;
+        }
+        uint32_t pw[2][4];                               // (s, z) of the values, tokens 4 kb .. of both tiles
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            const uint32_t w4[4] = {cur.vp[tt].x, cur.vp[tt].y, cur.vp[tt].z, cur.vp[tt].w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) pw[tt][x] = !MASKED || seen(chunk * kChunk + tt * 16 + 4 * kb + x) ? w4[x] : 0xE4000000u;   // else scale 0, zero point 0
+        }
+        uint32_t bw[2][2];                               // B operand: softmax weight * value scale, tokens 4 kb .. of both tiles
+#pragma unroll
+        for (int tt = 0; tt < NS; ++tt) {
+            float wf[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                // a masked score is -1e30: its weight underflows to 0 unless nothing has been seen yet (then m is -1e30 too),
+                // which the zero scale takes care of
+                const float pr = __builtin_amdgcn_exp2f(sc[tt][x] - m);
+                l += MASKED ? (seen(own + tt * 16 + x) ? pr : 0.f) : pr;
+                wf[x] = pr * (float)half_of(PK == 2 ? (second ? pw[1][x] : pw[0][x]) : pw[tt][x]);
+            }
+            const uint32_t b_lo = __builtin_bit_cast(uint32_t, (h2){(_Float16)wf[0], (_Float16)wf[1]});
+            const uint32_t b_hi = __builtin_bit_cast(uint32_t, (h2){(_Float16)wf[2], (_Float16)wf[3]});
+            if (PK == 2) {                               // a column takes part with its own tile only
+                bw[0][0] = second ? 0u : b_lo; bw[0][1] = second ? 0u : b_hi;
+                bw[1][0] = second ? b_lo : 0u; bw[1][1] = second ? b_hi : 0u;
+            } else {
+                bw[tt][0] = b_lo; bw[tt][1] = b_hi;
+            }
+        }
+        h2 vh[2][2][2][4];                               // [tile][u][h][j]: (token 4 kb + 2h, + 1) of element 4 (r16 + 16 u) + j
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            const uint32_t vw[4] = {cur.vc[tt].x, cur.vc[tt].y, cur.vc[tt].z, cur.vc[tt].w};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const h2 c = __builtin_bit_cast(h2, __builtin_amdgcn_perm(pw[tt][2 * h + 1], pw[tt][2 * h], 0x07060302u));
+                const h2 c16 = c + k960;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) unpack4(vw[2 * u + h], c, c16, vh[tt][u][h]);
+            }
+        }
+        const h8 b8 = join(__builtin_bit_cast(h2, bw[0][0]), __builtin_bit_cast(h2, bw[0][1]), __builtin_bit_cast(h2, bw[1][0]),
+                           __builtin_bit_cast(h2, bw[1][1]));
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                acc[4 * u + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(vh[0][u][0][j], vh[0][u][1][j], vh[1][u][0][j], vh[1][u][1][j]),
+                                                                        b8, acc[4 * u + j], 0, 0, 0);
+    };
+    auto process = [&](const Chunk& cur, int it, uint32_t id) __attribute__((always_inline)) {
+        const int chunk = chunk_of(it), t0 = chunk * kChunk, t1 = t0 + kChunk;
+        const bool held = id < p.pages;
+        if (held && t1 <= L && (t0 >= lo || t1 <= sinks)) process_as(cur, chunk, true, std::false_type{});
+        else process_as(cur, chunk, held, std::true_type{});
+    };
+
+    int it = 0;
+    for (; it + 2 < n_iter; it += 2) {
+        load_chunk(Bf, chunk_of(it + 1), id_b);
+        const uint32_t now = id_a;
+        id_a = page_of(it + 2);
+        process(A, it, now);
+        load_chunk(A, chunk_of(it + 2), id_a);
+        const uint32_t then = id_b;
+        id_b = page_of(it + 3);
+        process(Bf, it + 1, then);
+    }
+    if (it + 2 == n_iter) {
+        load_chunk(Bf, chunk_of(it + 1), id_b);
+        process(A, it, id_a);
+        process(Bf, it + 1, id_b);
+    } else if (n_iter > 0) {
+        process(A, it, id_a);
+    }
+
+    // ---- the partial results of the waves (and of the column halves) meet in LDS --------------
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    const int columns = PK * R;
+    if (head < R) {
+        float* part = s_part + (wave * columns + (second ? R : 0) + head) * kPartial;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) part[16 * kb + 4 * x + 64 * u + j] = acc[4 * u + j][x];
+        if (kb == 0) { part[kD] = m; part[kD + 1] = l; }
+    }
+    __syncthreads();
+    constexpr int N = kWaves * PK;                       // partial results of a head
+    float* mine = p.parts + ((size_t)bh * p.ns + split) * R * kPartial;
+    for (int x = threadIdx.x; x < R * kD; x += 64 * kWaves) {
+        const int r = x / kD, d = x % kD;
+        const float* part = s_part + r * kPartial;
+        float mm = -1e30f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) mm = fmaxf(mm, part[i * R * kPartial + kD]);
+        float num = 0.f, den = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float f = __builtin_amdgcn_exp2f(part[i * R * kPartial + kD] - mm);
+            num = fmaf(part[i * R * kPartial + d], f, num);
+            den = fmaf(part[i * R * kPartial + kD + 1], f, den);
+        }
+        if (nwg == 1) {
+            out_bh[x] = __float2half_rn(den > 0.f ? num / den : num);      // nothing seen: zero (NaN stays)
+        } else {
+            __hip_atomic_store(mine + r * kPartial + d, num, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (d == 0) {
+                __hip_atomic_store(mine + r * kPartial + kD, mm, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_store(mine + r * kPartial + kD + 1, den, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
+    }
+    if (nwg == 1) return;
+    // The stores above went past the caches that other workgroups do not share; they have arrived when the counter is raised.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int old = __hip_atomic_fetch_add(p.counters + bh, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_last = old == nwg - 1;
+        if (old == nwg - 1) __hip_atomic_store(p.counters + bh, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!s_last) return;
+    const float* parts = p.parts + (size_t)bh * p.ns * R * kPartial;
+    for (int x = threadIdx.x; x < R * kD; x += 64 * kWaves) {
+        const int r = x / kD, d = x % kD;
+        float mm = -1e30f, num = 0.f, den = 0.f;
+        for (int s0 = 0; s0 < nwg; s0 += 8) {
+            float a[8], ms[8], ls[8];
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                float* at = const_cast<float*>(parts) + ((size_t)min(s0 + s, nwg - 1) * R + r) * kPartial;
+                a[s] = __hip_atomic_load(at + d, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                ms[s] = __hip_atomic_load(at + kD, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                ls[s] = __hip_atomic_load(at + kD + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            float top = mm;
+#pragma unroll
+            for (int s = 0; s < 8; ++s) top = fmaxf(top, ms[s]);
+            const float keep = __builtin_amdgcn_exp2f(mm - top);
+            num *= keep; den *= keep; mm = top;
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const float f = s0 + s < nwg ? __builtin_amdgcn_exp2f(ms[s] - top) : 0.f;
+                num = fmaf(a[s], f, num);
+                den = fmaf(ls[s], f, den);
+            }
+        }
+        out_bh[x] = __float2half_rn(den > 0.f ? num / den : num);
+    }
+}
+
+}  // namespace
+
+int64_t kv4_page_bytes(int64_t Hkv) { return Hkv * kPageBytes; }
+
+hipError_t launch_rope_append(const RopeAppend& a, hipStream_t s)
+{
+    AppendArgs p{};
+    p.q = static_cast<const __half*>(a.q); p.k = static_cast<const __half*>(a.k); p.v = static_cast<const __half*>(a.v);
+    p.q_stride = a.q_stride; p.k_stride = a.k_stride; p.v_stride = a.v_stride;
+    p.q_gamma = static_cast<const __half*>(a.q_gamma); p.k_gamma = static_cast<const __half*>(a.k_gamma);
+    p.eps = a.eps;
+    p.angles = a.angles; p.angle_rows = (int)a.angle_rows; p.rot = (int)a.rot; p.interleaved = a.interleaved;
+    p.cu = a.cu; p.starts = a.starts;
+    p.M = (int)a.M; p.B = (int)a.B; p.H = (int)a.H; p.Hkv = (int)a.Hkv;
+    p.pool = a.pool; p.pages = (uint32_t)a.pages; p.table = a.table; p.width = (int)a.width;
+    p.q_out = static_cast<__half*>(a.q_out); p.k_out = static_cast<__half*>(a.k_out);
+    p.q_out_stride = a.q_out_stride; p.k_out_stride = a.k_out_stride;
+    const int64_t slots = a.M / 4 + 2 * a.B;             // a sequence of T tokens touches at most (T + 2) / 4 + 1 aligned quads
+    const int64_t quads = (a.M + 3) / 4;
+    p.q_heads = 1;
+    while (p.q_heads < 8 && quads * a.H / (2 * p.q_heads) >= 4096) p.q_heads *= 2;
+    p.q_groups = (uint32_t)((a.H + p.q_heads - 1) / p.q_heads);
+    const int64_t kv_items = slots * a.Hkv, q_items = p.q ? quads * p.q_groups : 0;
+    if (kv_items + q_items >= (int64_t)1 << 31) return hipErrorInvalidValue;
+    p.kv_items = (uint32_t)kv_items; p.q_items = (uint32_t)q_items;
+    rope_append_kernel<<<(unsigned)((kv_items + q_items + 3) / 4), 256, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_gather(const uint8_t* pool, int64_t pages, const int32_t* table, int64_t width, const int32_t* cu,
+                               const int32_t* starts, int64_t M, int64_t B, int64_t Hkv, void* k_out, void* v_out, hipStream_t s)
+{
+    const int64_t items = (M / 16 + 2 * B) * Hkv;
+    if (items >= (int64_t)1 << 31) return hipErrorInvalidValue;
+    paged_gather_kernel<<<(unsigned)((items + 3) / 4), 256, 0, s>>>(pool, table, cu, starts, static_cast<__half*>(k_out), static_cast<__half*>(v_out),
+                                                                     (uint32_t)pages, (int)width, (int)M, (int)B, (int)Hkv, (uint32_t)items);
+    return hipGetLastError();
+}
+
+// Workgroups that stand by for each (sequence, KV head), and the tokens that a query can see at most
+static int64_t most_seen(int64_t width, int64_t window, int64_t sinks)
+{
+    const int64_t S = width * kPageTokens;
+    return window ? std::min(S, window + sinks) : S;
+}
+constexpr int kDeal = 2;                                 // chunks that a wave is given before another workgroup attends
+static int paged_splits(int64_t B, int64_t Hkv, int64_t width, int64_t window, int64_t sinks)
+{
+    const int64_t pairs = B * Hkv;
+    if (pairs <= 0 || pairs > kMaxCounters) return 1;
+    int64_t ns = 512 / pairs;
+    ns = std::min<int64_t>(ns, kMaxSplits);
+    ns = std::min<int64_t>(ns, (most_seen(width, window, sinks) + kChunk * kWaves * kDeal - 1) / (kChunk * kWaves * kDeal));
+    return (int)std::max<int64_t>(ns, 1);
+}
+
+size_t paged_decode_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t width, int64_t window, int64_t sinks)
+{
+    const int ns = paged_splits(B, Hkv, width, window, sinks);
+    return ns <= 1 ? 0 : kCounterBytes + ((size_t)(B * H) * ns * kPartial * sizeof(float) + 15) / 16 * 16;
+}
+
+hipError_t launch_paged_decode(const void* q, int64_t q_stride, const uint8_t* pool, int64_t pages, const int32_t* table, int64_t width,
+                               const int32_t* seq_lens, int64_t B, int64_t H, int64_t Hkv, int64_t window, int64_t sinks, void* out,
+                               void* workspace, hipStream_t s)
+{
+    DecodeArgs p{};
+    p.q = static_cast<const __half*>(q); p.q_stride = q_stride;
+    p.pool = pool; p.pages = (uint32_t)pages; p.table = table; p.width = (int)width;
+    p.seq_lens = seq_lens;
+    p.out = static_cast<__half*>(out);
+    p.Hkv = (int)Hkv; p.R = (int)(H / Hkv);
+    p.ns = workspace ? paged_splits(B, Hkv, width, window, sinks) : 1;
+    p.deal = kDeal;
+    p.window = (int)window; p.sinks = window ? (int)sinks : 0;
+    p.counters = static_cast<int*>(workspace);
+    p.parts = workspace ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes) : nullptr;
+    const bool nt = B * Hkv * most_seen(width, window, sinks) / kPageTokens * kPageBytes >= (int64_t)24 << 20;
+    const dim3 grid((unsigned)(B * Hkv), (unsigned)p.ns);
+    const int PK = p.R <= 8 ? 2 : 1;
+    const size_t lds = (size_t)kWaves * PK * p.R * kPartial * sizeof(float);
+    auto* kernel = PK == 2 ? (nt ? paged_decode_kernel<2, true> : paged_decode_kernel<2, false>)
+                           : (nt ? paged_decode_kernel<1, true> : paged_decode_kernel<1, false>);
+    kernel<<<grid, 64 * kWaves, lds, s>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace qoq

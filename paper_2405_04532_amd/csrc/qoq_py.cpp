@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include <ATen/ops/empty.h>
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -39,7 +40,7 @@ const at::Tensor* dev_tensor(PyObject* o, at::ScalarType dtype, const char* name
 {
     const at::Tensor* t = tensor(o, name);
     if (!t || (t->is_cuda() && t->scalar_type() == dtype && t->is_contiguous())) return t;
-    const char* type = dtype == at::kHalf ? "torch.float16" : dtype == at::kChar ? "torch.int8" : dtype == at::kInt ? "torch.int32" : "torch.float32";
+    const char* type = dtype == at::kHalf ? "torch.float16" : dtype == at::kChar ? "torch.int8" : dtype == at::kInt ? "torch.int32" : dtype == at::kByte ? "torch.uint8" : "torch.float32";
     PyErr_Format(PyExc_TypeError, "%s: expected a contiguous %s tensor on the GPU", name, type);
     return nullptr;
 }
@@ -389,6 +390,253 @@ PyObject* kv4_attention_decode(PyObject*, PyObject* const* a, Py_ssize_t n)    /
     END_HANDLE_TH_ERRORS
 }
 
+// ---- paged cache and prompt attention: every tensor of a call lies on one GPU, which is the current one while the call launches ----
+
+// heads of tokens: FP16 [rows, heads, 128] on `device`, contiguous but for the stride from token to token
+const at::Tensor* heads_tensor(PyObject* o, const char* name, int device)
+{
+    const at::Tensor* t = tensor(o, name);
+    if (!t) return nullptr;
+    if (!t->is_cuda() || t->scalar_type() != at::kHalf) {
+        PyErr_Format(PyExc_TypeError, "%s: expected a torch.float16 tensor on the GPU", name);
+        return nullptr;
+    }
+    if (!has_dims(*t, 3, name)) return nullptr;
+    if (device >= 0 && t->get_device() != device) {
+        PyErr_Format(PyExc_ValueError, "%s: expected on the GPU of the other tensors", name);
+        return nullptr;
+    }
+    if (t->size(2) != 128 || (t->stride(2) != 1 && t->numel()) || (t->stride(1) != 128 && t->size(1) > 1 && t->numel())) {
+        PyErr_Format(PyExc_ValueError, "%s: expected [rows, heads, 128] with contiguous heads", name);
+        return nullptr;
+    }
+    return t;
+}
+// elements from token to token; a single token's stride means nothing
+int64_t token_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : (t.size(1) * 128 + 7) / 8 * 8; }
+
+bool have_shape(const at::Tensor& t, at::IntArrayRef shape, const char* name)
+{
+    if (t.sizes() == shape) return true;
+    PyErr_Format(PyExc_ValueError, "%s: unexpected shape", name);
+    return false;
+}
+
+// a contiguous tensor of this type and number of dimensions on `device`
+const at::Tensor* dense(PyObject* o, at::ScalarType dtype, int64_t dims, const char* name, int device)
+{
+    const at::Tensor* t = dev_tensor(o, dtype, name);
+    if (!t || !has_dims(*t, dims, name)) return nullptr;
+    if (t->get_device() == device) return t;
+    PyErr_Format(PyExc_ValueError, "%s: expected on the GPU of the other tensors", name);
+    return nullptr;
+}
+
+// None, or as above
+bool dense_or_none(PyObject* o, at::ScalarType dtype, int64_t dims, const char* name, int device, const at::Tensor** t)
+{
+    *t = nullptr;
+    return o == Py_None || (*t = dense(o, dtype, dims, name, device)) != nullptr;
+}
+
+struct Pool {
+    const at::Tensor *bytes, *table;
+    int64_t pages, width;
+    bool ready(PyObject* pool, PyObject* block_table, int64_t B, int64_t Hkv, int device)
+    {
+        bytes = dense(pool, at::kByte, 1, "pool", device);
+        table = bytes ? dense(block_table, at::kInt, 2, "block_table", device) : nullptr;
+        if (!table) return false;
+        if (table->size(0) != B) {
+            PyErr_SetString(PyExc_ValueError, "block_table: expected a row for each sequence");
+            return false;
+        }
+        const size_t page = qoq_kv4_pool_bytes(1, Hkv, 128);
+        pages = page ? (int64_t)((size_t)bytes->numel() / page) : 0;      // none: refused by the call
+        width = table->size(1);
+        return true;
+    }
+};
+
+struct Scratch {
+    void* ptr = nullptr;
+    size_t bytes = 0;
+    bool ready(PyObject* o, int device)
+    {
+        if (o == Py_None) return true;
+        const at::Tensor* t = tensor(o, "workspace");
+        if (!t) return false;
+        if (!t->is_cuda() || t->get_device() != device || !t->is_contiguous()) {
+            PyErr_SetString(PyExc_TypeError, "workspace: expected a contiguous tensor on the GPU of the other tensors");
+            return false;
+        }
+        ptr = t->data_ptr();
+        bytes = (size_t)t->numel() * t->element_size();
+        return true;
+    }
+};
+
+// q, k, v, pool, block_table, cu, starts, angles, q_gamma, k_gamma, eps, interleaved, q_out, k_out, want_k
+PyObject* qk_rope_kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (!counted(n, 15)) return nullptr;
+    const at::Tensor* k = heads_tensor(a[1], "k", -1);
+    if (!k) return nullptr;
+    const int dev = k->get_device();
+    const at::Tensor* v = heads_tensor(a[2], "v", dev);
+    if (!v) return nullptr;
+    const at::Tensor* q = nullptr;
+    if (a[0] != Py_None && !(q = heads_tensor(a[0], "q", dev))) return nullptr;
+    const at::Tensor* cu = dense(a[5], at::kInt, 1, "cu", dev);
+    if (!cu) return nullptr;
+    const int64_t M = k->size(0), Hkv = k->size(1), H = q ? q->size(1) : 0, B = cu->numel() - 1;
+    if (!have_shape(*v, {M, Hkv, 128}, "v") || (q && !have_shape(*q, {M, H, 128}, "q"))) return nullptr;
+    const at::Tensor *starts, *angles, *qg, *kg;
+    Pool pool;
+    double eps;
+    bool interleaved, want_k;
+    if (!dense_or_none(a[6], at::kInt, 1, "starts", dev, &starts) || (starts && !have_shape(*starts, {B}, "starts")) ||
+        !dense_or_none(a[7], at::kFloat, 2, "angles", dev, &angles) || !dense_or_none(a[8], at::kHalf, 1, "q_gamma", dev, &qg) ||
+        (qg && !have_shape(*qg, {128}, "q_gamma")) || !dense_or_none(a[9], at::kHalf, 1, "k_gamma", dev, &kg) ||
+        (kg && !have_shape(*kg, {128}, "k_gamma")) || !pool.ready(a[3], a[4], B, Hkv, dev) || !number(a[10], &eps) || !flag(a[11], &interleaved) ||
+        !flag(a[14], &want_k))
+        return nullptr;
+    c10::hip::HIPGuard guard(static_cast<c10::DeviceIndex>(dev));
+    at::Tensor q_out, k_out;
+    if (a[12] != Py_None) {
+        const at::Tensor* t = heads_tensor(a[12], "q_out", dev);
+        if (!t || !have_shape(*t, {M, H, 128}, "q_out")) return nullptr;
+        q_out = *t;
+    } else if (q) {
+        q_out = new_like(*q, {M, H, 128}, at::kHalf);
+    }
+    if (a[13] != Py_None) {
+        const at::Tensor* t = heads_tensor(a[13], "k_out", dev);
+        if (!t || !have_shape(*t, {M, Hkv, 128}, "k_out")) return nullptr;
+        k_out = *t;
+    } else if (want_k) {
+        k_out = new_like(*k, {M, Hkv, 128}, at::kHalf);
+    }
+    void* s = stream_of(*k);
+    auto at_or_null = [](const at::Tensor* t) { return t ? t->data_ptr() : nullptr; };
+    const void *qp = at_or_null(q), *kp = k->data_ptr(), *vp = v->data_ptr(), *qgp = at_or_null(qg), *kgp = at_or_null(kg);
+    const float* ap = static_cast<const float*>(at_or_null(angles));
+    const int32_t *cp = static_cast<const int32_t*>(cu->data_ptr()), *sp = static_cast<const int32_t*>(at_or_null(starts));
+    const int32_t* tp = static_cast<const int32_t*>(pool.table->data_ptr());
+    void *pp = pool.bytes->data_ptr(), *qo = q_out.defined() ? q_out.data_ptr() : nullptr, *ko = k_out.defined() ? k_out.data_ptr() : nullptr;
+    const int64_t qs = q ? token_stride(*q) : 0, ks = token_stride(*k), vs = token_stride(*v), qos = q_out.defined() ? token_stride(q_out) : 0,
+                  kos = k_out.defined() ? token_stride(k_out) : 0, rows = angles ? angles->size(0) : 0, rot = angles ? angles->size(1) : 0;
+    if (!call([&] {
+            return qoq_qk_rope_kv4_append(qp, qs, kp, ks, vp, vs, qgp, kgp, eps, ap, rows, rot, interleaved, cp, sp, M, B, H, Hkv, 128, pp, pool.pages, tp,
+                                          pool.width, qo, qos, ko, kos, s);
+        }))
+        return nullptr;
+    return Py_BuildValue("NN", Quantized::wrap(q_out), Quantized::wrap(k_out));
+    END_HANDLE_TH_ERRORS
+}
+
+// the caller's tensor of this shape, contiguous, or a new one
+bool dense_or_new(PyObject* o, const at::Tensor& on, at::IntArrayRef shape, const char* name, at::Tensor& t)
+{
+    if (o == Py_None) {
+        t = new_like(on, shape, at::kHalf);
+        return true;
+    }
+    const at::Tensor* given = dense(o, at::kHalf, (int64_t)shape.size(), name, on.get_device());
+    if (!given || !have_shape(*given, shape, name)) return false;
+    t = *given;
+    return true;
+}
+
+PyObject* kv4_paged_gather(PyObject*, PyObject* const* a, Py_ssize_t n)    // pool, block_table, cu, starts, rows, Hkv, k_out, v_out
+{
+    HANDLE_TH_ERRORS
+    if (!counted(n, 8)) return nullptr;
+    const at::Tensor* cu = dev_tensor(a[2], at::kInt, "cu");
+    if (!cu || !has_dims(*cu, 1, "cu")) return nullptr;
+    const int dev = cu->get_device();
+    const int64_t B = cu->numel() - 1;
+    const at::Tensor* starts;
+    int64_t M, Hkv;
+    Pool pool;
+    if (!dense_or_none(a[3], at::kInt, 1, "starts", dev, &starts) || (starts && !have_shape(*starts, {B}, "starts")) || !integer(a[4], &M) ||
+        !integer(a[5], &Hkv) || !pool.ready(a[0], a[1], B, Hkv, dev))
+        return nullptr;
+    c10::hip::HIPGuard guard(static_cast<c10::DeviceIndex>(dev));
+    at::Tensor k, v;
+    if (M < 0 || Hkv < 0) return call([] { return (int)QOQ_ERR_SHAPE; }), nullptr;
+    if (!dense_or_new(a[6], *cu, {M, Hkv, 128}, "k_out", k) || !dense_or_new(a[7], *cu, {M, Hkv, 128}, "v_out", v)) return nullptr;
+    void *s = stream_of(*cu), *kp = k.data_ptr(), *vp = v.data_ptr();
+    const void* pp = pool.bytes->data_ptr();
+    const int32_t *tp = static_cast<const int32_t*>(pool.table->data_ptr()), *cp = static_cast<const int32_t*>(cu->data_ptr());
+    const int32_t* sp = starts ? static_cast<const int32_t*>(starts->data_ptr()) : nullptr;
+    if (!call([&] { return qoq_kv4_paged_gather(pp, pool.pages, tp, pool.width, cp, sp, M, B, Hkv, 128, kp, vp, s); })) return nullptr;
+    return Py_BuildValue("NN", THPVariable_Wrap(k), THPVariable_Wrap(v));
+    END_HANDLE_TH_ERRORS
+}
+
+// q, pool, block_table, seq_lens, Hkv, window, sinks, out, workspace
+PyObject* kv4_paged_attention_decode(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (!counted(n, 9)) return nullptr;
+    const at::Tensor* q = heads_tensor(a[0], "q", -1);
+    if (!q) return nullptr;
+    const int dev = q->get_device();
+    const int64_t B = q->size(0), H = q->size(1);
+    const at::Tensor* lens = dense(a[3], at::kInt, 1, "seq_lens", dev);
+    int64_t Hkv, window, sinks;
+    Pool pool;
+    Scratch ws;
+    at::Tensor out;
+    if (!lens || !have_shape(*lens, {B}, "seq_lens") || !integer(a[4], &Hkv) || !integer(a[5], &window) || !integer(a[6], &sinks) ||
+        !pool.ready(a[1], a[2], B, Hkv, dev) || !ws.ready(a[8], dev))
+        return nullptr;
+    c10::hip::HIPGuard guard(static_cast<c10::DeviceIndex>(dev));
+    if (!dense_or_new(a[7], *q, {B, H, 128}, "out", out)) return nullptr;
+    void *s = stream_of(*q), *op = out.data_ptr();
+    const void *qp = q->data_ptr(), *pp = pool.bytes->data_ptr();
+    const int32_t *tp = static_cast<const int32_t*>(pool.table->data_ptr()), *lp = static_cast<const int32_t*>(lens->data_ptr());
+    const int64_t stride = token_stride(*q);
+    if (!call([&] {
+            return qoq_kv4_paged_attention_decode(qp, stride, pp, pool.pages, tp, pool.width, lp, B, H, Hkv, 128, window, sinks, op, ws.ptr, ws.bytes, s);
+        }))
+        return nullptr;
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* attention_prefill(PyObject*, PyObject* const* a, Py_ssize_t n)    // q, k, v, cu_q, cu_k, window, sinks, out, workspace
+{
+    HANDLE_TH_ERRORS
+    if (!counted(n, 9)) return nullptr;
+    const at::Tensor* q = heads_tensor(a[0], "q", -1);
+    if (!q) return nullptr;
+    const int dev = q->get_device();
+    const at::Tensor* k = heads_tensor(a[1], "k", dev);
+    const at::Tensor* v = k ? heads_tensor(a[2], "v", dev) : nullptr;
+    const at::Tensor* cu_q = v ? dense(a[3], at::kInt, 1, "cu_q", dev) : nullptr;
+    const at::Tensor* cu_k = cu_q ? dense(a[4], at::kInt, 1, "cu_k", dev) : nullptr;
+    int64_t window, sinks;
+    Scratch ws;
+    at::Tensor out;
+    if (!cu_k || !have_shape(*v, k->sizes(), "v") || !have_shape(*cu_k, cu_q->sizes(), "cu_k") || !integer(a[5], &window) || !integer(a[6], &sinks) ||
+        !ws.ready(a[8], dev))
+        return nullptr;
+    const int64_t M = q->size(0), H = q->size(1), Mk = k->size(0), Hkv = k->size(1), B = cu_q->numel() - 1;
+    c10::hip::HIPGuard guard(static_cast<c10::DeviceIndex>(dev));
+    if (!dense_or_new(a[7], *q, {M, H, 128}, "out", out)) return nullptr;
+    void *s = stream_of(*q), *op = out.data_ptr();
+    const void *qp = q->data_ptr(), *kp = k->data_ptr(), *vp = v->data_ptr();
+    const int32_t *cq = static_cast<const int32_t*>(cu_q->data_ptr()), *ck = static_cast<const int32_t*>(cu_k->data_ptr());
+    const int64_t qs = token_stride(*q), ks = token_stride(*k), vs = token_stride(*v);
+    if (!call([&] { return qoq_attention_prefill(qp, qs, kp, ks, vp, vs, cq, ck, M, Mk, B, H, Hkv, 128, window, sinks, op, ws.ptr, ws.bytes, s); }))
+        return nullptr;
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject* set_raise_status(PyObject*, PyObject* f)
 {
     Py_INCREF(f);
@@ -435,6 +683,7 @@ PyObject* channel_order(PyObject*, PyObject* const* a, Py_ssize_t n)    // salie
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(quant_act), FAST(quant_act_reordered), FAST(rmsnorm_quant), FAST(silu_mul_quant), FAST(w4a8_gemm),
                          FAST(w4a8_gemm_noalloc), FAST(w4a8_gemm_token_sum), FAST(w4a8_linear), FAST(kv4_append), FAST(kv4_attention_decode), FAST(channel_order),
+                         FAST(qk_rope_kv4_append), FAST(kv4_paged_gather), FAST(kv4_paged_attention_decode), FAST(attention_prefill),
                          {"set_raise_status", set_raise_status, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 #undef FAST
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_qoq_py", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

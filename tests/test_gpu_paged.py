@@ -1,0 +1,536 @@
+"""The paged KV4 cache and prompt attention on the GPU against the float64 oracle.
+
+Queries and keys after norm and rotation, codes, scales and zeros are bit-exact.  Attention is bounded term by term:
+    |got - ref| <= 2^-11 |ref|                      the result's rounding to FP16
+                 + 2^-11 sum_t p_t |v_t|            every softmax weight's (decode: weight times value scale's), half a step each
+                 + (2 e + 2^-20) sum_t p_t |v_t|    errors e of the scores, in weights and in their sum; exp2 and FP32 sums
+                 + n 2^-25 max|v|                   weights below FP16's normal numbers; the largest weight is at least 1
+  with e = 130 2^-24 max_t sum_d |q_d k_td| / sqrt(128), the FP32 sum of 128 products in any order.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv4, paged
+from paper_2405_04532_amd import api, workloads as wl
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+D, PAGE = 128, 64
+
+
+def _ints(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _heads(rows, heads, seed, stream=3, gain=8.0):
+    """[rows, heads, 128] FP16 on the GPU, two large channels in every head."""
+    k, v = wl.make_kv(1, heads, rows, D, seed, DEV, gain=gain)
+    return (k if stream == 3 else v)[0].transpose(0, 1).contiguous()
+
+
+def _tables(totals, width, seed, spare=2):
+    """Pages of the sequences in any order; -1 behind them."""
+    need = [-(-t // PAGE) for t in totals]
+    pages = sum(need) + spare
+    perm = torch.randperm(pages, generator=torch.Generator().manual_seed(seed)).to(torch.int32)
+    table, at = torch.full((len(totals), width), -1, dtype=torch.int32), 0
+    for b, n in enumerate(need):
+        table[b, :n] = perm[at:at + n]
+        at += n
+    return table.to(DEV), pages
+
+
+def _codes(pool, table, pages, Hkv, B, width):
+    """Codes, scales and zeros of every place of a table of valid pages, through the contiguous cache's own unpacking."""
+    page = pool.view(pages, Hkv, 8704)[table.long().clamp(min=0)]          # [B, width, Hkv, 8704]
+    return [t.cpu().numpy() for t in api.kv4_unpack(page.transpose(1, 2).contiguous().view(-1), B, Hkv, width * PAGE)]
+
+
+def _same(a, b):
+    a, b = (x.cpu().numpy() if torch.is_tensor(x) else x for x in (a, b))
+    nan = np.isnan(a) & np.isnan(b)
+    return bool(((a.view(np.uint16) == b.view(np.uint16)) | nan).all())
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# Norm, rotation, append
+# ------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("H,Hkv,rot,near,norm,new,starts", [
+    (4, 2, 128, False, False, [1, 1, 1], [0, 63, 64]),
+    (4, 4, 128, True, True, [5, 0, 67, 1], [2, 9, 61, 127]),
+    (7, 1, 64, False, True, [130], [0]),
+    (3, 3, 64, True, False, [3, 2], [7, 100]),
+    (2, 1, 96, False, False, [9, 40], [1, 30]),
+    (5, 1, 16, False, True, [4, 4, 4, 4], [0, 1, 2, 3]),
+    (4, 2, 0, False, False, [33, 1], [0, 64]),
+    (4, 2, 0, False, True, [12], [50]),
+    (2, 2, 128, False, False, [1] * 70, list(range(70))),
+    (8, 8, 128, False, True, [300, 1, 17], [0, 200, 40])])
+def test_append(H, Hkv, rot, near, norm, new, starts):
+    B, M = len(new), sum(new)
+    width = max((s + n + PAGE - 1) // PAGE for s, n in zip(starts, new)) + 1
+    table, pages = _tables([width * PAGE] * B, width, 5)
+    qkv = torch.cat((_heads(M, H, 11), _heads(M, Hkv, 12), _heads(M, Hkv, 13, 4)), dim=1)       # a fused projection: strided slices
+    q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+    v[0, 0], k[M // 2, 0] = 0, 0                            # vectors of zeros
+    angles = api.rope_angles(width * PAGE, rot, device=DEV) if rot else None
+    gq = (1 + 0.1 * _heads(1, 1, 14)[0, 0]) if norm else None
+    gk = (1 + 0.1 * _heads(1, 1, 15)[0, 0]) if norm else None
+    cu = np.concatenate(([0], np.cumsum(new)))
+    pool = api.kv4_new_pool(pages, Hkv, DEV)
+    pool += 7
+    before = _codes(pool, table, pages, Hkv, B, width)
+    qo, ko = api.qk_rope_kv4_append(q, k, v, pool, table, _ints(cu), _ints(starts), angles, gq, gk, 1e-5, near, want_k=True)
+    seq, pos = paged.rows_of(cu, starts, M)
+    host = lambda t: None if t is None else t.cpu().numpy()                # noqa: E731
+    want_q = paged.turn_heads(host(q), host(gq), 1e-5, host(angles), pos, near)
+    want_k = paged.turn_heads(host(k), host(gk), 1e-5, host(angles), pos, near)
+    assert _same(qo, want_q) and _same(ko, want_k)
+    # what the pages hold: the new tokens' numbers, and what was there everywhere else
+    after = _codes(pool, table, pages, Hkv, B, width)
+    want = [x.copy() for x in before]
+    for x, at in ((want_k, 0), (host(v), 3)):
+        c, s, z = kv4.kv4_quantize(x)
+        want[at][seq, :, pos], want[at + 1][seq, :, pos], want[at + 2][seq, :, pos] = c, s, z
+    for got, exp in zip(after, want):
+        assert _same(got, exp) if got.dtype == np.float16 else np.array_equal(got, exp)
+    # and back: dequantized, rounded once
+    gk_, gv_ = api.kv4_paged_gather(pool, table, _ints(cu), _ints(starts), M, Hkv)
+    assert _same(gk_, paged.quantized(want_k).astype(np.float16)) and _same(gv_, paged.quantized(host(v)).astype(np.float16))
+    # in place, into the projection itself
+    pool2 = api.kv4_new_pool(pages, Hkv, DEV)
+    a, b = api.qk_rope_kv4_append(q, k, v, pool2, table, _ints(cu), _ints(starts), angles, gq, gk, 1e-5, near, q_out=q, k_out=k)
+    assert a.data_ptr() == q.data_ptr() and b.data_ptr() == k.data_ptr()
+    assert _same(q.contiguous(), want_q) and _same(k.contiguous(), want_k) and _same(v.contiguous(), host(v))
+    assert _same(api.kv4_paged_gather(pool2, table, _ints(cu), _ints(starts), M, Hkv)[0], gk_)
+
+
+def test_append_drops_what_has_no_place_and_leaves_other_rows():
+    """Positions before and behind the table, pages that are none, rows of no sequence, an empty batch of rows."""
+    Hkv, width, pages = 2, 2, 3
+    table = _ints([[2, -1], [7, 0], [1, 1 << 30]])
+    cu, starts = [1, 9, 75, 77], [-3, 60, 126]                             # rows 0 and 77, 78 belong to none
+    M = 79
+    k, v, q = _heads(M, Hkv, 21), _heads(M, Hkv, 22, 4), _heads(M, 3, 23)
+    angles = api.rope_angles(100, device=DEV)                              # positions past it take its last row
+    pool = torch.full((pages * Hkv * 8704,), 9, dtype=torch.uint8, device=DEV)
+    qo, ko = torch.full_like(q, 5.0), torch.full_like(k, 6.0)
+    api.qk_rope_kv4_append(q, k, v, pool, table, _ints(cu), _ints(starts), angles, q_out=qo, k_out=ko)
+    seq, pos = paged.rows_of(cu, starts, M)
+    live = seq >= 0
+    ang = angles.cpu().numpy()
+    want_k = paged.turn_heads(k.cpu().numpy(), None, 0, ang, pos, False)
+    assert _same(qo[live], paged.turn_heads(q.cpu().numpy(), None, 0, ang, pos, False)[live]) and _same(ko[live], want_k[live])
+    assert bool((qo[~live] == 5).all()) and bool((ko[~live] == 6).all())
+    want = np.full((pages, Hkv, 64, 128), -1)
+    expect = {}
+    for row in np.flatnonzero(live):
+        at = paged.place(table.cpu().numpy(), pages, seq[row], pos[row])
+        if at:
+            expect[at] = row
+    got = _codes(pool, torch.arange(pages, device=DEV)[:, None], pages, Hkv, pages, 1)
+    kc, vc = kv4.kv4_quantize(want_k)[0], kv4.kv4_quantize(v.cpu().numpy())[0]
+    blank = _codes(torch.full_like(pool, 9), torch.arange(pages, device=DEV)[:, None], pages, Hkv, pages, 1)
+    for page in range(pages):
+        for t in range(64):
+            row = expect.get((page, t))
+            assert np.array_equal(got[0][page, :, t], blank[0][page, :, t] if row is None else kc[row]), (page, t)
+            assert np.array_equal(got[3][page, :, t], blank[3][page, :, t] if row is None else vc[row]), (page, t)
+    assert len(expect) == 5 + 62 and want.size
+    # read back: zeros where there is no page, other rows as they were
+    gk, gv = torch.full((M, Hkv, D), 3.0, dtype=torch.float16, device=DEV), torch.full((M, Hkv, D), 4.0, dtype=torch.float16, device=DEV)
+    api.kv4_paged_gather(pool, table, _ints(cu), _ints(starts), M, Hkv, gk, gv)
+    on = np.array([i in expect.values() for i in range(M)])
+    assert bool((gk[~live] == 3).all()) and bool((gv[~live] == 4).all())
+    assert not gk[torch.from_numpy(live & ~on).to(DEV)].any() and not gv[torch.from_numpy(live & ~on).to(DEV)].any()
+    assert _same(gk[torch.from_numpy(on).to(DEV)], paged.quantized(want_k[on]).astype(np.float16))
+    # no rows at all
+    none = torch.empty((0, Hkv, D), dtype=torch.float16, device=DEV)
+    api.kv4_paged_append(pool, none, none, table, _ints([0, 0, 0, 0]))
+    assert api.kv4_paged_gather(pool, table, _ints([0, 0, 0, 0]), None, 0, Hkv)[0].shape == (0, Hkv, D)
+
+
+def test_append_rounds_once():
+    """Results at and next to midpoints of FP16 numbers, subnormal and overflowing ones, infinities and NaN: the float64 evaluation
+    rounded once."""
+    M, H = 64, 4
+    g = torch.Generator().manual_seed(8)
+    x = (torch.randn(M, H, D, generator=g) * torch.exp2(torch.randint(-24, 16, (M, H, 1), generator=g).float())).half()
+    x[0, 0, 0], x[1, 1, 3], x[2, 2, 2] = float("inf"), float("nan"), -float("inf")
+    x[3] = torch.arange(512).view(4, 128).half() / 512 * 2.0 ** -14
+    angles = torch.zeros(M, D)
+    angles[:, :64] = 1.0                                                   # no turn: numbers come back as they are
+    angles[1::3, :64], angles[1::3, 64:] = 0.5, 0.5                        # sums at midpoints
+    angles[2::3] = torch.rand(angles[2::3].shape, generator=g) * 3 - 1
+    angles[5, :64] = 1.0 + 2.0 ** -11                                      # beside midpoints of odd numbers
+    angles[8, :64] = 1.0 + 2.0 ** -11 + 2.0 ** -23
+    angles[11, :64] = 1.0 + 2.0 ** -11 - 2.0 ** -23
+    for near in (False, True):
+        kv = torch.zeros(M, 1, D, dtype=torch.float16, device=DEV)
+        pool, table = api.kv4_new_pool(1, 1, DEV), _ints([[0]])
+        qo, _ = api.qk_rope_kv4_append(x.to(DEV), kv, kv, pool, table, _ints([0, M]), None, angles.to(DEV), interleaved=near)
+        with np.errstate(invalid="ignore"):
+            want = paged.turn_heads(x.numpy(), None, 0, angles.numpy(), np.arange(M), near)
+        assert _same(qo, want)
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# Decode attention
+# ------------------------------------------------------------------------------------------------------------------
+def _bound(q, k, ref, spread, n):
+    r = q.shape[1] // k.shape[1]
+    e = 0.0
+    for h in range(q.shape[1]):
+        if k.shape[0] and q.shape[0]:
+            e = max(e, float((np.abs(k[:, h // r]) @ np.abs(q[:, h]).T).max()))
+    e *= 130 * 2.0 ** -24 / np.sqrt(128.0)
+    return 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2 * e + 2.0 ** -20) * spread, e
+
+
+def _filled(lens, Hkv, width, seed, spare=2):
+    """A pool with these sequences' tokens, and its dequantized keys and values."""
+    table, pages = _tables(lens, width, seed, spare)
+    M = sum(lens)
+    k, v = _heads(max(M, 1), Hkv, seed), _heads(max(M, 1), Hkv, seed + 1, 4)
+    cu = np.concatenate(([0], np.cumsum(lens)))
+    pool = torch.full((pages * Hkv * 8704,), 0xFF, dtype=torch.uint8, device=DEV)      # NaN parameters where nothing is written
+    api.kv4_paged_append(pool, k[:M].contiguous(), v[:M].contiguous(), table, _ints(cu))
+    return pool, table, pages, cu, paged.quantized(k[:M].cpu().numpy()), paged.quantized(v[:M].cpu().numpy())
+
+
+def _check_decode(out, q, kh, vh, cu, lens, window, sinks, held=None):
+    got, qd = out.cpu().numpy().astype(np.float64), q.cpu().numpy().astype(np.float64)
+    for b, L in enumerate(lens):
+        k, v = kh[cu[b]:cu[b] + L], vh[cu[b]:cu[b] + L]
+        ref, spread = paged.attention(qd[b:b + 1], k, v, [L - 1], window, sinks, None if held is None else held[b][:L])
+        tol, _ = _bound(qd[b:b + 1], k, ref, spread, L)
+        tol = tol + L * 15 * 2.0 ** -25 + 2.0 ** -25
+        assert (np.abs(got[b] - ref[0]) <= tol[0]).all(), (b, L, float(np.abs(got[b] - ref[0]).max()))
+        if L == 0:
+            assert not got[b].any()
+
+
+@pytest.mark.parametrize("H,Hkv", [(4, 4), (8, 2), (7, 1), (16, 1), (9, 1)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (50, 0), (33, 4), (64, 70), (500, 3)])
+def test_decode(H, Hkv, window, sinks):
+    lens = [0, 1, 5, 31, 32, 33, 63, 64, 65, 130, 200, 257]
+    width = 6
+    pool, table, pages, cu, kh, vh = _filled(lens, Hkv, width, 31 + H)
+    q = wl.make_queries(len(lens), H, D, 33, DEV)
+    out = api.kv4_paged_attention_decode(q, pool, table, _ints(lens), Hkv, window=window, sinks=sinks)
+    _check_decode(out, q, kh, vh, cu, lens, window, sinks)
+
+
+@pytest.mark.parametrize("B,H,Hkv,lens,window,sinks", [
+    (1, 4, 1, [4097], 0, 0), (1, 16, 1, [3000], 0, 0), (2, 8, 2, [2049, 1], 0, 0), (3, 4, 4, [900, 0, 511], 0, 0), (2, 4, 2, [5000, 130], 2000, 4),
+    (1, 8, 1, [4200], 700, 100), (5, 6, 2, [64, 1500, 257, 1024, 3], 0, 0)])
+def test_decode_shared_by_workgroups(B, H, Hkv, lens, window, sinks):
+    """Long sequences with few heads, in a workspace that other calls use in turn; the same bits every time, and in a graph."""
+    width = max(-(-n // PAGE) for n in lens) + 1
+    pool, table, pages, cu, kh, vh = _filled(lens, Hkv, width, 51)
+    q = wl.make_queries(B, H, D, 53, DEV)
+    need = api.kv4_paged_attention_workspace_bytes(B, H, Hkv, width, window, sinks)
+    assert need > api.GEMM_COUNTER_BYTES
+    ws = api.new_workspace(need, DEV)
+    ws[api.GEMM_COUNTER_BYTES:] = 0xFF                                     # only the counters have to be zero
+    seq = _ints(lens)
+    out = api.kv4_paged_attention_decode(q, pool, table, seq, Hkv, window, sinks, workspace=ws)
+    _check_decode(out, q, kh, vh, cu, lens, window, sinks)
+    for _ in range(5):
+        again = api.kv4_paged_attention_decode(q, pool, table, seq, Hkv, window, sinks, workspace=ws)
+        assert _same(again, out)
+    assert not ws[:api.GEMM_COUNTER_BYTES].any()
+    alone = api.kv4_paged_attention_decode(q, pool, table, seq, Hkv, window, sinks)
+    _check_decode(alone, q, kh, vh, cu, lens, window, sinks)
+    # two captured graphs that take turns in one workspace, with shorter sequences in the second
+    short = _ints([max(n // 2, 0) for n in lens])
+    outs, graphs = [torch.zeros_like(out), torch.zeros_like(out)], []
+    side = torch.cuda.Stream()
+    for o, s in zip(outs, (seq, short)):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            api.kv4_paged_attention_decode(q, pool, table, s, Hkv, window, sinks, out=o, workspace=ws)
+        graphs.append(graph)
+    want = [out, api.kv4_paged_attention_decode(q, pool, table, short, Hkv, window, sinks, workspace=ws)]
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert _same(outs[0], want[0]) and _same(outs[1], want[1])
+    with pytest.raises(api.QoqError):
+        api.kv4_paged_attention_decode(q, pool, table, seq, Hkv, window, sinks, workspace=ws[:need - 16])
+
+
+def test_decode_many_splits_of_garbage_lengths_and_pages():
+    """Lengths past the table and below zero, pages that are none, in the middle and all of them."""
+    B, H, Hkv, width = 4, 4, 2, 40
+    full = width * PAGE
+    pool, table, pages, cu, kh, vh = _filled([full, 700, 640, 100], Hkv, width, 61)
+    holes = table.clone()
+    holes[1, 3] = pages
+    holes[1, 7] = -5
+    holes[2] = 1 << 30
+    held = [np.ones(full, dtype=bool) for _ in range(B)]
+    held[1][3 * 64:4 * 64] = held[1][7 * 64:8 * 64] = False
+    held[2][:] = False
+    q = wl.make_queries(B, H, D, 63, DEV)
+    ws = api.new_workspace(api.kv4_paged_attention_workspace_bytes(B, H, Hkv, width), DEV)
+    for room in (None, ws):
+        out = api.kv4_paged_attention_decode(q, pool, holes, _ints([1 << 30, 700, 640, -9]), Hkv, workspace=room)
+        _check_decode(out, q, kh, vh, cu, [full, 700, 640, 0], 0, 0, held)
+        assert not out[2:].any()
+
+
+def test_decode_window_does_not_need_the_pages_in_front_of_it():
+    """Pages between the sinks and the window are given away: their entries are gone, their bytes are NaN."""
+    L, H, Hkv = 1000, 4, 1
+    pool, table, pages, cu, kh, vh = _filled([L], Hkv, 16, 71)
+    q = wl.make_queries(1, H, D, 73, DEV)
+    want = api.kv4_paged_attention_decode(q, pool, table, _ints([L]), Hkv, window=200, sinks=4)
+    gone = table.clone()
+    gone[0, 1:(L - 200) // 64] = -1
+    pool.view(pages, -1)[table[0, 1:(L - 200) // 64].long()] = 0xFF
+    assert _same(api.kv4_paged_attention_decode(q, pool, gone, _ints([L]), Hkv, window=200, sinks=4), want)
+    _check_decode(want, q, kh, vh, cu, [L], 200, 4)
+
+
+def test_decode_strided_queries_and_a_large_batch():
+    B, H, Hkv = 150, 4, 2
+    lens = [(37 * i) % 140 for i in range(B)]
+    pool, table, pages, cu, kh, vh = _filled(lens, Hkv, 3, 81)
+    fused = wl.make_queries(B, H + 3, D, 83, DEV)
+    q = fused[:, 1:1 + H]
+    out = api.kv4_paged_attention_decode(q, pool, table, _ints(lens), Hkv)
+    _check_decode(out, q, kh, vh, cu, lens, 0, 0)
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# Prompt attention
+# ------------------------------------------------------------------------------------------------------------------
+def _prompts(new, held, H, Hkv, seed, behind=0):
+    total = [n + h for n, h in zip(new, held)]
+    M, Mk = sum(new) + behind, sum(total) + behind
+    q = _heads(max(M, 1), H, seed, 4)[:M].contiguous()
+    k, v = _heads(max(Mk, 1), Hkv, seed + 1)[:Mk].contiguous(), _heads(max(Mk, 1), Hkv, seed + 2, 4)[:Mk].contiguous()
+    return q, k, v, np.concatenate(([0], np.cumsum(new))), np.concatenate(([0], np.cumsum(total)))
+
+
+def _check_prefill(out, q, k, v, cu_q, cu_k, window, sinks, rows=None):
+    got, qd, kd, vd = (t.cpu().numpy().astype(np.float64) for t in (out, q, k, v))
+    for b in range(len(cu_q) - 1):
+        n, m = cu_q[b + 1] - cu_q[b], cu_k[b + 1] - cu_k[b]
+        pick = np.arange(n) if rows is None or n <= rows else np.unique(np.concatenate((np.arange(4), np.linspace(0, n - 1, rows).astype(int), np.arange(n - 4, n))))
+        kb, vb = kd[cu_k[b]:cu_k[b + 1]], vd[cu_k[b]:cu_k[b + 1]]
+        qb = qd[cu_q[b]:cu_q[b + 1]][pick]
+        ref, spread = paged.attention(qb, kb, vb, m - n + pick, window, sinks)
+        tol, _ = _bound(qb, kb, ref, spread, m)
+        tol = tol + m * 2.0 ** -25 * (np.abs(vb).max() if m else 0) + 2.0 ** -25
+        have = got[cu_q[b]:cu_q[b + 1]][pick]
+        assert (np.abs(have - ref) <= tol).all(), (b, float((np.abs(have - ref) - tol).max()))
+        blind = m - n + pick < 0
+        assert not have[blind].any()
+
+
+@pytest.mark.parametrize("H,Hkv", [(2, 2), (4, 1), (7, 1), (6, 2), (40, 1)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (40, 0), (100, 5), (64, 70)])
+def test_prefill(H, Hkv, window, sinks):
+    new, held = [1, 0, 33, 64, 130, 3], [0, 5, 0, 1, 70, 200]
+    q, k, v, cu_q, cu_k = _prompts(new, held, H, Hkv, 91 + H)
+    out = api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), window=window, sinks=sinks)
+    _check_prefill(out, q, k, v, cu_q, cu_k, window, sinks)
+
+
+@pytest.mark.parametrize("new,held,H,Hkv,window,sinks", [([700], [0], 4, 4, 0, 0), ([515, 260], [300, 0], 8, 2, 0, 0), ([300], [1500], 4, 1, 256, 4),
+                                                         ([1], [2000], 8, 2, 0, 0), ([3, 1, 2], [1999, 900, 64], 8, 1, 0, 0), ([2], [3500], 4, 4, 1500, 64)])
+def test_prefill_longer(new, held, H, Hkv, window, sinks):
+    q, k, v, cu_q, cu_k = _prompts(new, held, H, Hkv, 95)
+    need = api.attention_prefill_workspace_bytes(len(q), len(k), len(new), H, Hkv, window, sinks)
+    ws = api.new_workspace(need, DEV)
+    out = api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), window=window, sinks=sinks)
+    _check_prefill(out, q, k, v, cu_q, cu_k, window, sinks, rows=40)
+    shared = api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), window=window, sinks=sinks, workspace=ws)
+    _check_prefill(shared, q, k, v, cu_q, cu_k, window, sinks, rows=40)
+    for _ in range(3):
+        assert _same(api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), window=window, sinks=sinks, workspace=ws), shared)
+
+
+def test_prefill_more_queries_than_tokens_and_rows_of_no_sequence():
+    """Queries in front of a sequence's first token see nothing; rows behind the last sequence stay as they were."""
+    H, Hkv = 4, 2
+    q, k, v, _, _ = _prompts([80], [80], H, Hkv, 97)
+    cu_q, cu_k = [2, 40, 60, 75], [0, 10, 10, 90]                          # 38 queries of 10 tokens, 20 of none, 15 of 80
+    out = torch.full((80, H, D), 9.0, dtype=torch.float16, device=DEV)
+    api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), out=out)
+    _check_prefill(out, q, k, v, cu_q, cu_k, 0, 0)
+    assert bool((out[:2] == 9).all()) and bool((out[75:] == 9).all()) and not out[40:60].any()
+    out.fill_(9.0)
+    api.attention_prefill(q, k, v, _ints([0, 200]), _ints([-4, 500]), out=out)      # bounds past the rows: the nearest ones
+    _check_prefill(out, q, k, v, [0, 80], [0, 160], 0, 0)
+    none = torch.empty((0, Hkv, D), dtype=torch.float16, device=DEV)
+    assert not api.attention_prefill(q, none, none, _ints([0, 80]), _ints([0, 0])).any()
+
+
+def test_prefill_strided_slices():
+    H, Hkv, M = 8, 2, 150
+    qkv = torch.cat((_heads(M, H, 101, 4), _heads(M, Hkv, 102), _heads(M, Hkv, 103, 4)), dim=1)
+    q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+    cu = [0, 90, M]
+    out = api.attention_prefill(q, k, v, _ints(cu), _ints(cu))
+    assert _same(out, api.attention_prefill(q.contiguous(), k.contiguous(), v.contiguous(), _ints(cu), _ints(cu)))
+    _check_prefill(out, q, k, v, cu, cu, 0, 0)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (30, 2)])
+def test_prefill_infinities_and_nan_reach_only_the_queries_that_see_them(window, sinks):
+    """Values and keys that are not finite at some tokens: earlier queries, and later ones whose window has passed, are as without."""
+    H, Hkv, T = 2, 1, 200
+    q, k, v, cu, _ = _prompts([T], [0], H, Hkv, 105)
+    clean = api.attention_prefill(q, k, v, _ints(cu), _ints(cu), window=window, sinks=sinks)
+    spots = {70: (3, float("inf")), 71: (4, float("nan")), 100: (5, -float("inf")), 101: (3, -float("inf")), 130: (5, -float("inf"))}
+    v2 = v.clone()
+    for t, (d, x) in spots.items():
+        v2[t, 0, d] = x
+    got = api.attention_prefill(q, k, v2, _ints(cu), _ints(cu), window=window, sinks=sinks).cpu().numpy().astype(np.float64)
+    clean = clean.cpu().numpy()
+    for i in range(T):
+        for d in (2, 3, 4, 5):
+            seen = [x for t, (dd, x) in spots.items() if dd == d and paged.visible(i, t, window, sinks)]
+            if not seen:
+                assert np.array_equal(got[i, :, d], clean[i, :, d].astype(np.float64)), (i, d)
+            elif any(np.isnan(seen)) or len(set(seen)) > 1:
+                assert np.isnan(got[i, :, d]).all(), (i, d)
+            else:                                                          # (a weight may be zero: NaN)
+                ok = (got[i, :, d] == seen[0]) | np.isnan(got[i, :, d])
+                assert ok.all(), (i, d)
+    k2 = k.clone()
+    k2[150] = float("nan")
+    got = api.attention_prefill(q, k2, v, _ints(cu), _ints(cu), window=window, sinks=sinks).cpu().numpy()
+    for i in range(T):
+        if paged.visible(i, 150, window, sinks):
+            assert np.isnan(got[i]).all()
+        else:
+            assert np.array_equal(got[i], clean[i])
+
+
+def test_scores_of_any_size():
+    """Scores far below zero for every token, and differences that leave one token alone."""
+    H, Hkv, T = 2, 1, 100
+    q, k, v, cu, _ = _prompts([T], [0], H, Hkv, 107)
+    for scale in (3000.0, -3000.0):
+        qs = torch.ones_like(q) * 50
+        ks = (torch.sign(torch.ones_like(k)) * scale + k).half()
+        out = api.attention_prefill(qs, ks, v, _ints(cu), _ints(cu))
+        assert bool(torch.isfinite(out).all())
+        got, kd, vd = out.cpu().numpy().astype(np.float64), ks.cpu().numpy().astype(np.float64), v.cpu().numpy().astype(np.float64)
+        ref, spread = paged.attention(qs.cpu().numpy().astype(np.float64), kd, vd, np.arange(T))
+        e = 130 * 2.0 ** -24 * 50 * 3100 * 128 / np.sqrt(128.0)             # scores of 1.7e6: FP32 holds them to about 0.1
+        tol = 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2 * (np.exp(e) - 1)) * spread + T * 2.0 ** -25 * np.abs(vd).max()
+        assert (np.abs(got - ref) <= tol).all()
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# Together, as a serving program runs them
+# ------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("H,Hkv,window,sinks", [(4, 4, 0, 0), (8, 2, 90, 4)])
+def test_prompt_continued_prompt_and_generation(H, Hkv, window, sinks):
+    """Two prompts, one of them in two parts (the second behind what the cache holds), then tokens one at a time."""
+    B, width, eps = 2, 5, 1e-6
+    lens, parts, steps = [150, 90], [[100, 90], [50, 0]], 3
+    total = [n + steps for n in lens]
+    table, pages = _tables([width * PAGE] * B, width, 7)
+    qkv = [torch.cat((_heads(n, H, 200 + b), _heads(n, Hkv, 210 + b), _heads(n, Hkv, 220 + b, 4)), dim=1) for b, n in enumerate(total)]
+    gq, gk = 1 + 0.1 * _heads(1, 1, 231)[0, 0], 1 + 0.1 * _heads(1, 1, 232)[0, 0]
+    angles = api.rope_angles(width * PAGE, device=DEV)
+    pool = api.kv4_new_pool(pages, Hkv, DEV)
+    ws = api.new_workspace(max(api.kv4_paged_attention_workspace_bytes(B, H, Hkv, width, window, sinks),
+                               api.attention_prefill_workspace_bytes(400, 400, B, H, Hkv, window, sinks)), DEV)
+    turned = []
+    for b, n in enumerate(total):
+        x, pos = qkv[b].cpu().numpy(), np.arange(n)
+        ang = angles.cpu().numpy()
+        turned.append((paged.turn_heads(x[:, :H], gq.cpu().numpy(), eps, ang, pos, False), paged.turn_heads(x[:, H:H + Hkv], gk.cpu().numpy(), eps, ang, pos, False), x[:, H + Hkv:]))
+    done = [0, 0]
+    for part in parts:
+        M = sum(part)
+        cu, starts = np.concatenate(([0], np.cumsum(part))), list(done)
+        rows = torch.cat([qkv[b][done[b]:done[b] + part[b]] for b in range(B)])
+        q, k = api.qk_rope_kv4_append(rows[:, :H], rows[:, H:H + Hkv], rows[:, H + Hkv:], pool, table, _ints(cu), _ints(starts), angles, gq, gk, eps,
+                                      want_k=True)
+        if any(done):                                                      # keys and values of everything so far, out of the cache
+            have = [done[b] + part[b] if part[b] else 0 for b in range(B)]
+            cu_k = np.concatenate(([0], np.cumsum(have)))
+            kk, vv = api.kv4_paged_gather(pool, table, _ints(cu_k), None, sum(have), Hkv)
+            kd = [paged.quantized(turned[b][1][:have[b]]).astype(np.float16) for b in range(B)]
+            vd = [paged.quantized(turned[b][2][:have[b]]).astype(np.float16) for b in range(B)]
+            assert _same(kk, np.concatenate(kd)) and _same(vv, np.concatenate(vd))
+        else:
+            cu_k, kk, vv = cu, k, rows[:, H + Hkv:]
+        out = api.attention_prefill(q, kk, vv, _ints(cu), _ints(cu_k), window, sinks, workspace=ws)
+        assert _same(q, np.concatenate([turned[b][0][done[b]:done[b] + part[b]] for b in range(B)]))
+        _check_prefill(out, q, kk, vv, cu, cu_k, window, sinks)
+        done = [d + p for d, p in zip(done, part)]
+        assert out.shape[0] == M
+    cu = list(range(B + 1))
+    for _ in range(steps):
+        rows = torch.stack([qkv[b][done[b]] for b in range(B)])
+        q, _ = api.qk_rope_kv4_append(rows[:, :H], rows[:, H:H + Hkv], rows[:, H + Hkv:], pool, table, _ints(cu), _ints(done), angles, gq, gk, eps)
+        done = [d + 1 for d in done]
+        out = api.kv4_paged_attention_decode(q, pool, table, _ints(done), Hkv, window, sinks, workspace=ws)
+        kh = np.concatenate([paged.quantized(turned[b][1][:done[b]]) for b in range(B)])
+        vh = np.concatenate([paged.quantized(turned[b][2][:done[b]]) for b in range(B)])
+        _check_decode(out, q, kh, vh, np.concatenate(([0], np.cumsum(done))), done, window, sinks)
+
+
+def test_pages_and_contiguous_cache_agree():
+    """The same tokens in both caches: the same codes, and attention within the rounding of its weights."""
+    B, H, Hkv, S = 3, 8, 2, 130
+    k, v = wl.make_kv(B, Hkv, S, D, 41, DEV)
+    q = wl.make_queries(B, H, D, 41, DEV)
+    rows = lambda x: x.transpose(1, 2).contiguous()                        # noqa: E731
+    cache = api.kv4_new_cache(B, Hkv, S, DEV)
+    api.kv4_append(cache, rows(k), rows(v), _ints([0] * B), S)
+    table, pages = _tables([S] * B, 3, 43)
+    pool = api.kv4_new_pool(pages, Hkv, DEV)
+    api.kv4_paged_append(pool, rows(k).view(B * S, Hkv, D), rows(v).view(B * S, Hkv, D), table, _ints([0, S, 2 * S, 3 * S]))
+    a = api.kv4_unpack(cache, B, Hkv, S)
+    b = _codes(pool, table, pages, Hkv, B, 3)
+    for x, y in zip(a, b):
+        assert np.array_equal(x.cpu().numpy().view(np.uint8), np.ascontiguousarray(y[:, :, :S]).view(np.uint8))
+    lens = _ints([S, 64, 1])
+    one, two = api.kv4_attention_decode(q, cache, lens, Hkv, S), api.kv4_paged_attention_decode(q, pool, table, lens, Hkv)
+    assert torch.allclose(one.float(), two.float(), rtol=2e-3, atol=2e-3)
+
+
+def test_another_stream_and_refusals_of_the_binding():
+    H, Hkv, T = 4, 2, 70
+    q, k, v, cu, _ = _prompts([T], [0], H, Hkv, 111)
+    pool, table = api.kv4_new_pool(2, Hkv, DEV), _ints([[1, 0]])
+    want = api.attention_prefill(q, k, v, _ints(cu), _ints(cu))
+    c = _ints(cu)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = api.attention_prefill(q, k, v, c, c)
+        api.kv4_paged_append(pool, k, v, table, c)
+        gk, _ = api.kv4_paged_gather(pool, table, c, None, T, Hkv)
+    side.synchronize()
+    assert _same(got, want) and _same(gk, paged.quantized(k.cpu().numpy()).astype(np.float16))
+    for bad in (dict(q=q.float()), dict(q=q.cpu()), dict(k=k[:, :, ::2]), dict(k=k[:-1]), dict(cu_k=c[:1]), dict(cu_q=c.long()), dict(out=q[:, :2]),
+                dict(q=q.transpose(0, 1)), dict(workspace=torch.zeros(8)), dict(q=None), dict(window="x")):
+        with pytest.raises((TypeError, ValueError, api.QoqError)):
+            api.attention_prefill(**{**dict(q=q, k=k, v=v, cu_q=c, cu_k=c), **bad})
+    for bad in (dict(pool=pool.float()), dict(block_table=table[0]), dict(block_table=table.repeat(2, 1)), dict(angles=torch.zeros(4, 120, device=DEV)),
+                dict(q_gamma=torch.zeros(64, dtype=torch.float16, device=DEV)), dict(starts=_ints([0, 0])), dict(v=v[:, :1]), dict(q_out=q[:3]),
+                dict(pool=pool[:8704]), dict(eps=-1.0), dict(q=None, q_out=q)):
+        with pytest.raises((TypeError, ValueError, api.QoqError)):
+            api.qk_rope_kv4_append(**{**dict(q=q, k=k, v=v, pool=pool, block_table=table, cu=c, starts=None, angles=None), **bad})
+    lens = _ints([T])
+    for bad in (dict(q=q), dict(seq_lens=_ints([1, 2])), dict(Hkv=3), dict(Hkv=0), dict(window=-1), dict(block_table=table.long()), dict(out=q[:2])):
+        with pytest.raises((TypeError, ValueError, api.QoqError)):
+            api.kv4_paged_attention_decode(**{**dict(q=q[:1], pool=pool, block_table=table, seq_lens=lens, Hkv=Hkv), **bad})
+    for bad in (dict(rows=-1), dict(Hkv=0), dict(k_out=k[:5]), dict(cu=c.long()), dict(starts=_ints([0, 0]))):
+        with pytest.raises((TypeError, ValueError, api.QoqError)):
+            api.kv4_paged_gather(**{**dict(pool=pool, block_table=table, cu=c, starts=None, rows=T, Hkv=Hkv), **bad})
