@@ -49,6 +49,19 @@ __device__ __forceinline__ float row_max16(float v)
     return fmaxf(v, row_move<0x121>(v));
 }
 
+// the larger of a lane's number and that of the lane 16 (32) further on or back: rows (halves) change places between two registers,
+// without the way through LDS that a shuffle takes
+__device__ __forceinline__ float max_other_row(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_other_half(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // Eq. 1 of one vector of 128 elements spread over a row of 16 lanes, 8 elements (16 bytes) each: this lane's eight codes, the
 // scale's FP16 bits, and the FP16 bits of -(1024 + z) (an exact integer), the constant that the decode kernels add to their
 // unpacked codes.  Lanes that hold nothing bring any words; every lane of a row has to take part.

@@ -299,55 +299,51 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(const uint8_t* __rest
 // their waves take the chunks in turn.  Unnormalised sums, maxima and weight sums meet in the workspace; the last workgroup to
 // arrive adds them up, in the order of the workgroups whichever arrives when, and leaves the counter at zero.
 // ------------------------------------------------------------------------------------------
-constexpr int kPartial = kD + 2;                         // floats per head: 128 sums, the maximum, the weight sum
+constexpr int kPartial = kD + 4;                         // floats per head: 128 sums, the maximum, the weight sum (rows of 16 bytes)
 constexpr int kChunk = 32;                               // tokens per chunk: two tiles of 16 (divides the page)
-constexpr int kWaves = 4;
-constexpr int kMaxSplits = 32;
+constexpr int kMaxRatio = 16;                            // query heads per KV head: the columns of one matrix instruction
+constexpr int kWaves = 4;                                // of a workgroup
+constexpr int kAlone = 5;                                // chunks per wave up to which one workgroup attends alone
+constexpr int kInFlight = 8;                            // sums of a thread of the join
+constexpr int kMaxSplits = 64;                          // workgroups to a (sequence, KV head): the lanes of a wave
 
-struct DecodeArgs {
+struct DecodeTail {                                      // arguments that are not needed at once
     const __half* q;
-    const uint8_t* pool;
-    const int32_t* table;
-    const int32_t* seq_lens;
     __half* out;
     int* counters;
     float* parts;
     int64_t q_stride;
-    uint32_t pages;
-    int width, Hkv, R, ns, deal, window, sinks;
+    int R, sinks;
 };
 
-template <int PK, bool NT>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(PK == 1 ? 2 : 3))) void paged_decode_kernel(DecodeArgs p)
+// pages are addressed by a base in scalar registers, which comes out of the block table, and a lane's offset
+typedef const __attribute__((address_space(1))) uint8_t* global_bytes;
+typedef const __attribute__((address_space(1))) u32x4* global_u32x4;
+
+__device__ __forceinline__ float4 load_part(const float* at)
 {
-    extern __shared__ float s_part[];                    // [wave][column][kPartial]
+    const v4i v = load_through(reinterpret_cast<const int4*>(at));
+    return make_float4(__int_as_float(v.x), __int_as_float(v.y), __int_as_float(v.z), __int_as_float(v.w));
+}
+
+template <int PK, bool NT>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))) void paged_decode_kernel(
+    const uint8_t* __restrict__ pool, const int32_t* __restrict__ table, const int32_t* __restrict__ seq_lens, uint32_t pages, int width,
+    int Hkv, int ns, int window, DecodeTail p)
+{
+    extern __shared__ __align__(16) float s_part[];      // [wave][column][kPartial], then as the join needs it
     __shared__ int s_last;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, kb = lane >> 4;
     const int R = p.R, head = PK == 2 ? r16 & 7 : r16;
     const bool second = PK == 2 && r16 >= 8;
-    const uint32_t bh = blockIdx.x, b = bh / (uint32_t)p.Hkv, hk = bh - b * (uint32_t)p.Hkv;
+    const uint32_t bh = blockIdx.x, b = bh / (uint32_t)Hkv, hk = bh - b * (uint32_t)Hkv;
     const int split = blockIdx.y;
 
-    // what is seen: tokens below `first_end`, and from `lo` to L
-    const int L = min(max(p.seq_lens[b], 0), p.width * kPageTokens);
-    const int lo = p.window ? max(L - p.window, 0) : 0, sinks = p.sinks;
-    const int chunks = (L + kChunk - 1) / kChunk;
-    const int n_first = min((sinks + kChunk - 1) / kChunk, chunks);        // chunks of the sinks
-    const int gap = max(lo / kChunk - n_first, 0);                         // chunks behind them that nothing sees
-    const int n = chunks - gap;                                            // the list: i < n_first ? i : i + gap
-    const int nwg = min(p.ns, max(1, (n + kWaves * p.deal - 1) / (kWaves * p.deal)));
-    if (split >= nwg) return;
-    __half* out_bh = p.out + (size_t)bh * R * kD;
-    if (n == 0) {
-        for (int x = threadIdx.x; x < R * kD; x += 64 * kWaves) out_bh[x] = __float2half_rn(0.f);
-        return;
-    }
-    const int stride = nwg * kWaves, i0 = split * kWaves + wave;
-    const int n_iter = i0 < n ? (n - i0 + stride - 1) / stride : 0;
-    const int32_t* pages_of = p.table + (int64_t)b * p.width;
-
+    const int32_t* pages_of = table + (int64_t)b * width;
+    const int i0 = split * kWaves + wave;                    // without a window the wave's first chunk, whose page is looked up beside the length
+    const uint32_t first_id = window ? 0u : (uint32_t)pages_of[min(i0, 2 * width - 1) >> 1];
     struct Chunk {
         uint4 kc[2];        // keys: token r16 of the tile, elements 32 kb ..
         uint4 vc[2];        // values: this lane's 16 bytes of the tile
@@ -355,73 +351,113 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(PK 
         uint4 ks[2 / PK];   // (s, z) of tokens 4 kb .. 4 kb + 3 (scales of the scores this lane keeps)
         uint4 vp[2];        // (s, z) of tokens 4 kb .. 4 kb + 3 of the values
     };
-    const uint32_t off_kc = (uint32_t)(r16 * (kD / 2) + kb * 16), off_kz = (uint32_t)(kCodeBytes + r16 * 4);
-    const uint32_t off_ks = (uint32_t)(kCodeBytes + kb * 16 + (second ? 64 : 0)), off_vc = (uint32_t)(kHalfPage + lane * 16);
-    const uint32_t off_vp = (uint32_t)(kHalfPage + kCodeBytes + kb * 16);
-    auto code_words = [](const uint8_t* at) __attribute__((always_inline)) {
-        const uint4* x = reinterpret_cast<const uint4*>(at);
-        return NT ? load_nontemporal(x) : *x;
+    uint32_t off_kc = (uint32_t)(r16 * (kD / 2) + kb * 16), off_kz = (uint32_t)(kCodeBytes + r16 * 4);
+    uint32_t off_ks = (uint32_t)(kCodeBytes + kb * 16 + (second ? 64 : 0)), off_vc = (uint32_t)(kHalfPage + lane * 16);
+    uint32_t off_vp = (uint32_t)(kHalfPage + kCodeBytes + kb * 16);
+    auto words = [](global_bytes at) __attribute__((always_inline)) { return __builtin_bit_cast(uint4, *(global_u32x4)at); };
+    auto code_words = [&](global_bytes at) __attribute__((always_inline)) {
+        return NT ? __builtin_bit_cast(uint4, __builtin_nontemporal_load((global_u32x4)at)) : words(at);
     };
-    auto chunk_of = [&](int it) __attribute__((always_inline)) {           // of the wave's it-th turn; past its last one, the last of the list
-        const int i = min(i0 + it * stride, n - 1);
-        return __builtin_amdgcn_readfirstlane(i < n_first ? i : i + gap);
-    };
-    auto page_of = [&](int it) __attribute__((always_inline)) { return (uint32_t)pages_of[chunk_of(it) >> 1]; };
     auto load_chunk = [&](Chunk& c, int chunk, uint32_t id) __attribute__((always_inline)) {
-        const uint32_t held = id < p.pages ? id : 0;                       // (no page: any, and nothing of it counts)
-        const uint8_t* page = p.pool + ((int64_t)held * p.Hkv + hk) * kPageBytes;
+        const uint32_t held = id < pages ? id : 0;                       // (no page: any, and nothing of it counts)
+        const auto page = (global_bytes)(uintptr_t)to_sgpr(pool + ((int64_t)held * Hkv + hk) * kPageBytes);
         const int tin = (chunk & 1) * kChunk;
-        const uint8_t* codes = page + tin * (kD / 2);
-        const uint8_t* prm = page + tin * 4;
+        const auto codes = page + tin * (kD / 2), prm = page + tin * 4;
+        // (extended to 64 bits outside the loop, the offsets would take register pairs and an addition for each load)
+        asm("" : "+v"(off_kc), "+v"(off_kz), "+v"(off_ks), "+v"(off_vc), "+v"(off_vp));
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
             c.kc[tt] = code_words(codes + tt * 1024 + off_kc);
-            c.kz[tt] = *reinterpret_cast<const uint32_t*>(prm + tt * 64 + off_kz);
-            if (tt < 2 / PK) c.ks[tt] = *reinterpret_cast<const uint4*>(prm + tt * 64 + off_ks);
+            c.kz[tt] = *(const __attribute__((address_space(1))) uint32_t*)(prm + tt * 64 + off_kz);
+            if (tt < 2 / PK) c.ks[tt] = words(prm + tt * 64 + off_ks);
         }
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
             c.vc[tt] = code_words(codes + tt * 1024 + off_vc);
-            c.vp[tt] = *reinterpret_cast<const uint4*>(prm + tt * 64 + off_vp);
+            c.vp[tt] = words(prm + tt * 64 + off_vp);
         }
     };
     Chunk A, Bf;
-    uint32_t id_a = page_of(0), id_b = page_of(1);
+    // what is seen: tokens below `sinks`, and from `lo` to L
+    const int L = min(max(seq_lens[b], 0), width * kPageTokens);
+    const int lo = window ? max(L - window, 0) : 0, sinks = p.sinks;
+    const int chunks = (L + kChunk - 1) / kChunk;
+    const int n_first = min((sinks + kChunk - 1) / kChunk, chunks);        // chunks of the sinks
+    const int gap = max(lo / kChunk - n_first, 0);                         // chunks behind them that nothing sees
+    const int n = chunks - gap;                                            // the list: i < n_first ? i : i + gap
+    const int deal = max(2, (int)(__builtin_sqrtf((float)n) * 0.25f));
+    const int nwg = n <= kAlone * kWaves ? 1 : min(ns, (n + kWaves * deal - 1) / (kWaves * deal));
+    if (split >= nwg) return;
+    __half* out_bh = p.out + (size_t)bh * R * kD;
+    if (n == 0) {
+        for (int x = threadIdx.x; x < R * kD; x += 64 * kWaves) out_bh[x] = __float2half_rn(0.f);
+        return;
+    }
+    const int stride = nwg * kWaves;
+    const int n_iter = i0 < n ? (n - i0 + stride - 1) / stride : 0;
+
+    auto chunk_of = [&](int it) __attribute__((always_inline)) {           // of the wave's it-th turn, or its last
+        const int i = min(i0 + max(min(it, n_iter - 1), 0) * stride, n - 1);
+        return __builtin_amdgcn_readfirstlane(i < n_first ? i : i + gap);
+    };
+    auto page_of = [&](int it) __attribute__((always_inline)) { return (uint32_t)pages_of[chunk_of(it) >> 1]; };
+    uint32_t id_a = window ? page_of(0) : first_id, id_b = page_of(1);
     load_chunk(A, chunk_of(0), id_a);
 
     // B operand of S = K q^T: column = head (both halves of the columns with PK = 2; heads >= R: zero), k-block kb = elements 32 kb ..
-    h2 qv[16];
+    uint4 qv[4];
     {
         const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_stride + ((int)hk * R + min(head, R - 1)) * kD + kb * 32);
+        const uint32_t some = head < R ? ~0u : 0u;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint4 t = src[e];
-            const uint32_t u[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-            for (int x = 0; x < 4; ++x) qv[4 * e + x] = __builtin_bit_cast(h2, head < R ? u[x] : 0u);
+            qv[e] = make_uint4(t.x & some, t.y & some, t.z & some, t.w & some);
         }
     }
 
-    float m = -1e30f, l = 0.f;                           // of this lane's column, over the tokens it has seen
+    float m = -1e29f, l = 0.f;                           // of this lane's column, over the tokens it has seen
     f4 acc[8];                                           // acc[4u + j][x]: element d = 16 kb + 4x + 64u + j of the column
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = (f4){0.f, 0.f, 0.f, 0.f};
     const float kScale = 1.4426950408889634f * 0.08838834764831845f;      // log2(e) / sqrt(128)
     const h2 k960 = {(_Float16)960.0f, (_Float16)960.0f};
 
-    // One chunk of arithmetic.  MASKED: not all of its tokens are seen; the parameters of those that are not are whatever the
-    // cache holds and must not enter the arithmetic.
-    auto process_as = [&](const Chunk& cur, int chunk, bool held, auto masked_tag) __attribute__((always_inline)) {
-        constexpr bool MASKED = decltype(masked_tag)::value;
-        constexpr int NS = 2 / PK;
-        const int own = chunk * kChunk + (second ? 16 : 0) + 4 * kb;       // first token of the lane's (first) score vector
+    // A chunk of which not every token is seen: the parameters of the others are whatever the cache holds and must not enter the
+    // arithmetic.  Their codes become small numbers, their scales zero, and their scores fall to -1e30 by `bias`, whose weight is 0
+    // against any maximum (which starts at -1e29).
+    auto hide = [&](Chunk& cur, int chunk, bool held, f4 (&bias)[2 / PK]) __attribute__((always_inline)) {
         const int end = held ? L : 0, end_first = held ? sinks : 0;
         auto seen = [&](int t) { return t < end && (t >= lo || t < end_first); };
+        auto kept = [&](uint4 v, int t, uint32_t none) {                   // parameters of tokens t .. t + 3
+            return make_uint4(seen(t) ? v.x : none, seen(t + 1) ? v.y : none, seen(t + 2) ? v.z : none, seen(t + 3) ? v.w : none);
+        };
+        const int t0 = chunk * kChunk;
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            cur.kz[tt] = seen(t0 + tt * 16 + r16) ? cur.kz[tt] : 0xE4000000u;                     // -(1024 + 0)
+            cur.vp[tt] = kept(cur.vp[tt], t0 + tt * 16 + 4 * kb, 0xE4000000u);
+        }
+#pragma unroll
+        for (int tt = 0; tt < 2 / PK; ++tt) {
+            const int t = t0 + (second ? 16 : 0) + tt * 16 + 4 * kb;
+            cur.ks[tt] = kept(cur.ks[tt], t, 0u);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) bias[tt][x] = seen(t + x) ? 0.f : -1e30f;
+        }
+    };
+    auto process = [&](Chunk& cur, int it, uint32_t id) __attribute__((always_inline)) {
+        constexpr int NS = 2 / PK;
+        const int chunk = chunk_of(it);
+        f4 bias[NS];
+#pragma unroll
+        for (int tt = 0; tt < NS; ++tt) bias[tt] = (f4){0.f, 0.f, 0.f, 0.f};
+        if (!(id < pages && chunk * kChunk + kChunk <= L && (chunk * kChunk >= lo || chunk * kChunk + kChunk <= sinks)))
+            hide(cur, chunk, id < pages, bias);
         f4 d[2];
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
-            uint32_t kz = cur.kz[tt];
-            if (MASKED) kz = seen(chunk * kChunk + tt * 16 + r16) ? kz : 0xE4000000u;   // -(1024 + 0)
+            const uint32_t kz = cur.kz[tt];
             const h2 c = __builtin_bit_cast(h2, __builtin_amdgcn_perm(kz, kz, 0x07060706u));   // high half in both halves
             const h2 c16 = c + k960;
             const uint32_t kw[4] = {cur.kc[tt].x, cur.kc[tt].y, cur.kc[tt].z, cur.kc[tt].w};
@@ -431,10 +467,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(PK 
                 h2 kh[4];
                 unpack4(kw[w], c, c16, kh);              // kh[j] = elements 8w + 2j, 8w + 2j + 1 of this lane's 32
                 d[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(kh[0], kh[1], kh[2], kh[3]),
-                                                               join(qv[4 * w], qv[4 * w + 1], qv[4 * w + 2], qv[4 * w + 3]), d[tt], 0, 0, 0);
+                                                               __builtin_bit_cast(h8, qv[w]), d[tt], 0, 0, 0);
             }
         }
-        f4 sc[NS];                                       // [x] = token own + x (+ 16 for the second vector)
+        f4 sc[NS];                                       // [x] = token 4 kb + x of the lane's tile (of both tiles with PK = 1)
         if (PK == 2) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) sc[0][x] = second ? d[1][x] : d[0][x];
@@ -448,13 +484,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(PK 
             const uint32_t sw[4] = {cur.ks[tt].x, cur.ks[tt].y, cur.ks[tt].z, cur.ks[tt].w};
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                sc[tt][x] *= (float)half_of(sw[x]) * kScale;
-                if (MASKED) sc[tt][x] = seen(own + tt * 16 + x) ? sc[tt][x] : -1e30f;
+                sc[tt][x] = fmaf(sc[tt][x], (float)half_of(sw[x]) * kScale, bias[tt][x]);
                 m_new = fmaxf(m_new, sc[tt][x]);
             }
         }
-        m_new = fmaxf(m_new, __shfl_xor(m_new, 16, 64));  // the four k-blocks of a column agree on the maximum
-        m_new = fmaxf(m_new, __shfl_xor(m_new, 32, 64));
+        m_new = max_other_half(max_other_row(m_new));    // the four k-blocks of a column agree on the maximum
         if (__builtin_amdgcn_ballot_w64(m_new != m) != 0) {                  // rare once a few chunks have been seen
             const float alpha = __builtin_amdgcn_exp2f(m - m_new);
             m = m_new;
@@ -462,23 +496,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(PK 
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[i] *= alpha;
         }
-        uint32_t pw[2][4];                               // (s, z) of the values, tokens 4 kb .. of both tiles
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-            const uint32_t w4[4] = {cur.vp[tt].x, cur.vp[tt].y, cur.vp[tt].z, cur.vp[tt].w};
-#pragma unroll
-            for (int x = 0; x < 4; ++x) pw[tt][x] = !MASKED || seen(chunk * kChunk + tt * 16 + 4 * kb + x) ? w4[x] : 0xE4000000u;   // else scale 0, zero point 0
-        }
         uint32_t bw[2][2];                               // B operand: softmax weight * value scale, tokens 4 kb .. of both tiles
 #pragma unroll
         for (int tt = 0; tt < NS; ++tt) {
+            const uint32_t pw[2][4] = {{cur.vp[0].x, cur.vp[0].y, cur.vp[0].z, cur.vp[0].w}, {cur.vp[1].x, cur.vp[1].y, cur.vp[1].z, cur.vp[1].w}};
             float wf[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                // a masked score is -1e30: its weight underflows to 0 unless nothing has been seen yet (then m is -1e30 too),
-                // which the zero scale takes care of
                 const float pr = __builtin_amdgcn_exp2f(sc[tt][x] - m);
-                l += MASKED ? (seen(own + tt * 16 + x) ? pr : 0.f) : pr;
+                l += pr;
                 wf[x] = pr * (float)half_of(PK == 2 ? (second ? pw[1][x] : pw[0][x]) : pw[tt][x]);
             }
             const uint32_t b_lo = __builtin_bit_cast(uint32_t, (h2){(_Float16)wf[0], (_Float16)wf[1]});
@@ -490,34 +516,36 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(PK 
                 bw[tt][0] = b_lo; bw[tt][1] = b_hi;
             }
         }
-        h2 vh[2][2][2][4];                               // [tile][u][h][j]: (token 4 kb + 2h, + 1) of element 4 (r16 + 16 u) + j
+        h2 cz[2][2], cz16[2][2];
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
-            const uint32_t vw[4] = {cur.vc[tt].x, cur.vc[tt].y, cur.vc[tt].z, cur.vc[tt].w};
+            const uint32_t pw[4] = {cur.vp[tt].x, cur.vp[tt].y, cur.vp[tt].z, cur.vp[tt].w};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const h2 c = __builtin_bit_cast(h2, __builtin_amdgcn_perm(pw[tt][2 * h + 1], pw[tt][2 * h], 0x07060302u));
-                const h2 c16 = c + k960;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) unpack4(vw[2 * u + h], c, c16, vh[tt][u][h]);
+                cz[tt][h] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(pw[2 * h + 1], pw[2 * h], 0x07060302u));
+                cz16[tt][h] = cz[tt][h] + k960;
             }
         }
         const h8 b8 = join(__builtin_bit_cast(h2, bw[0][0]), __builtin_bit_cast(h2, bw[0][1]), __builtin_bit_cast(h2, bw[1][0]),
                            __builtin_bit_cast(h2, bw[1][1]));
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < 2; ++u) {                    // (one half of the elements after the other: registers)
+            __builtin_amdgcn_sched_barrier(0);
+            h2 vh[2][2][4];                              // [tile][h][j]: (token 4 kb + 2h, + 1) of element 4 (r16 + 16 u) + j
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                const uint32_t vw[4] = {cur.vc[tt].x, cur.vc[tt].y, cur.vc[tt].z, cur.vc[tt].w};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) unpack4(vw[2 * u + h], cz[tt][h], cz16[tt][h], vh[tt][h]);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                acc[4 * u + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(vh[0][u][0][j], vh[0][u][1][j], vh[1][u][0][j], vh[1][u][1][j]),
-                                                                        b8, acc[4 * u + j], 0, 0, 0);
-    };
-    auto process = [&](const Chunk& cur, int it, uint32_t id) __attribute__((always_inline)) {
-        const int chunk = chunk_of(it), t0 = chunk * kChunk, t1 = t0 + kChunk;
-        const bool held = id < p.pages;
-        if (held && t1 <= L && (t0 >= lo || t1 <= sinks)) process_as(cur, chunk, true, std::false_type{});
-        else process_as(cur, chunk, held, std::true_type{});
+                acc[4 * u + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(vh[0][0][j], vh[0][1][j], vh[1][0][j], vh[1][1][j]), b8, acc[4 * u + j], 0, 0, 0);
+        }
     };
 
+    // Two copies of the arithmetic and no more: a call on short sequences runs through its code once, and pays for fetching it.  The wave's
+    // last turn therefore requests its own chunk again (which is in the caches), as does a wave without chunks the list's last.
     int it = 0;
     for (; it + 2 < n_iter; it += 2) {
         load_chunk(Bf, chunk_of(it + 1), id_b);
@@ -546,35 +574,43 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(PK 
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) part[16 * kb + 4 * x + 64 * u + j] = acc[4 * u + j][x];
-        if (kb == 0) { part[kD] = m; part[kD + 1] = l; }
+            for (int x = 0; x < 4; ++x)
+                *reinterpret_cast<float4*>(part + 16 * kb + 4 * x + 64 * u) = make_float4(acc[4 * u][x], acc[4 * u + 1][x], acc[4 * u + 2][x], acc[4 * u + 3][x]);
+        if (kb == 0) *reinterpret_cast<float2*>(part + kD) = make_float2(m, l);
     }
     __syncthreads();
-    constexpr int N = kWaves * PK;                       // partial results of a head
-    float* mine = p.parts + ((size_t)bh * p.ns + split) * R * kPartial;
-    for (int x = threadIdx.x; x < R * kD; x += 64 * kWaves) {
-        const int r = x / kD, d = x % kD;
+    constexpr int N = kWaves * PK;                           // partial results of a head
+    const int n4 = R * (kD / 4);                         // results, four elements each
+    float* mine = p.parts + ((size_t)bh * ns + split) * R * kPartial;
+    auto write_out = [&](int x, float4 num, float den) {
+        const float inv = den > 0.f ? 1.f / den : 1.f;   // nothing seen: zero, as the sums are (NaN stays)
+        const h2 a = {(_Float16)(num.x * inv), (_Float16)(num.y * inv)}, c = {(_Float16)(num.z * inv), (_Float16)(num.w * inv)};
+        reinterpret_cast<uint2*>(out_bh)[x] = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
+    };
+    for (int x = threadIdx.x; x < n4; x += 64 * kWaves) {
+        const int r = x / (kD / 4), d = x % (kD / 4) * 4;
         const float* part = s_part + r * kPartial;
-        float mm = -1e30f;
+        float mm = -1e29f;
 #pragma unroll
         for (int i = 0; i < N; ++i) mm = fmaxf(mm, part[i * R * kPartial + kD]);
-        float num = 0.f, den = 0.f;
+        float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+        float den = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float f = __builtin_amdgcn_exp2f(part[i * R * kPartial + kD] - mm);
-            num = fmaf(part[i * R * kPartial + d], f, num);
-            den = fmaf(part[i * R * kPartial + kD + 1], f, den);
+            const float2 ml = *reinterpret_cast<const float2*>(part + i * R * kPartial + kD);
+            const float4 a = *reinterpret_cast<const float4*>(part + i * R * kPartial + d);
+            const float f = __builtin_amdgcn_exp2f(ml.x - mm);
+            num.x = fmaf(a.x, f, num.x); num.y = fmaf(a.y, f, num.y); num.z = fmaf(a.z, f, num.z); num.w = fmaf(a.w, f, num.w);
+            den = fmaf(ml.y, f, den);
         }
         if (nwg == 1) {
-            out_bh[x] = __float2half_rn(den > 0.f ? num / den : num);      // nothing seen: zero (NaN stays)
+            write_out(x, num, den);
         } else {
-            __hip_atomic_store(mine + r * kPartial + d, num, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (d == 0) {
-                __hip_atomic_store(mine + r * kPartial + kD, mm, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                __hip_atomic_store(mine + r * kPartial + kD + 1, den, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
+            auto put = [&](int at, float4 v) {
+                store_through(reinterpret_cast<int4*>(mine + r * kPartial + at), __float_as_int(v.x), __float_as_int(v.y), __float_as_int(v.z), __float_as_int(v.w));
+            };
+            put(d, num);
+            if (d == 0) put(kD, make_float4(mm, den, 0.f, 0.f));
         }
     }
     if (nwg == 1) return;
@@ -588,32 +624,80 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(PK 
     }
     __syncthreads();
     if (!s_last) return;
-    const float* parts = p.parts + (size_t)bh * p.ns * R * kPartial;
-    for (int x = threadIdx.x; x < R * kD; x += 64 * kWaves) {
-        const int r = x / kD, d = x % kD;
-        float mm = -1e30f, num = 0.f, den = 0.f;
-        for (int s0 = 0; s0 < nwg; s0 += 8) {
-            float a[8], ms[8], ls[8];
+    // The join: `groups` groups of n4 threads take the workgroups' sums in turn, kInFlight in flight beside the
+    // maxima; the groups' own sums meet in LDS.
+    const float* parts = p.parts + (size_t)bh * ns * R * kPartial;
+    float* s_factor = s_part;                            // [nwg][R]: 2^(maximum - the largest)
+    float* s_den = s_factor + kMaxSplits * kMaxRatio;    // [R]
+    float4* s_sum = reinterpret_cast<float4*>(s_den + kMaxRatio);          // [groups][n4]
+    const int groups = max(1, 64 * kWaves / n4);
+    const int g0 = groups > 1 ? (int)threadIdx.x / n4 : 0;
+    int x = groups > 1 ? (int)threadIdx.x - g0 * n4 : (int)threadIdx.x, s0 = g0;
+    bool some = g0 < groups && x < n4;
+    float4 a[kInFlight];
+    auto fetch = [&]() __attribute__((always_inline)) {
+        const float* at = parts + (size_t)(some ? x / (kD / 4) : 0) * kPartial + (some ? x % (kD / 4) * 4 : 0);
 #pragma unroll
-            for (int s = 0; s < 8; ++s) {
-                float* at = const_cast<float*>(parts) + ((size_t)min(s0 + s, nwg - 1) * R + r) * kPartial;
-                a[s] = __hip_atomic_load(at + d, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                ms[s] = __hip_atomic_load(at + kD, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                ls[s] = __hip_atomic_load(at + kD + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            float top = mm;
-#pragma unroll
-            for (int s = 0; s < 8; ++s) top = fmaxf(top, ms[s]);
-            const float keep = __builtin_amdgcn_exp2f(mm - top);
-            num *= keep; den *= keep; mm = top;
-#pragma unroll
-            for (int s = 0; s < 8; ++s) {
-                const float f = s0 + s < nwg ? __builtin_amdgcn_exp2f(ms[s] - top) : 0.f;
-                num = fmaf(a[s], f, num);
-                den = fmaf(ls[s], f, den);
-            }
+        for (int i = 0; i < kInFlight; ++i) {
+            a[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (s0 + i * groups < nwg) a[i] = load_part(at + (size_t)(s0 + i * groups) * R * kPartial);
         }
-        out_bh[x] = __float2half_rn(den > 0.f ? num / den : num);
+    };
+    unsigned long long ml[kMaxRatio / kWaves];           // a wave per head, a lane per workgroup: maximum and weight sum
+#pragma unroll
+    for (int i = 0; i < kMaxRatio / kWaves; ++i)
+        ml[i] = __hip_atomic_load(reinterpret_cast<unsigned long long*>(const_cast<float*>(parts) + ((size_t)min(lane, nwg - 1) * R + min(wave + i * kWaves, R - 1)) * kPartial + kD),
+                                  __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    fetch();
+#pragma unroll
+    for (int i = 0; i < kMaxRatio / kWaves; ++i) {
+        const int r = wave + i * kWaves;
+        if (r >= R) break;
+        const float ms = __uint_as_float((uint32_t)ml[i]);
+        float top = ms;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+        const float f = lane < nwg ? __builtin_amdgcn_exp2f(ms - top) : 0.f;
+        float den = lane < nwg ? __uint_as_float((uint32_t)(ml[i] >> 32)) * f : 0.f;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) den += __shfl_xor(den, o, 64);
+        s_factor[lane * R + r] = f;
+        if (lane == 0) s_den[r] = den;
+    }
+    __syncthreads();
+    while (true) {                                       // (once, unless a KV head serves more heads than the threads have sums for)
+        const int r = some ? x / (kD / 4) : 0;
+        float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+        while (true) {
+#pragma unroll
+            for (int i = 0; i < kInFlight; ++i) {
+                const int s = s0 + i * groups;
+                const float f = s < nwg ? s_factor[s * R + r] : 0.f;
+                num.x = fmaf(a[i].x, f, num.x); num.y = fmaf(a[i].y, f, num.y); num.z = fmaf(a[i].z, f, num.z); num.w = fmaf(a[i].w, f, num.w);
+            }
+            s0 += kInFlight * groups;
+            if (s0 >= nwg) break;
+            fetch();
+        }
+        if (groups > 1) {
+            if (some) s_sum[g0 * n4 + x] = num;
+            break;
+        }
+        if (some) write_out(x, num, s_den[r]);
+        x += 64 * kWaves;
+        s0 = 0;
+        some = x < n4;
+        if (!some) return;
+        fetch();
+    }
+    __syncthreads();
+    for (int y = threadIdx.x; y < n4; y += 64 * kWaves) {
+        float4 num = s_sum[y];
+        for (int g = 1; g < groups; ++g) {
+            const float4 c = s_sum[g * n4 + y];
+            num.x += c.x; num.y += c.y; num.z += c.z; num.w += c.w;
+        }
+        write_out(y, num, s_den[y / (kD / 4)]);
     }
 }
 
@@ -662,14 +746,14 @@ static int64_t most_seen(int64_t width, int64_t window, int64_t sinks)
     const int64_t S = width * kPageTokens;
     return window ? std::min(S, window + sinks) : S;
 }
-constexpr int kDeal = 2;                                 // chunks that a wave is given before another workgroup attends
 static int paged_splits(int64_t B, int64_t Hkv, int64_t width, int64_t window, int64_t sinks)
 {
     const int64_t pairs = B * Hkv;
     if (pairs <= 0 || pairs > kMaxCounters) return 1;
     int64_t ns = 512 / pairs;
     ns = std::min<int64_t>(ns, kMaxSplits);
-    ns = std::min<int64_t>(ns, (most_seen(width, window, sinks) + kChunk * kWaves * kDeal - 1) / (kChunk * kWaves * kDeal));
+    ns = std::min<int64_t>(ns, (most_seen(width, window, sinks) / kChunk + 2 + 2 * kWaves - 1) / (2 * kWaves));
+    if (most_seen(width, window, sinks) / kChunk + 2 <= kAlone * kWaves) return 1;
     return (int)std::max<int64_t>(ns, 1);
 }
 
@@ -683,24 +767,21 @@ hipError_t launch_paged_decode(const void* q, int64_t q_stride, const uint8_t* p
                                const int32_t* seq_lens, int64_t B, int64_t H, int64_t Hkv, int64_t window, int64_t sinks, void* out,
                                void* workspace, hipStream_t s)
 {
-    DecodeArgs p{};
+    DecodeTail p{};
     p.q = static_cast<const __half*>(q); p.q_stride = q_stride;
-    p.pool = pool; p.pages = (uint32_t)pages; p.table = table; p.width = (int)width;
-    p.seq_lens = seq_lens;
     p.out = static_cast<__half*>(out);
-    p.Hkv = (int)Hkv; p.R = (int)(H / Hkv);
-    p.ns = workspace ? paged_splits(B, Hkv, width, window, sinks) : 1;
-    p.deal = kDeal;
-    p.window = (int)window; p.sinks = window ? (int)sinks : 0;
+    p.R = (int)(H / Hkv);
+    p.sinks = window ? (int)sinks : 0;
     p.counters = static_cast<int*>(workspace);
     p.parts = workspace ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes) : nullptr;
+    const int ns = workspace ? paged_splits(B, Hkv, width, window, sinks) : 1;
     const bool nt = B * Hkv * most_seen(width, window, sinks) / kPageTokens * kPageBytes >= (int64_t)24 << 20;
-    const dim3 grid((unsigned)(B * Hkv), (unsigned)p.ns);
+    const dim3 grid((unsigned)(B * Hkv), (unsigned)ns);
     const int PK = p.R <= 8 ? 2 : 1;
-    const size_t lds = (size_t)kWaves * PK * p.R * kPartial * sizeof(float);
+    const size_t lds = std::max((size_t)kWaves * PK * p.R * kPartial * sizeof(float), (kMaxSplits + 1) * kMaxRatio * sizeof(float) + 64 * kWaves * sizeof(float4));
     auto* kernel = PK == 2 ? (nt ? paged_decode_kernel<2, true> : paged_decode_kernel<2, false>)
                            : (nt ? paged_decode_kernel<1, true> : paged_decode_kernel<1, false>);
-    kernel<<<grid, 64 * kWaves, lds, s>>>(p);
+    kernel<<<grid, 64 * kWaves, lds, s>>>(pool, table, seq_lens, (uint32_t)pages, (int)width, (int)Hkv, ns, (int)window, p);
     return hipGetLastError();
 }
 
