@@ -385,7 +385,9 @@ def test_prefill_strided_slices():
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (30, 2)])
 def test_prefill_infinities_and_nan_reach_only_the_queries_that_see_them(window, sinks):
-    """Values and keys that are not finite at some tokens: earlier queries, and later ones whose window has passed, are as without."""
+    """Values and keys that are not finite at some tokens: earlier queries, and later ones whose window has passed, are as without: within the
+    bound above of the same float64 result.  (Rows that share a tile with such a value are summed in another order than without it,
+    so their bits may differ; the bound holds for any order.)"""
     H, Hkv, T = 2, 1, 200
     q, k, v, cu, _ = _prompts([T], [0], H, Hkv, 105)
     clean = api.attention_prefill(q, k, v, _ints(cu), _ints(cu), window=window, sinks=sinks)
@@ -395,11 +397,16 @@ def test_prefill_infinities_and_nan_reach_only_the_queries_that_see_them(window,
         v2[t, 0, d] = x
     got = api.attention_prefill(q, k, v2, _ints(cu), _ints(cu), window=window, sinks=sinks).cpu().numpy().astype(np.float64)
     clean = clean.cpu().numpy()
+    kd, vd, qd = (x.cpu().numpy().astype(np.float64) for x in (k, v, q))
+    ref, spread = paged.attention(qd, kd, vd, np.arange(T), window, sinks)
+    tol, _ = _bound(qd, kd, ref, spread, T)
+    tol = tol + T * 2.0 ** -25 * np.abs(vd).max() + 2.0 ** -25
+    assert (np.abs(clean - ref) <= tol).all()
     for i in range(T):
         for d in (2, 3, 4, 5):
             seen = [x for t, (dd, x) in spots.items() if dd == d and paged.visible(i, t, window, sinks)]
             if not seen:
-                assert np.array_equal(got[i, :, d], clean[i, :, d].astype(np.float64)), (i, d)
+                assert (np.abs(got[i, :, d] - ref[i, :, d]) <= tol[i, :, d]).all(), (i, d)
             elif any(np.isnan(seen)) or len(set(seen)) > 1:
                 assert np.isnan(got[i, :, d]).all(), (i, d)
             else:                                                          # (a weight may be zero: NaN)
