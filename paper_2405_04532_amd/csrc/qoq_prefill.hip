@@ -19,6 +19,7 @@
 #include "qoq_gemm_common.h"
 #include "qoq_kv4_common.h"
 #include "qoq_ragged.h"
+#include "qoq_workspace.h"
 
 namespace qoq {
 namespace {
@@ -27,9 +28,14 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBM = 128, kBN = 64, kPrefillThreads = 256;
+constexpr int kRows = 32, kKeys = 32;                    // of the narrow kernel's tiles
+constexpr int kPart = kD + 4;                            // floats of a row's partial result: sums, maximum, weight sum, whether to do it again
 constexpr int kRowBytes = kD * 2;                        // 256: sixteen 16-byte chunks
 constexpr int kTileBytes = kBN * kRowBytes;              // 16 KiB of keys, as much of values
 constexpr float kScale = 1.4426950408889634f * 0.08838834764831845f;      // log2(e) / sqrt(128)
+constexpr int kMaxParts = 64;                            // workgroups to a row tile
+constexpr int kWideDeal = 8;                            // key tiles that a workgroup is given before another one attends
+constexpr int kNarrowDeal = 2;                          // key tiles that a wave is given before another workgroup attends
 constexpr float kSlack = 8.f / kScale;                   // in units of the scores
 
 struct PrefillArgs {
@@ -39,6 +45,9 @@ struct PrefillArgs {
     int64_t q_stride, k_stride, v_stride;                // elements per token
     int M, Mk, B, H, Hkv, r, window, sinks;
     uint32_t slots;
+    // the narrow kernel's: workgroups that stand by for a row tile, and their partial results
+    int ns;
+    float* parts;
 };
 
 // LDS position of chunk c of row `row`.  Keys are read 32 rows at a time, the same chunk of each: c ^ row % 16 spreads 16
@@ -53,6 +62,118 @@ __device__ __forceinline__ h8 v_operand(const uint8_t* lo, const uint8_t* hi)   
     return __builtin_bit_cast(h8, t);
 }
 
+// Where a workgroup's rows lie: ROWS rows of a (sequence, KV head), and the list of key tiles of BN keys that some of them see: those of
+// the sinks, then those of the window (without one all up to the last row's position).
+template <int ROWS, int BN>
+struct RowTile {
+    int q0, Tq, k0, Tk, first;                           // the sequence's queries and keys; the tile's first row, of Tq r
+    int lo_pos, hi_pos;                                  // positions of its first and last row
+    int n_first, gap, n;                                 // key tile i of the list: i < n_first ? i : i + gap
+
+    __device__ __forceinline__ bool find(const PrefillArgs& p, uint32_t slot, int lane)
+    {
+        const int b = count_before(p.B, lane, [&](int i) { return (int64_t)p.cu_q[i] * p.r / ROWS + i <= (int64_t)slot; });
+        if (b >= p.B) return false;
+        auto bounded = [](int v, int most) { return min(max(v, 0), most); };
+        q0 = bounded(p.cu_q[b], p.M);
+        k0 = bounded(p.cu_k[b], p.Mk);
+        Tq = bounded(p.cu_q[b + 1], p.M) - q0;
+        Tk = max(bounded(p.cu_k[b + 1], p.Mk) - k0, 0);
+        const int64_t tile = (int64_t)slot - ((int64_t)p.cu_q[b] * p.r / ROWS + b);
+        if (Tq <= 0 || tile < 0 || tile * ROWS >= (int64_t)Tq * p.r) return false;
+        first = (int)(tile * ROWS);                      // below 2^31
+        lo_pos = Tk - Tq + first / p.r;
+        hi_pos = Tk - Tq + min((first + ROWS - 1) / p.r, Tq - 1);
+        const int end = max(hi_pos + 1, 0), from = p.window ? max(lo_pos - p.window + 1, 0) : 0, tiles = (end + BN - 1) / BN;
+        n_first = min((p.sinks + BN - 1) / BN, tiles);
+        gap = max(min(from / BN, tiles) - n_first, 0);
+        n = tiles - gap;
+        return true;
+    }
+    __device__ __forceinline__ int rows(const PrefillArgs& p) const { return min(ROWS, Tq * p.r - first); }
+    __device__ __forceinline__ int tile_of(int i) const { return i < n_first ? i : i + gap; }
+    // query and head of a row of the tile
+    __device__ __forceinline__ void row(const PrefillArgs& p, int x, int& query, int& head) const
+    {
+        query = (first + x) / p.r;
+        head = first + x - query * p.r;
+    }
+};
+
+// workgroups that share the keys of a row tile: as many as stand by, get their deal of key tiles each
+template <int ROWS, int BN>
+__device__ __forceinline__ int attending(const PrefillArgs& p, const RowTile<ROWS, BN>& t)
+{
+    constexpr int deal = ROWS == kBM ? kWideDeal : 4 * kNarrowDeal;
+    return min(p.ns, max(1, (t.n + deal - 1) / deal));
+}
+
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }       // a row that sees nothing is zero (NaN stays)
+
+// A zero weight times infinity or NaN is NaN, in rows that do not see that value.  Rows `begin` .. `end` - 1 of a tile that shares keys with such
+// a value are done again by a wave, one after the other, with the keys they see and no others: 64 scores at a time, a lane each, then
+// two elements of the values a lane.
+template <int ROWS, int BN>
+__device__ void redo_rows(const PrefillArgs& p, const RowTile<ROWS, BN>& t, int hk, int begin, int end, int lane)
+{
+    const __half* k_rows = p.k + (int64_t)t.k0 * p.k_stride + hk * kD;
+    const __half* v_rows = p.v + (int64_t)t.k0 * p.v_stride + hk * kD;
+    for (int x = begin; x < min(end, t.rows(p)); ++x) {
+        int query, head;
+        t.row(p, x, query, head);
+        const int pos = t.Tk - t.Tq + query;
+        const __half* q_row = p.q + (int64_t)(t.q0 + query) * p.q_stride + (hk * p.r + head) * kD;
+        float top = -1e30f, sum = 0.f, o0 = 0.f, o1 = 0.f;
+        for (int i = 0; i < t.n; ++i)
+            for (int at = t.tile_of(i) * BN; at < t.tile_of(i) * BN + BN; at += 64) {
+                const int key = at + lane;
+                const bool sees = key < t.tile_of(i) * BN + BN && key <= pos && (!p.window || key > pos - p.window || key < p.sinks);
+                float s = 0.f;
+                if (sees)
+                    for (int d = 0; d < kD; ++d) s = fmaf(__half2float(k_rows[(int64_t)key * p.k_stride + d]), __half2float(q_row[d]), s);
+                float most = sees ? s : -__builtin_inff();
+                for (int step = 32; step; step >>= 1) most = fmaxf(most, __shfl_xor(most, step, 64));
+                most = fmaxf(most, top);
+                const float keep = __builtin_amdgcn_exp2f((top - most) * kScale), weight = sees ? __builtin_amdgcn_exp2f((s - most) * kScale) : 0.f;
+                top = most;
+                sum = sum * keep + weight;
+                o0 *= keep;
+                o1 *= keep;
+                for (uint64_t left = __builtin_amdgcn_ballot_w64(sees); left; left &= left - 1) {
+                    const int from = __ffsll((unsigned long long)left) - 1;
+                    const float w = __shfl(weight, from, 64);
+                    const __half* v_row = v_rows + (int64_t)(at + from) * p.v_stride + 2 * lane;
+                    o0 = fmaf(w, __half2float(v_row[0]), o0);
+                    o1 = fmaf(w, __half2float(v_row[1]), o1);
+                }
+            }
+        for (int step = 32; step; step >>= 1) sum += __shfl_xor(sum, step, 64);
+        const float inv = inverse(sum);
+        const h2 pair = {(_Float16)(o0 * inv), (_Float16)(o1 * inv)};
+        reinterpret_cast<uint32_t*>(p.out + ((int64_t)(t.q0 + query) * p.H + hk * p.r + head) * kD)[lane] = __builtin_bit_cast(uint32_t, pair);
+    }
+}
+
+// four elements of a row's result
+template <int ROWS, int BN>
+__device__ __forceinline__ void write_out(const PrefillArgs& p, const RowTile<ROWS, BN>& t, int hk, int x, int d, float4 num, float inv)
+{
+    int query, head;
+    t.row(p, x, query, head);
+    const h2 a = {(_Float16)(num.x * inv), (_Float16)(num.y * inv)}, c = {(_Float16)(num.z * inv), (_Float16)(num.w * inv)};
+    *reinterpret_cast<uint2*>(p.out + ((int64_t)(t.q0 + query) * p.H + hk * p.r + head) * kD + d) =
+        make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
+}
+
+// NaN if some element is not finite
+__device__ __forceinline__ float not_finite(const h8& a, float bad)
+{
+    struct { h2 v[4]; } t = __builtin_bit_cast(decltype(t), a);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) bad = __builtin_amdgcn_fdot2(t.v[x], (h2){(_Float16)0.f, (_Float16)0.f}, bad, false);
+    return bad;
+}
+
 __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void prefill_kernel(PrefillArgs p)
 {
     __shared__ __align__(256) uint8_t s_tiles[2][2][kTileBytes];           // [buffer][keys | values]
@@ -61,34 +182,26 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
     // the last tiles of a sequence, which see the most keys, come first
     const uint32_t slot = p.slots - 1 - blockIdx.x / (uint32_t)p.Hkv;
     const int hk = (int)(blockIdx.x % (uint32_t)p.Hkv);
-    const int b = count_before(p.B, lane, [&](int i) { return ((int64_t)p.cu_q[i] * p.r >> 7) + i <= (int64_t)slot; });
-    if (b >= p.B) return;
-    auto bounded = [](int v, int most) { return min(max(v, 0), most); };
-    const int q0 = bounded(p.cu_q[b], p.M), q1 = bounded(p.cu_q[b + 1], p.M), k0 = bounded(p.cu_k[b], p.Mk), k1 = bounded(p.cu_k[b + 1], p.Mk);
-    const int Tq = q1 - q0, Tk = max(k1 - k0, 0);
-    const int64_t tile = (int64_t)slot - (((int64_t)p.cu_q[b] * p.r >> 7) + b);
-    if (Tq <= 0 || tile < 0 || tile * kBM >= (int64_t)Tq * p.r) return;
-    const int first = (int)(tile * kBM);                                   // row of the (sequence, KV head); below 2^31
+    RowTile<kBM, kBN> t;
+    if (!t.find(p, slot, lane)) return;
+    // workgroups that share the keys take one range of the list after the other
+    const int nwg = attending(p, t), split = blockIdx.y, per = (t.n + nwg - 1) / nwg, it0 = min(split * per, t.n), n = min(t.n, it0 + per) - it0;
+    if (split >= nwg) return;
+    const int q0 = t.q0, Tq = t.Tq, Tk = t.Tk, n_first = t.n_first, gap = t.gap;
     // this lane's row
-    const int rho = first + wave * 32 + col, i = rho / p.r, j = rho - i * p.r;
+    int i, j;
+    t.row(p, wave * 32 + col, i, j);
     const bool there = i < Tq;
     const int pos = Tk - Tq + i;
-    // the wave's and the workgroup's positions
-    const int i_wave = (first + wave * 32) / p.r, i_wave_end = min((first + wave * 32 + 31) / p.r, Tq - 1);
-    const int lo_wave = Tk - Tq + i_wave, hi_wave = Tk - Tq + i_wave_end;  // hi < lo: no row
-    const int lo_pos = Tk - Tq + first / p.r, hi_pos = Tk - Tq + min((first + kBM - 1) / p.r, Tq - 1);
-    // the list of key tiles: those of the sinks, then those of the window
-    const int end = max(hi_pos + 1, 0), from = p.window ? max(lo_pos - p.window + 1, 0) : 0;
-    const int tiles = (end + kBN - 1) / kBN, n_first = min((p.sinks + kBN - 1) / kBN, tiles), gap = max(min(from / kBN, tiles) - n_first, 0);
-    const int n = tiles - gap;
-
+    // the wave's positions; hi < lo: no row
+    const int lo_wave = Tk - Tq + (t.first + wave * 32) / p.r, hi_wave = Tk - Tq + min((t.first + wave * 32 + 31) / p.r, Tq - 1);
     // tiles of the list that hold a key which some row of the wave sees
     const int tiles_wave = hi_wave < max(lo_wave, 0) ? 0 : hi_wave / kBN + 1;
-    const int n_wave = tiles_wave <= n_first ? tiles_wave : max(tiles_wave - gap, n_first);
+    const int n_wave = min((tiles_wave <= n_first ? tiles_wave : max(tiles_wave - gap, n_first)) - it0, n);
 
-    const __half* k_rows = p.k + (int64_t)k0 * p.k_stride + hk * kD;
-    const __half* v_rows = p.v + (int64_t)k0 * p.v_stride + hk * kD;
-    auto tile_of = [&](int it) __attribute__((always_inline)) { return it < n_first ? it : it + gap; };
+    const __half* k_rows = p.k + (int64_t)t.k0 * p.k_stride + hk * kD;
+    const __half* v_rows = p.v + (int64_t)t.k0 * p.v_stride + hk * kD;
+    auto tile_of = [&](int it) __attribute__((always_inline)) { return t.tile_of(it0 + it); };
     // A wave copies 16 rows of a tile, four at a time; rows past the end repeat the last one.  Within a tile that is whole the lanes' offsets
     // never change: row 16 wave + 4 x + lane / 16 has its chunks at place ^ 4 x (keys), or where every fourth row has them (values).
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&s_tiles[0][0][0] + wave * 4096;
@@ -159,12 +272,6 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
     auto values = [&](int it, int s, int d) __attribute__((always_inline)) {   // v's operand: 16 keys of step s, 32 elements of block d
         const uint8_t* at = s_tiles[it & 1][1] + 16 * s * kRowBytes + v_off[d];
         return v_operand(at, at + 8 * kRowBytes);
-    };
-    auto not_finite = [&](const h8& a, float bad) __attribute__((always_inline)) {  // NaN if some element is not finite
-        struct { h2 v[4]; } t = __builtin_bit_cast(decltype(t), a);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) bad = __builtin_amdgcn_fdot2(t.v[x], (h2){(_Float16)0.f, (_Float16)0.f}, bad, false);
-        return bad;
     };
     bool odd = false;                                                      // some value that not every row sees is not finite
     // One tile: the weights of scores `sc` (with their maximum `top`, m among them) and their product with the values, while the
@@ -272,61 +379,278 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
         turn(it, sa, sb);
         if (it + 1 < n) turn(it + 1, sb, sa);
     }
-    if (odd) {
-        // A zero weight times infinity or NaN is NaN, in rows that do not see that value.  Such a wave's rows are done again here, one after
-        // the other, with the keys they see and no others: 64 scores at a time, a lane each, then two elements of the values a lane.
-        for (int x = 0; x < 32; ++x) {
-            const int row = first + wave * 32 + x, qi = row / p.r, h = hk * p.r + row - qi * p.r, at = Tk - Tq + qi;
-            if (qi >= Tq) break;
-            const __half* q_row = p.q + (int64_t)(q0 + qi) * p.q_stride + h * kD;
-            float top = -1e30f, sum = 0.f, o0 = 0.f, o1 = 0.f;
-            for (int it = 0; it < n; ++it) {
-                const int t = tile_of(it) * kBN + lane;
-                const bool sees = t <= at && (!p.window || t > at - p.window || t < p.sinks);
-                float s = 0.f;
-                if (sees)
-                    for (int d = 0; d < kD; ++d) s = fmaf(__half2float(k_rows[(int64_t)t * p.k_stride + d]), __half2float(q_row[d]), s);
-                float most = sees ? s : -__builtin_inff();
-                for (int step = 32; step; step >>= 1) most = fmaxf(most, __shfl_xor(most, step, 64));
-                most = fmaxf(most, top);
-                const float keep = __builtin_amdgcn_exp2f((top - most) * kScale), weight = sees ? __builtin_amdgcn_exp2f((s - most) * kScale) : 0.f;
-                top = most;
-                sum = sum * keep + weight;
-                o0 *= keep;
-                o1 *= keep;
-                for (uint64_t left = __builtin_amdgcn_ballot_w64(sees); left; left &= left - 1) {
-                    const int from = __ffsll((unsigned long long)left) - 1;
-                    const float wt = __shfl(weight, from, 64);
-                    const __half* v_row = v_rows + (int64_t)(tile_of(it) * kBN + from) * p.v_stride + 2 * lane;
-                    o0 = fmaf(wt, __half2float(v_row[0]), o0);
-                    o1 = fmaf(wt, __half2float(v_row[1]), o1);
-                }
-            }
-            for (int step = 32; step; step >>= 1) sum += __shfl_xor(sum, step, 64);
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            const h2 pair = {(_Float16)(o0 * inv), (_Float16)(o1 * inv)};
-            reinterpret_cast<uint32_t*>(p.out + ((int64_t)(q0 + qi) * p.H + h) * kD)[lane] = __builtin_bit_cast(uint32_t, pair);
-        }
+    if (odd && nwg == 1) {
+        redo_rows(p, t, hk, wave * 32, wave * 32 + 32, lane);
         return;
     }
     float total = (l[0] + l[1]) + (l[2] + l[3]);
     total += __shfl_xor(total, 32, 64);
     if (!there) return;
-    const float inv = total == 0.f ? 0.f : 1.f / total;                    // a row that sees nothing is zero (NaN stays)
-    __half* dst = p.out + ((int64_t)(q0 + i) * p.H + hk * p.r + j) * kD + 4 * hl;
+    if (nwg > 1) {                                                         // to be added up by the second launch
+        float* mine = p.parts + ((((size_t)slot * p.Hkv + hk) * p.ns + split) * kBM + wave * 32 + col) * kPart;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                *reinterpret_cast<float4*>(mine + 32 * d + 8 * y + 4 * hl) = make_float4(acc[d][4 * y], acc[d][4 * y + 1], acc[d][4 * y + 2], acc[d][4 * y + 3]);
+        if (hl == 0) *reinterpret_cast<float4*>(mine + kD) = make_float4(m * kScale, total, odd ? 1.f : 0.f, 0.f);
+        return;
+    }
+    const float inv = inverse(total);
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            const h2 a = {(_Float16)(acc[d][4 * y] * inv), (_Float16)(acc[d][4 * y + 1] * inv)};
-            const h2 c = {(_Float16)(acc[d][4 * y + 2] * inv), (_Float16)(acc[d][4 * y + 3] * inv)};
-            *reinterpret_cast<uint2*>(dst + 32 * d + 8 * y) = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
+        for (int y = 0; y < 4; ++y)
+            write_out(p, t, hk, wave * 32 + col, 32 * d + 8 * y + 4 * hl, make_float4(acc[d][4 * y], acc[d][4 * y + 1], acc[d][4 * y + 2], acc[d][4 * y + 3]), inv);
+}
+
+// ------------------------------------------------------------------------------------------
+// Few rows.  A workgroup takes 32 rows, and its four waves take key tiles of 32 in turn, each through a ring of its own in LDS (two tiles of
+// keys and values), without meeting; p.ns workgroups stand by for a row tile, of which as many attend as get kNarrowDeal key tiles a
+// wave.  Sums, maxima and weight sums of the waves meet in LDS, those of the workgroups in the workspace, added up by a second launch.
+// ------------------------------------------------------------------------------------------
+constexpr int kRing = 2 * kKeys * kRowBytes;             // a key tile's keys and values
+
+__global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void prefill_narrow_kernel(PrefillArgs p)
+{
+    __shared__ __align__(256) uint8_t s_ring[4][2][kRing];                 // [wave][buffer][keys, values]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hl = lane >> 5, col = lane & 31;
+    const uint32_t slot = p.slots - 1 - blockIdx.x / (uint32_t)p.Hkv;
+    const int hk = (int)(blockIdx.x % (uint32_t)p.Hkv), split = blockIdx.y;
+    RowTile<kRows, kKeys> t;
+    if (!t.find(p, slot, lane)) return;
+    const int nwg = attending(p, t);
+    if (split >= nwg) return;
+    int i, j;
+    t.row(p, col, i, j);
+    const bool there = i < t.Tq;
+    const int pos = t.Tk - t.Tq + i, at_once = 4 * nwg, mine0 = split * 4 + wave;
+    const int n = mine0 < t.n ? (t.n - mine0 + at_once - 1) / at_once : 0;
+
+    const __half* k_rows = p.k + (int64_t)t.k0 * p.k_stride + hk * kD;
+    const __half* v_rows = p.v + (int64_t)t.k0 * p.v_stride + hk * kD;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&s_ring[wave][0][0];
+    auto first_key = [&](int it) __attribute__((always_inline)) { return t.tile_of(mine0 + it * at_once) * kKeys; };
+    auto fetch = [&](int it) __attribute__((always_inline)) {              // rows past the end repeat the last one
+        const int t0 = first_key(it), most = t.Tk - 1 - t0;
+        const uint32_t to = lds + (it & 1) * kRing;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int row = 4 * x + (lane >> 4);
+            dma16(k_rows + (int64_t)t0 * p.k_stride, (uint32_t)(min(row, most) * (int)p.k_stride * 2 + k_place(row, lane & 15) * 16), to + x * 1024);
         }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int row = 4 * x + (lane >> 4);
+            dma16(v_rows + (int64_t)t0 * p.v_stride, (uint32_t)(min(row, most) * (int)p.v_stride * 2 + v_place(row, lane & 15) * 16),
+                  to + kKeys * kRowBytes + x * 1024);
+        }
+    };
+    h8 qf[8];
+    {
+        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)(t.q0 + (there ? i : 0)) * p.q_stride + (hk * p.r + (there ? j : 0)) * kD);
+        const uint32_t some = there ? ~0u : 0u;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const uint4 x = src[2 * s + hl];
+            qf[s] = __builtin_bit_cast(h8, make_uint4(x.x & some, x.y & some, x.z & some, x.w & some));
+        }
+    }
+    if (n > 0) fetch(0);
+    if (n > 1) fetch(1);
+    float m = -1e30f, l[4] = {0.f, 0.f, 0.f, 0.f};
+    f16v acc[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) acc[d] = (f16v)(0.f);
+    const int key = 4 * hl + ((lane & 15) >> 2), within = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    bool odd = false;
+    for (int it = 0; it < n; ++it) {
+        if (it + 1 < n) wait_vmcnt<16>();                                  // the next tile may still be on its way
+        else wait_vmcnt<0>();
+        const uint8_t* ks = s_ring[wave][it & 1];
+        const uint8_t* vs = ks + kKeys * kRowBytes;
+        auto values = [&](int s, int d) __attribute__((always_inline)) {
+            const uint8_t* at = vs + (16 * s + key) * kRowBytes + v_place(key, 4 * d + within) * 16 + (lane & 1) * 8;
+            return v_operand(at, at + 8 * kRowBytes);
+        };
+        f16v sc[2] = {(f16v)(0.f), (f16v)(0.f)};                           // two chains of products
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+            sc[s & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(ks + col * kRowBytes + k_place(col, 2 * s + hl) * 16), qf[s], sc[s & 1], 0, 0, 0);
+        sc[0] += sc[1];
+        const int t0 = first_key(it), t1 = t0 + kKeys - 1;
+        if (!(t1 <= t.lo_pos && (!p.window || t0 > t.hi_pos - p.window || t1 < p.sinks))) {
+            const int at_most = (there ? pos - t0 : -1) - 4 * hl, above = (p.window ? pos - p.window - t0 : -1) - 4 * hl, below = p.sinks - t0 - 4 * hl;
+#pragma unroll
+            for (int y = 0; y < 16; ++y) {
+                const int e = 8 * (y >> 2) + (y & 3);
+                sc[0][y] = e <= at_most && (e > above || e < below) ? sc[0][y] : -__builtin_inff();
+            }
+            float bad = 0.f;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) bad = not_finite(values(s, d), bad);
+            if (__builtin_amdgcn_ballot_w64(bad != bad) != 0) odd = true;
+        }
+        float top = m;
+#pragma unroll
+        for (int y = 0; y < 16; ++y) top = fmaxf(top, sc[0][y]);
+        top = max_other_half(top);
+        if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
+            const float alpha = __builtin_amdgcn_exp2f((m - top) * kScale);
+            m = top;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) l[x] *= alpha;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) acc[d] *= alpha;
+        }
+        const float shift = -m * kScale;
+        h8 w[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            h2 o[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                o[y] = (h2){(_Float16)__builtin_amdgcn_exp2f(fmaf(sc[0][8 * s + 2 * y], kScale, shift)),
+                            (_Float16)__builtin_amdgcn_exp2f(fmaf(sc[0][8 * s + 2 * y + 1], kScale, shift))};
+                l[y] = __builtin_amdgcn_fdot2(o[y], (h2){(_Float16)1.f, (_Float16)1.f}, l[y], false);
+            }
+            w[s] = join(o[0], o[1], o[2], o[3]);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values(s, d), w[s], acc[d], 0, 0, 0);
+        if (it + 2 < n) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // the ring's tile has been read
+            fetch(it + 2);
+        }
+    }
+    // ---- the waves meet ----
+    float total = (l[0] + l[1]) + (l[2] + l[3]);
+    total += __shfl_xor(total, 32, 64);
+    float* own = reinterpret_cast<float*>(&s_ring[wave][0][0]) + col * kPart;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+            *reinterpret_cast<float4*>(own + 32 * d + 8 * y + 4 * hl) = make_float4(acc[d][4 * y], acc[d][4 * y + 1], acc[d][4 * y + 2], acc[d][4 * y + 3]);
+    if (hl == 0) *reinterpret_cast<float4*>(own + kD) = make_float4(m * kScale, total, odd ? 1.f : 0.f, 0.f);
+    __syncthreads();
+    const int rows = t.rows(p);
+    float* part = p.parts + (((size_t)slot * p.Hkv + hk) * p.ns + split) * kRows * kPart;
+    bool again = false;
+    for (int x = threadIdx.x; x < rows * (kD / 4); x += kPrefillThreads) {
+        const int row = x / (kD / 4), d = x % (kD / 4) * 4;
+        float4 ml[4];
+        float most = -1e30f * kScale, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            ml[w] = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(&s_ring[w][0][0]) + row * kPart + kD);
+            most = fmaxf(most, ml[w].x);
+        }
+        float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+        bool redo = false;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float4 a = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(&s_ring[w][0][0]) + row * kPart + d);
+            const float f = __builtin_amdgcn_exp2f(ml[w].x - most);
+            num.x = fmaf(a.x, f, num.x); num.y = fmaf(a.y, f, num.y); num.z = fmaf(a.z, f, num.z); num.w = fmaf(a.w, f, num.w);
+            sum = fmaf(ml[w].y, f, sum);
+            redo |= ml[w].z != 0.f;
+        }
+        again |= redo;
+        if (nwg > 1) {
+            *reinterpret_cast<float4*>(part + row * kPart + d) = num;
+            if (d == 0) *reinterpret_cast<float4*>(part + row * kPart + kD) = make_float4(most, sum, redo ? 1.f : 0.f, 0.f);
+        } else if (!redo) {
+            write_out(p, t, hk, row, d, num, inverse(sum));
+        }
+    }
+    // (a wave's `odd` stands at all of its rows, so every thread that has a row knows)
+    if (nwg == 1 && __builtin_amdgcn_ballot_w64(again) != 0) redo_rows(p, t, hk, wave * 8, wave * 8 + 8, lane);
+}
+
+// Second launch: the workgroups' partial results of a row tile, added up in their order.
+template <int ROWS, int BN>
+__global__ __launch_bounds__(kPrefillThreads) void prefill_combine_kernel(PrefillArgs p)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t slot = blockIdx.x / (uint32_t)p.Hkv;
+    const int hk = (int)(blockIdx.x % (uint32_t)p.Hkv);
+    RowTile<ROWS, BN> t;
+    if (!t.find(p, slot, lane)) return;
+    const int nwg = attending(p, t), rows = t.rows(p);
+    if (nwg == 1 || (int)blockIdx.y * 8 >= rows) return;
+    const float* parts = p.parts + ((size_t)slot * p.Hkv + hk) * p.ns * ROWS * kPart;
+    // eight rows of the tile to a workgroup, two to a wave
+    const int row = blockIdx.y * 8 + wave * 2 + (lane >> 5), d = (lane & 31) * 4;
+    const bool there = row < rows;
+    float most = -1e30f * kScale, sum = 0.f;
+    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+    bool redo = false;
+    for (int s0 = 0; s0 < nwg; s0 += 8) {
+        float4 a[8], ml[8];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const float* at = parts + ((size_t)min(s0 + s, nwg - 1) * ROWS + (there ? row : 0)) * kPart;
+            a[s] = *reinterpret_cast<const float4*>(at + d);
+            ml[s] = *reinterpret_cast<const float4*>(at + kD);
+        }
+        float top = most;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) top = fmaxf(top, ml[s].x);
+        const float keep = __builtin_amdgcn_exp2f(most - top);
+        num.x *= keep; num.y *= keep; num.z *= keep; num.w *= keep;
+        sum *= keep;
+        most = top;
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+            if (s0 + s < nwg) {
+                const float f = __builtin_amdgcn_exp2f(ml[s].x - top);
+                num.x = fmaf(a[s].x, f, num.x); num.y = fmaf(a[s].y, f, num.y); num.z = fmaf(a[s].z, f, num.z); num.w = fmaf(a[s].w, f, num.w);
+                sum = fmaf(ml[s].y, f, sum);
+                redo |= ml[s].z != 0.f;
+            }
+    }
+    if (there && !redo) write_out(p, t, hk, row, d, num, inverse(sum));
+    if (__builtin_amdgcn_ballot_w64(there && redo) != 0) redo_rows(p, t, hk, blockIdx.y * 8 + wave * 2, blockIdx.y * 8 + wave * 2 + 2, lane);
 }
 
 }  // namespace
 
-size_t prefill_workspace_bytes(int64_t, int64_t, int64_t, int64_t, int64_t, int64_t, int64_t) { return 0; }
+static int64_t row_tiles(int64_t M, int64_t B, int64_t H, int64_t Hkv, int64_t rows) { return (M * (H / Hkv) / rows + B) * Hkv; }
+// Which kernel, and how many workgroups stand by for each of its row tiles.  The host knows the rows and the sequences, not their
+// lengths: `seen` is what a row may see, of twice the mean length.
+// The narrow kernel reads the keys again for every 32 rows, the wide one for every 128, but has a compute unit's four waves on different
+// keys.  Measured, narrow and wide: 32 / 8 heads, 20 tokens behind 3000 15.0 and 17.7 us, 200 behind 4000 45 and 36, 300 behind 2000 48 and 32; 200 alone
+// 8.8 and 13.3; 32 / 32 heads, 256 alone 9.0 and 15.2, 512 18.4 and 21.5; 32 / 8 heads, 800 alone 34 and 23.
+// The keys of wide tiles are shared while there are less than two for each compute unit: 512 behind 4000 88 us whole, 60 shared; not where a
+// workgroup is through them before a second launch pays: 800 alone 23 whole, 28 shared.
+struct Plan { bool narrow; int ns; int64_t tiles; };
+static Plan prefill_plan(int64_t M, int64_t Mk, int64_t B, int64_t H, int64_t Hkv, int64_t window, int64_t sinks)
+{
+    const int64_t narrow_tiles = row_tiles(M, B, H, Hkv, kRows);
+    int64_t seen = std::min(Mk, 2 * (Mk / std::max<int64_t>(B, 1) + 1));
+    if (window) seen = std::min(seen, window + sinks + std::min<int64_t>(M, kRows));
+    const bool narrow = narrow_tiles <= 128 || (narrow_tiles <= 640 && narrow_tiles * seen <= 512 * 1024);
+    const int64_t tiles = narrow ? narrow_tiles : row_tiles(M, B, H, Hkv, kBM);
+    const int64_t deal = narrow ? 4 * kNarrowDeal * kKeys : kWideDeal * kBN;
+    int64_t ns = 1;
+    if (narrow || seen > 1024) {
+        ns = std::min<int64_t>((narrow ? 256 : 512) / std::max<int64_t>(tiles, 1), kMaxParts);
+        ns = std::min(ns, (seen + 2 * kBN + deal - 1) / deal);
+    }
+    return {narrow, (int)std::max<int64_t>(ns, 1), tiles};
+}
+
+size_t prefill_workspace_bytes(int64_t M, int64_t Mk, int64_t B, int64_t H, int64_t Hkv, int64_t window, int64_t sinks)
+{
+    const Plan plan = prefill_plan(M, Mk, B, H, Hkv, window, sinks);
+    return plan.ns <= 1 ? 0 : kCounterBytes + (size_t)(plan.tiles * plan.ns * (plan.narrow ? kRows : kBM) * kPart) * sizeof(float);
+}
 
 hipError_t launch_prefill(const Prefill& a, hipStream_t s)
 {
@@ -337,10 +661,20 @@ hipError_t launch_prefill(const Prefill& a, hipStream_t s)
     p.q_stride = a.q_stride; p.k_stride = a.k_stride; p.v_stride = a.v_stride;
     p.M = (int)a.M; p.Mk = (int)a.Mk; p.B = (int)a.B; p.H = (int)a.H; p.Hkv = (int)a.Hkv; p.r = (int)(a.H / a.Hkv);
     p.window = (int)a.window; p.sinks = a.window ? (int)a.sinks : 0;
-    const int64_t slots = a.M * p.r / kBM + a.B;
-    if (slots * a.Hkv >= (int64_t)1 << 31) return hipErrorInvalidValue;
-    p.slots = (uint32_t)slots;
-    prefill_kernel<<<(unsigned)(slots * a.Hkv), kPrefillThreads, 0, s>>>(p);
+    const Plan plan = prefill_plan(a.M, a.Mk, a.B, a.H, a.Hkv, a.window, a.sinks);
+    if (plan.tiles >= (int64_t)1 << 31) return hipErrorInvalidValue;
+    p.slots = (uint32_t)(plan.tiles / a.Hkv);
+    p.ns = a.workspace ? plan.ns : 1;
+    p.parts = p.ns > 1 ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + kCounterBytes) : nullptr;
+    const dim3 grid((unsigned)plan.tiles, (unsigned)p.ns);
+    if (plan.narrow) prefill_narrow_kernel<<<grid, kPrefillThreads, 0, s>>>(p);
+    else prefill_kernel<<<grid, kPrefillThreads, 0, s>>>(p);
+    if (p.ns > 1) {
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (plan.narrow) prefill_combine_kernel<kRows, kKeys><<<dim3((unsigned)plan.tiles, kRows / 8), kPrefillThreads, 0, s>>>(p);
+        else prefill_combine_kernel<kBM, kBN><<<dim3((unsigned)plan.tiles, kBM / 8), kPrefillThreads, 0, s>>>(p);
+    }
     return hipGetLastError();
 }
 

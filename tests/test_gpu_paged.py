@@ -344,7 +344,8 @@ def test_prefill(H, Hkv, window, sinks):
 
 
 @pytest.mark.parametrize("new,held,H,Hkv,window,sinks", [([700], [0], 4, 4, 0, 0), ([515, 260], [300, 0], 8, 2, 0, 0), ([300], [1500], 4, 1, 256, 4),
-                                                         ([1], [2000], 8, 2, 0, 0), ([3, 1, 2], [1999, 900, 64], 8, 1, 0, 0), ([2], [3500], 4, 4, 1500, 64)])
+                                                         ([1], [2000], 8, 2, 0, 0), ([3, 1, 2], [1999, 900, 64], 8, 1, 0, 0), ([2], [3500], 4, 4, 1500, 64),
+                                                         ([1], [6000], 4, 1, 0, 0), ([40, 1, 0, 9], [100, 5000, 70, 0], 7, 1, 0, 0), ([65], [2000], 2, 1, 900, 130)])
 def test_prefill_longer(new, held, H, Hkv, window, sinks):
     q, k, v, cu_q, cu_k = _prompts(new, held, H, Hkv, 95)
     need = api.attention_prefill_workspace_bytes(len(q), len(k), len(new), H, Hkv, window, sinks)
@@ -355,6 +356,12 @@ def test_prefill_longer(new, held, H, Hkv, window, sinks):
     _check_prefill(shared, q, k, v, cu_q, cu_k, window, sinks, rows=40)
     for _ in range(3):
         assert _same(api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), window=window, sinks=sinks, workspace=ws), shared)
+    assert not ws[:api.GEMM_COUNTER_BYTES].any()
+    if need:                                               # contents behind the counters are irrelevant; a smaller one is refused
+        ws[api.GEMM_COUNTER_BYTES:] = 0xFF
+        assert _same(api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), window=window, sinks=sinks, workspace=ws), shared)
+        with pytest.raises(api.QoqError):
+            api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), window=window, sinks=sinks, workspace=ws[:need - 16])
 
 
 def test_prefill_more_queries_than_tokens_and_rows_of_no_sequence():
@@ -420,6 +427,27 @@ def test_prefill_infinities_and_nan_reach_only_the_queries_that_see_them(window,
             assert np.isnan(got[i]).all()
         else:
             assert np.array_equal(got[i], clean[i])
+
+
+def test_prefill_values_that_are_not_finite_where_workgroups_share_keys():
+    """The rows next to such values are done again by the workgroup that joins the others' sums."""
+    H, Hkv, T = 2, 1, 900
+    q, k, v, cu, _ = _prompts([T], [0], H, Hkv, 109)
+    ws = api.new_workspace(api.attention_prefill_workspace_bytes(T, T, 1, H, Hkv), DEV)
+    assert ws.numel() > api.GEMM_COUNTER_BYTES
+    v2 = v.clone()
+    v2[130, 0, 7], v2[700, 0, 8] = float("inf"), float("nan")
+    got = api.attention_prefill(q, k, v2, _ints(cu), _ints(cu), workspace=ws).cpu().numpy().astype(np.float64)
+    kd, vd, qd = (x.cpu().numpy().astype(np.float64) for x in (k, v, q))
+    ref, spread = paged.attention(qd, kd, vd, np.arange(T))
+    tol, _ = _bound(qd, kd, ref, spread, T)
+    tol = tol + T * 2.0 ** -25 * np.abs(vd).max() + 2.0 ** -25
+    hit = np.zeros(got.shape, dtype=bool)
+    hit[130:, :, 7], hit[700:, :, 8] = True, True
+    assert (np.abs(got - ref) <= tol)[~hit].all() and not np.isfinite(got[hit]).any()
+    assert np.isnan(got[700:, :, 8]).all()
+    assert _same(api.attention_prefill(q, k, v2, _ints(cu), _ints(cu), workspace=ws), got.astype(np.float16))
+    assert not ws[:api.GEMM_COUNTER_BYTES].any()
 
 
 def test_scores_of_any_size():
