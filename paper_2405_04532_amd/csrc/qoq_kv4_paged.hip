@@ -37,10 +37,12 @@ struct AppendArgs {
     int width;
     __half *q_out, *k_out;                       // k_out may be null
     int64_t q_out_stride, k_out_stride;
-    uint32_t kv_items, q_items, q_groups, q_heads;      // waves for keys and values, for queries; groups of q_heads heads per four rows
+    uint32_t kv_items, kv_groups, kv_heads;      // waves for keys and values: groups of kv_heads heads per aligned quad of positions
+    uint32_t q_items, q_groups, q_heads;         // waves for queries: groups of q_heads heads per four rows
 };
 
-// a number as FP16, rounded once: through FP32 unless that could be a midpoint of two FP16 numbers (its last 12 bits are then zero)
+// Numbers as FP16, rounded once: through FP32 unless that could be a midpoint of two FP16 numbers (its last 12 bits are then zero).
+// There the FP32 number is cut off instead and its last bit set where something was: no midpoint, and on the right side of it.
 __device__ __forceinline__ uint4 halves_of(const double (&y)[8])
 {
     float f[8];
@@ -50,172 +52,228 @@ __device__ __forceinline__ uint4 halves_of(const double (&y)[8])
         f[e] = (float)y[e];
         least = min(least, (uint32_t)__float_as_int(f[e]) & 0xFFFu);
     }
+    if (least == 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const double back = f[e];
+            uint32_t bits = __float_as_uint(f[e]);
+            bits -= fabs(back) > fabs(y[e]) ? 1u : 0u;
+            f[e] = __uint_as_float(bits | (back != y[e] ? 1u : 0u));
+        }
+    }
     uint32_t o[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = __builtin_bit_cast(uint32_t, (h2){(_Float16)f[2 * e], (_Float16)f[2 * e + 1]});
-    if (least == 0) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (((uint32_t)__float_as_int(f[e]) & 0xFFFu) == 0 && (__float_as_int(f[e]) & 0x7F800000) != 0x7F800000) {
-                const uint32_t h = double_to_half_rne(y[e]);
-                o[e >> 1] = (e & 1) ? (o[e >> 1] & 0xFFFFu) | (h << 16) : (o[e >> 1] & 0xFFFF0000u) | h;
-            }
-    }
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+template <int CTRL>
+__device__ __forceinline__ uint32_t row_word(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false); }
+template <int CTRL>
+__device__ __forceinline__ double row_double(double v)
+{
+    const uint64_t b = (uint64_t)__double_as_longlong(v);
+    return __longlong_as_double((int64_t)((uint64_t)row_word<CTRL>((uint32_t)(b >> 32)) << 32 | row_word<CTRL>((uint32_t)b)));
+}
 __device__ __forceinline__ double row_sum16(double v)
 {
+    v += row_double<0x128>(v);                                             // rotations by 8, 4, 2, 1 lanes
+    v += row_double<0x124>(v);
+    v += row_double<0x122>(v);
+    return v + row_double<0x121>(v);
+}
+// 1 / sqrt(v), v >= 0, to a few units in the last place: the instruction is good to 2^-23, each step doubles that
+__device__ __forceinline__ double inverse_root(double v)
+{
+    double r = __builtin_amdgcn_rsq(v);
 #pragma unroll
-    for (int o = 8; o; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+    for (int i = 0; i < 2; ++i) r = r * fma(-0.5 * v * r, r, 1.5);
+    return v == 0.0 ? __builtin_inf() : v == __builtin_inf() ? 0.0 : r;
 }
 
-// What the lanes of one token's heads share: the angles' cosines and sines for a lane's elements
+// Angles of a token for a lane's 8 elements, and the weights of a norm.  NEAR: pairs of neighbours, else of halves (i, i + rot / 2).
+// WHOLE: all 128 elements are turned, so a lane's other halves lie 8 lanes further on.
+template <bool NEAR, bool WHOLE>
 struct Turn {
-    float c[8], s[8];                            // 8 pairs (half pairs) or 4 (neighbours: c[0..3], s[0..3])
-    int partner;                                 // lane that holds the other half of the pairs
-    bool turned, first;                          // this lane's elements are rotated; they are the first of their pairs
+    double c[NEAR ? 4 : 8], s[NEAR ? 4 : 8];     // s: with the sign that the lane's elements take it with
+    int partner;
+    bool turned;
+
+    __device__ __forceinline__ void load(const AppendArgs& p, int64_t pos, int lane)
+    {
+        const int w = lane & 15, half = p.rot / 2;
+        turned = WHOLE || 8 * w < p.rot;
+        const bool first = 8 * w < half;
+        partner = NEAR || !turned ? lane : first ? lane + p.rot / 16 : lane - p.rot / 16;
+#pragma unroll
+        for (int e = 0; e < (NEAR ? 4 : 8); ++e) { c[e] = 1.0; s[e] = 0.0; }
+        if (!turned) return;
+        const int64_t row = pos < 0 ? 0 : pos < p.angle_rows ? pos : p.angle_rows - 1;
+        const float* at = p.angles + row * p.rot + (NEAR ? 4 * w : first ? 8 * w : 8 * w - half);
+        const float sign = NEAR || !first ? 1.f : -1.f;
+#pragma unroll
+        for (int e = 0; e < (NEAR ? 1 : 2); ++e) {
+            const float4 cc = reinterpret_cast<const float4*>(at)[e], ss = reinterpret_cast<const float4*>(at + half)[e];
+            c[4 * e] = cc.x; c[4 * e + 1] = cc.y; c[4 * e + 2] = cc.z; c[4 * e + 3] = cc.w;
+            s[4 * e] = ss.x * sign; s[4 * e + 1] = ss.y * sign; s[4 * e + 2] = ss.z * sign; s[4 * e + 3] = ss.w * sign;
+        }
+    }
+
+    // one head of a token; every lane of the row takes part.  g, gp: the norm's weights of the lane's and of its partner's elements
+    __device__ __forceinline__ uint4 head(const uint4& raw, bool norm, const uint4& g, const uint4& gp, const AppendArgs& p) const
+    {
+        if (!norm && p.rot == 0) return raw;
+        const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w}, gw[4] = {g.x, g.y, g.z, g.w};
+        auto element = [](const uint32_t (&v)[4], int e) { return (float)half_of(v[e >> 1] >> (16 * (e & 1))); };
+        float x[8];                                                        // x gamma, exact
+        double r = 1.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = element(rw, e);
+        if (norm) {
+            double sum = 0.0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fma((double)x[e], (double)x[e], sum);
+            r = inverse_root(fma(row_sum16(sum), 1.0 / kD, p.eps));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= element(gw, e);
+        }
+        double y[8];
+        if constexpr (NEAR) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const double a = x[2 * e], b = x[2 * e + 1];
+                y[2 * e] = fma(a, c[e], -(b * s[e]));
+                y[2 * e + 1] = fma(b, c[e], a * s[e]);
+            }
+        } else {
+            uint32_t pw[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pw[e] = WHOLE ? row_word<0x128>(rw[e]) : (uint32_t)__shfl((int)rw[e], partner, 64);
+            const uint32_t gq[4] = {gp.x, gp.y, gp.z, gp.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float o = element(pw, e);
+                if (norm) o *= element(gq, e);
+                y[e] = fma((double)x[e], c[e], (double)o * s[e]);
+            }
+        }
+        if (norm)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] *= r;
+        const uint4 out = halves_of(y);
+        if (!WHOLE && !norm && !turned) return raw;                        // (its bits, whatever they are)
+        return out;
+    }
+    __device__ __forceinline__ void gammas(const __half* gamma, int lane, uint4& g, uint4& gp) const
+    {
+        g = gp = make_uint4(0, 0, 0, 0);
+        if (!gamma) return;
+        g = reinterpret_cast<const uint4*>(gamma)[lane & 15];
+        gp = reinterpret_cast<const uint4*>(gamma)[partner & 15];
+    }
 };
 
-__device__ __forceinline__ void load_turn(Turn& t, const AppendArgs& p, int64_t pos, int lane)
-{
-    const int w = lane & 15, half = p.rot / 2;
-    t.turned = 8 * w < p.rot;
-    t.first = 8 * w < half;
-    t.partner = lane;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) { t.c[e] = 1.f; t.s[e] = 0.f; }
-    if (!t.turned) return;
-    const int64_t row = pos < 0 ? 0 : pos < p.angle_rows ? pos : p.angle_rows - 1;
-    const float* at = p.angles + row * p.rot;
-    if (p.interleaved) {
-        const float4 c = reinterpret_cast<const float4*>(at)[w], s = reinterpret_cast<const float4*>(at + half)[w];
-        t.c[0] = c.x; t.c[1] = c.y; t.c[2] = c.z; t.c[3] = c.w;
-        t.s[0] = s.x; t.s[1] = s.y; t.s[2] = s.z; t.s[3] = s.w;
-    } else {
-        t.partner = t.first ? lane + p.rot / 16 : lane - p.rot / 16;
-        const int i = t.first ? 8 * w : 8 * w - half;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const float4 c = reinterpret_cast<const float4*>(at + i)[e], s = reinterpret_cast<const float4*>(at + half + i)[e];
-            t.c[4 * e] = c.x; t.c[4 * e + 1] = c.y; t.c[4 * e + 2] = c.z; t.c[4 * e + 3] = c.w;
-            t.s[4 * e] = s.x; t.s[4 * e + 1] = s.y; t.s[4 * e + 2] = s.z; t.s[4 * e + 3] = s.w;
-        }
-    }
-}
-
-// one head of a token: every lane of the row takes part
-__device__ __forceinline__ uint4 turn_head(const uint4& raw, const Turn& t, const __half* gamma, const AppendArgs& p, int lane)
-{
-    if (!gamma && p.rot == 0) return raw;
-    const int w = lane & 15;
-    const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
-    float x[8];                                                            // x gamma
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)half_of(rw[e >> 1] >> (16 * (e & 1)));
-    double r = 1.0;
-    if (gamma) {
-        double sum = 0.0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fma((double)x[e], (double)x[e], sum);
-        r = 1.0 / sqrt(row_sum16(sum) * (1.0 / kD) + p.eps);
-        const uint4 g4 = reinterpret_cast<const uint4*>(gamma)[w];
-        const uint32_t g[4] = {g4.x, g4.y, g4.z, g4.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= (float)half_of(g[e >> 1] >> (16 * (e & 1)));
-    }
-    double y[8];
-    if (p.interleaved) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const double a = x[2 * e], b = x[2 * e + 1], c = t.c[e], s = t.s[e];
-            y[2 * e] = fma(a, c, -(b * s));
-            y[2 * e + 1] = fma(b, c, a * s);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const double other = (double)__shfl(x[e], t.partner, 64) * (double)t.s[e];
-            y[e] = fma((double)x[e], (double)t.c[e], t.first ? -other : other);
-        }
-    }
-    if (gamma)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= r;
-    if (!gamma && !t.turned) return raw;                                   // (its bits, whatever they are)
-    return halves_of(y);
-}
-
+template <bool NEAR, bool WHOLE>
 __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs p)
 {
     __shared__ uint4 s_block[4][16];                                       // per wave: the value codes of its quad
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, w = lane & 15;
     uint32_t item = blockIdx.x * 4 + (uint32_t)wave;
-    Turn turn;
+    Window window;
+    Turn<NEAR, WHOLE> turn;
+    uint4 gamma, gamma_partner;
     if (item < p.kv_items) {
-        // keys and values: an aligned quad of token positions of one sequence, one KV head
-        const uint32_t slot = item / (uint32_t)p.Hkv;
-        const int h = (int)(item - slot * (uint32_t)p.Hkv);
-        const int b = count_before(p.B, lane, [&](int i) { return (uint32_t)(p.cu[i] >> 2) + 2u * (uint32_t)i <= slot; });
-        if (b >= p.B) return;
-        const int64_t row0 = p.cu[b], T = (int64_t)p.cu[b + 1] - row0, p0 = p.starts ? p.starts[b] : 0;
+        // keys and values: an aligned quad of token positions of one sequence, a group of KV heads
+        const uint32_t slot = item / p.kv_groups, group = item - slot * p.kv_groups;
+        auto before = [&](int end, int i) { return (uint32_t)(end >> 2) + 2u * (uint32_t)i <= slot; };
+        window.load(p.cu, p.starts, p.B, near_before(p.B, lane, [&](int i) { return before(p.cu[i], i); }), lane);
+        const int c = __popcll(__builtin_amdgcn_ballot_w64(lane < window.held && before(window.end, window.lo + lane + 1)));
+        if (c >= window.held) return;
+        const int b = window.lo + c;
+        const int64_t row0 = window.first_row(b, false), T = (int64_t)window.end_row(b) - row0, p0 = window.start_of(b, false);
         const int64_t j = (int64_t)slot - ((row0 >> 2) + 2 * (int64_t)b);
         const int64_t pos = ((p0 >> 2) + j) * 4 + g, t = pos - p0, row = row0 + t;
         const bool there = t >= 0 && t < T && row >= 0 && row < p.M;       // a token of the call
         if (__builtin_amdgcn_ballot_w64(there) == 0) return;
         const bool held = there && pos >= 0 && pos < (int64_t)p.width * kPageTokens;
         const uint32_t id = held ? (uint32_t)p.table[(int64_t)b * p.width + pos / kPageTokens] : ~0u;
+        const int64_t at = there ? row : 0;
+        const uint4* k_src = reinterpret_cast<const uint4*>(p.k + at * p.k_stride) + w;
+        const uint4* v_src = reinterpret_cast<const uint4*>(p.v + at * p.v_stride) + w;
+        const int h0 = (int)(group * p.kv_heads), h1 = min(h0 + (int)p.kv_heads, p.Hkv);
+        uint4 next_k[2], next_v[2];                                        // two heads on their way
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            next_k[x] = k_src[min(h0 + x, h1 - 1) * (kD / 8)];
+            next_v[x] = v_src[min(h0 + x, h1 - 1) * (kD / 8)];
+        }
+        turn.load(p, pos, lane);
+        turn.gammas(p.k_gamma, lane, gamma, gamma_partner);
         const bool valid = held && id < p.pages;
-        const int64_t at = there ? row : row0 > 0 && row0 < p.M ? row0 : 0;
-        const uint4 rk = reinterpret_cast<const uint4*>(p.k + at * p.k_stride + h * kD)[w];
-        const uint4 rv = reinterpret_cast<const uint4*>(p.v + at * p.v_stride + h * kD)[w];
-        load_turn(turn, p, pos, lane);
-        const uint4 k = turn_head(rk, turn, p.k_gamma, p, lane);
-        if (p.k_out && there) reinterpret_cast<uint4*>(p.k_out + row * p.k_out_stride + h * kD)[w] = k;
         const uint64_t written = __builtin_amdgcn_ballot_w64(valid);
-        if (written == 0) return;
-        uint8_t* page = p.pool + ((int64_t)(valid ? id : 0) * p.Hkv + h) * kPageBytes;
+        uint8_t* page = p.pool + (int64_t)(valid ? id : 0) * p.Hkv * kPageBytes;
         const int tin = (int)(pos & (kPageTokens - 1));
-        write_token<false>(k, page, tin, w, lane, written == ~0ull, valid, s_block[wave]);
-        write_token<true>(rv, page, tin, w, lane, written == ~0ull, valid, s_block[wave]);
+        for (int h = h0; h < h1; h += 2) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint4 rk = next_k[x], rv = next_v[x];
+                const int ahead = min(h + x + 2, h1 - 1) * (kD / 8);
+                next_k[x] = k_src[ahead];
+                next_v[x] = v_src[ahead];
+                if (h + x >= h1) break;
+                const uint4 k = turn.head(rk, p.k_gamma != nullptr, gamma, gamma_partner, p);
+                if (p.k_out && there) reinterpret_cast<uint4*>(p.k_out + row * p.k_out_stride + (h + x) * kD)[w] = k;
+                if (written == 0) continue;
+                uint8_t* at_page = page + (int64_t)(h + x) * kPageBytes;
+                write_token<false>(k, at_page, tin, w, lane, written == ~0ull, valid, s_block[wave]);
+                write_token<true>(rv, at_page, tin, w, lane, written == ~0ull, valid, s_block[wave]);
+            }
+        }
         return;
     }
     // queries: four rows, a group of heads
     item -= p.kv_items;
     if (item >= p.q_items) return;
     const uint32_t quad = item / p.q_groups, group = item - quad * p.q_groups;
+    window.load(p.cu, p.starts, p.B, near_before(p.B, lane, [&](int x) { return p.cu[x] <= (int)(4 * quad); }), lane);
     int b = 0;
-    if (p.B <= 64) {
-        const int end = lane < p.B ? p.cu[lane + 1] : INT32_MAX;
+    bool far = false;                                                      // so many empty sequences that a row lies past the window
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = __popcll(__builtin_amdgcn_ballot_w64(end <= (int)(4 * quad + i)));
-            b = g == i ? c : b;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = count_before(p.B, lane, [&](int x) { return p.cu[x] <= (int)(4 * quad + i); });
-            b = g == i ? c : b;
-        }
+    for (int i = 0; i < 4; ++i) {
+        const int c = __popcll(__builtin_amdgcn_ballot_w64(lane < window.held && window.end <= (int)(4 * quad) + i));
+        far |= c == 64;
+        b = g == i ? window.lo + c : b;
     }
+    if (far)
+        for (int i = 0; i < 4; ++i) {
+            const int c = count_before(p.B, lane, [&](int x) { return p.cu[x] <= (int)(4 * quad) + i; });
+            b = g == i ? c : b;
+        }
     const int64_t row = 4 * (int64_t)quad + g;
-    const int64_t row0 = b < p.B ? p.cu[b] : 0;
+    const int b_in = min(b, p.B - 1);
+    const int64_t row0 = window.first_row(b_in, far);
     const bool there = b < p.B && row >= row0 && row < p.M;
-    const int64_t pos = (there && p.starts ? p.starts[b] : 0) + row - row0;
-    load_turn(turn, p, there ? pos : 0, lane);
+    const int64_t pos = window.start_of(b_in, far) + row - row0;
     const int64_t at = there ? row : 0;
     const int h0 = (int)(group * p.q_heads), h1 = min(h0 + (int)p.q_heads, p.H);
     const uint4* src = reinterpret_cast<const uint4*>(p.q + at * p.q_stride) + w;
     uint4* dst = reinterpret_cast<uint4*>(p.q_out + at * p.q_out_stride) + w;
-    uint4 next = src[h0 * (kD / 8)];
-    for (int h = h0; h < h1; ++h) {
-        const uint4 raw = next;
-        next = src[min(h + 1, h1 - 1) * (kD / 8)];
-        const uint4 y = turn_head(raw, turn, p.q_gamma, p, lane);
-        if (there) dst[h * (kD / 8)] = y;
+    constexpr int kAhead = 4;                                              // heads on their way
+    uint4 next[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) next[x] = src[min(h0 + x, h1 - 1) * (kD / 8)];
+    turn.load(p, there ? pos : 0, lane);
+    turn.gammas(p.q_gamma, lane, gamma, gamma_partner);
+    for (int h = h0; h < h1; h += kAhead) {
+#pragma unroll
+        for (int x = 0; x < kAhead; ++x) {
+            const uint4 raw = next[x];
+            next[x] = src[min(h + x + kAhead, h1 - 1) * (kD / 8)];
+            if (h + x >= h1) break;
+            const uint4 y = turn.head(raw, p.q_gamma != nullptr, gamma, gamma_partner, p);
+            if (there) dst[(h + x) * (kD / 8)] = y;
+        }
     }
 }
 
@@ -241,9 +299,13 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(const uint8_t* __rest
     if (item >= items) return;
     const uint32_t slot = item / (uint32_t)Hkv;
     const int h = (int)(item - slot * (uint32_t)Hkv);
-    const int b = count_before(B, lane, [&](int i) { return (uint32_t)(cu[i] >> 4) + 2u * (uint32_t)i <= slot; });
-    if (b >= B) return;
-    const int64_t row0 = cu[b], T = (int64_t)cu[b + 1] - row0, p0 = starts ? starts[b] : 0;
+    auto before = [&](int end, int i) { return (uint32_t)(end >> 4) + 2u * (uint32_t)i <= slot; };
+    Window window;
+    window.load(cu, starts, B, near_before(B, lane, [&](int i) { return before(cu[i], i); }), lane);
+    const int c = __popcll(__builtin_amdgcn_ballot_w64(lane < window.held && before(window.end, window.lo + lane + 1)));
+    if (c >= window.held) return;
+    const int b = window.lo + c;
+    const int64_t row0 = window.first_row(b, false), T = (int64_t)window.end_row(b) - row0, p0 = window.start_of(b, false);
     const int64_t j = (int64_t)slot - ((row0 >> 4) + 2 * (int64_t)b);
     const int64_t pos0 = ((p0 >> 4) + j) * 16;                             // floor(p0 / 16) also for negative p0
     if (pos0 >= p0 + T || pos0 + 16 <= p0) return;
@@ -705,6 +767,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
 
 int64_t kv4_page_bytes(int64_t Hkv) { return Hkv * kPageBytes; }
 
+constexpr int64_t kFill = 4096;
 hipError_t launch_rope_append(const RopeAppend& a, hipStream_t s)
 {
     AppendArgs p{};
@@ -720,13 +783,22 @@ hipError_t launch_rope_append(const RopeAppend& a, hipStream_t s)
     p.q_out_stride = a.q_out_stride; p.k_out_stride = a.k_out_stride;
     const int64_t slots = a.M / 4 + 2 * a.B;             // a sequence of T tokens touches at most (T + 2) / 4 + 1 aligned quads
     const int64_t quads = (a.M + 3) / 4;
-    p.q_heads = 1;
-    while (p.q_heads < 8 && quads * a.H / (2 * p.q_heads) >= 4096) p.q_heads *= 2;
+    // heads to a wave: as many as leave kFill waves, since they share the look-up of the rows and the angles
+    auto heads_to_a_wave = [](int64_t rows, int64_t heads) {
+        uint32_t n = 1;
+        while (n < 8 && rows * heads / (2 * n) >= kFill) n *= 2;
+        return n;
+    };
+    p.q_heads = heads_to_a_wave(quads, a.H);
     p.q_groups = (uint32_t)((a.H + p.q_heads - 1) / p.q_heads);
-    const int64_t kv_items = slots * a.Hkv, q_items = p.q ? quads * p.q_groups : 0;
+    p.kv_heads = heads_to_a_wave(quads, a.Hkv);
+    p.kv_groups = (uint32_t)((a.Hkv + p.kv_heads - 1) / p.kv_heads);
+    const int64_t kv_items = slots * p.kv_groups, q_items = p.q ? quads * p.q_groups : 0;
     if (kv_items + q_items >= (int64_t)1 << 31) return hipErrorInvalidValue;
     p.kv_items = (uint32_t)kv_items; p.q_items = (uint32_t)q_items;
-    rope_append_kernel<<<(unsigned)((kv_items + q_items + 3) / 4), 256, 0, s>>>(p);
+    auto* kernel = a.rot == kD ? (a.interleaved ? rope_append_kernel<true, true> : rope_append_kernel<false, true>)
+                               : (a.interleaved ? rope_append_kernel<true, false> : rope_append_kernel<false, false>);
+    kernel<<<(unsigned)((kv_items + q_items + 3) / 4), 256, 0, s>>>(p);
     return hipGetLastError();
 }
 

@@ -10,18 +10,55 @@
 namespace qoq {
 
 // Number of b in 1 .. B for which before(b) holds, a condition that is true up to some b and false from there on: a search by the
-// 64 lanes of a wave, one round of loads for up to 64 sequences, two up to 4096.  The result lies in 0 .. B whatever before() says.
+// 64 lanes of a wave, no round of loads for up to 64 sequences, one up to 4096, until the number lies in lo .. lo + 63, the result.  It
+// lies in 0 .. B whatever before() says.
 template <class F>
-__device__ __forceinline__ int count_before(int B, int lane, F&& before)
+__device__ __forceinline__ int near_before(int B, int lane, F&& before)
 {
-    int lo = 0, n = B;                                       // the result lies in lo .. lo + n
+    int lo = 0, n = B;                                       // the number lies in lo .. lo + n
     while (n > 64) {
         const int step = (n + 63) / 64, at = lo + (lane + 1) * step;
         const int c = __popcll(__builtin_amdgcn_ballot_w64(at <= lo + n && before(at)));
         n = min(step - 1, n - c * step);
         lo += c * step;
     }
-    return lo + __popcll(__builtin_amdgcn_ballot_w64(lane < n && before(lo + lane + 1)));
+    return lo;
 }
+template <class F>
+__device__ __forceinline__ int count_before(int B, int lane, F&& before)
+{
+    const int lo = near_before(B, lane, before);
+    return lo + __popcll(__builtin_amdgcn_ballot_w64(lane < B - lo && before(lo + lane + 1)));
+}
+
+// 64 sequences from `lo` on, one to a lane, in flight at once: where their rows end and where those are placed.
+struct Window {
+    const int32_t *cu, *starts;
+    int lo, held, end, start, begin;                         // end past the last sequence: above every row
+
+    __device__ __forceinline__ void load(const int32_t* cu_, const int32_t* starts_, int B, int lo_, int lane)
+    {
+        cu = cu_;
+        starts = starts_;
+        lo = lo_;
+        held = min(B - lo, 64);
+        end = lane < held ? cu[lo + lane + 1] : INT32_MAX;
+        start = lane < held && starts ? starts[lo + lane] : 0;
+        begin = cu[lo];
+    }
+    // by every lane of the wave (a lane that is off gives no other its numbers); b: inside the window, or anywhere up to B - 1 with `far`
+    __device__ __forceinline__ int first_row(int b, bool far) const
+    {
+        if (far) return cu[b];
+        const int before = __shfl(end, max(b - lo - 1, 0), 64);
+        return b > lo ? before : begin;
+    }
+    __device__ __forceinline__ int end_row(int b) const { return __shfl(end, b - lo, 64); }
+    __device__ __forceinline__ int start_of(int b, bool far) const
+    {
+        if (far) return starts ? starts[b] : 0;
+        return __shfl(start, b - lo, 64);
+    }
+};
 
 }  // namespace qoq

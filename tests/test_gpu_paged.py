@@ -173,6 +173,35 @@ def test_append_rounds_once():
         with np.errstate(invalid="ignore"):
             want = paged.turn_heads(x.numpy(), None, 0, angles.numpy(), np.arange(M), near)
         assert _same(qo, want)
+        # the same behind a norm; heads of zeros without an eps are 0 / 0
+        x[4] = 0
+        gamma = (1 + torch.randn(D, generator=g)).half()
+        for eps in (0.0, 1e-5, 3e4):
+            qo, _ = api.qk_rope_kv4_append(x.to(DEV), kv, kv, pool, table, _ints([0, M]), None, angles.to(DEV), q_gamma=gamma.to(DEV), eps=eps, interleaved=near)
+            with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
+                want = paged.turn_heads(x.numpy(), gamma.numpy(), eps, angles.numpy(), np.arange(M), near)
+            # bit for bit, but that in a head with an infinity 1 / sqrt is 0: the products are zeros whose sign goes by their order
+            endless = np.isinf(x.numpy().astype(np.float32)).any(axis=-1)
+            assert _same(qo.cpu().numpy()[~endless], want[~endless]) and np.array_equal(qo.cpu().numpy()[endless], want[endless], equal_nan=True)
+
+
+@pytest.mark.parametrize("B", [1, 63, 64, 65, 130, 5000])
+def test_append_and_gather_of_many_sequences(B):
+    """Up to 64 sequences are looked up by the lanes of a wave, more by a search; empty ones among them, the same token count at both ends."""
+    new = [(3 * b) % 4 for b in range(B - 1)] + [2]
+    starts = [(17 * b) % 70 for b in range(B)]
+    cu = np.concatenate(([0], np.cumsum(new)))
+    M = int(cu[-1])
+    table, pages = _tables([128] * B, 2, 9)
+    q, k, v = _heads(M, 2, 61), _heads(M, 1, 62), _heads(M, 1, 63, 4)
+    angles = api.rope_angles(80, device=DEV)
+    pool = api.kv4_new_pool(pages, 1, DEV)
+    qo, ko = api.qk_rope_kv4_append(q, k, v, pool, table, _ints(cu), _ints(starts), angles, want_k=True)
+    seq, pos = paged.rows_of(cu, starts, M)
+    want_k = paged.turn_heads(k.cpu().numpy(), None, 0, angles.cpu().numpy(), pos, False)
+    assert _same(qo, paged.turn_heads(q.cpu().numpy(), None, 0, angles.cpu().numpy(), pos, False)) and _same(ko, want_k)
+    gk, gv = api.kv4_paged_gather(pool, table, _ints(cu), _ints(starts), M, 1)
+    assert _same(gk, paged.quantized(want_k).astype(np.float16)) and _same(gv, paged.quantized(v.cpu().numpy()).astype(np.float16))
 
 
 # ------------------------------------------------------------------------------------------------------------------
