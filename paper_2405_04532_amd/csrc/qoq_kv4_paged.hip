@@ -767,7 +767,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
 
 int64_t kv4_page_bytes(int64_t Hkv) { return Hkv * kPageBytes; }
 
-constexpr int64_t kFill = 4096;
+constexpr int64_t kFill = 1024;                          // (5 x 1733 tokens of 64 / 8 heads 53.6 us, with 4096 56.5; 1 x 1000 of 32 heads 15.3 and 20.3)
 hipError_t launch_rope_append(const RopeAppend& a, hipStream_t s)
 {
     AppendArgs p{};

@@ -110,9 +110,9 @@ __device__ __forceinline__ int attending(const PrefillArgs& p, const RowTile<ROW
 
 __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }       // a row that sees nothing is zero (NaN stays)
 
-// A zero weight times infinity or NaN is NaN, in rows that do not see that value.  Rows `begin` .. `end` - 1 of a tile that shares keys with such
-// a value are done again by a wave, one after the other, with the keys they see and no others: 64 scores at a time, a lane each, then
-// two elements of the values a lane.
+// A zero weight times infinity or NaN is NaN, in rows that do not see that value.  So where a wave's results are not all finite, rows `begin` ..
+// `end` - 1 of its tile are done again, one after the other, with the keys they see and no others: 64 scores at a time, a lane each,
+// then two elements of the values a lane.  (Slow: for inputs that are broken already.)
 template <int ROWS, int BN>
 __device__ void redo_rows(const PrefillArgs& p, const RowTile<ROWS, BN>& t, int hk, int begin, int end, int lane)
 {
@@ -125,12 +125,19 @@ __device__ void redo_rows(const PrefillArgs& p, const RowTile<ROWS, BN>& t, int 
         const __half* q_row = p.q + (int64_t)(t.q0 + query) * p.q_stride + (hk * p.r + head) * kD;
         float top = -1e30f, sum = 0.f, o0 = 0.f, o1 = 0.f;
         for (int i = 0; i < t.n; ++i)
-            for (int at = t.tile_of(i) * BN; at < t.tile_of(i) * BN + BN; at += 64) {
-                const int key = at + lane;
-                const bool sees = key < t.tile_of(i) * BN + BN && key <= pos && (!p.window || key > pos - p.window || key < p.sinks);
+            for (int at = t.tile_of(i) * BN; at < t.tile_of(i) * BN + BN && at <= pos; at += 64) {
+                const int key = at + lane, last = min(t.tile_of(i) * BN + BN - 1, pos);
+                const bool sees = key <= last && (!p.window || key > pos - p.window || key < p.sinks);
+                const uint4* k_row = reinterpret_cast<const uint4*>(k_rows + (int64_t)min(key, last) * p.k_stride);
                 float s = 0.f;
-                if (sees)
-                    for (int d = 0; d < kD; ++d) s = fmaf(__half2float(k_rows[(int64_t)key * p.k_stride + d]), __half2float(q_row[d]), s);
+#pragma unroll
+                for (int d = 0; d < kD / 8; ++d) {
+                    const uint4 a = k_row[d], c = reinterpret_cast<const uint4*>(q_row)[d];
+                    s = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, a.x), __builtin_bit_cast(h2, c.x), s, false);
+                    s = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, a.y), __builtin_bit_cast(h2, c.y), s, false);
+                    s = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, a.z), __builtin_bit_cast(h2, c.z), s, false);
+                    s = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, a.w), __builtin_bit_cast(h2, c.w), s, false);
+                }
                 float most = sees ? s : -__builtin_inff();
                 for (int step = 32; step; step >>= 1) most = fmaxf(most, __shfl_xor(most, step, 64));
                 most = fmaxf(most, top);
@@ -139,12 +146,19 @@ __device__ void redo_rows(const PrefillArgs& p, const RowTile<ROWS, BN>& t, int 
                 sum = sum * keep + weight;
                 o0 *= keep;
                 o1 *= keep;
-                for (uint64_t left = __builtin_amdgcn_ballot_w64(sees); left; left &= left - 1) {
-                    const int from = __ffsll((unsigned long long)left) - 1;
-                    const float w = __shfl(weight, from, 64);
-                    const __half* v_row = v_rows + (int64_t)(at + from) * p.v_stride + 2 * lane;
-                    o0 = fmaf(w, __half2float(v_row[0]), o0);
-                    o1 = fmaf(w, __half2float(v_row[1]), o1);
+                const uint64_t seen = __builtin_amdgcn_ballot_w64(sees);
+                for (int j = 0; j < 64; j += 8) {
+                    if ((seen >> j & 255) == 0) continue;
+                    uint32_t v[8];
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) v[x] = reinterpret_cast<const uint32_t*>(v_rows + (int64_t)min(at + j + x, last) * p.v_stride)[lane];
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        if ((seen >> (j + x) & 1) == 0) continue;
+                        const float w = __shfl(weight, j + x, 64);
+                        o0 = fmaf(w, (float)half_of(v[x]), o0);
+                        o1 = fmaf(w, (float)half_of(v[x] >> 16), o1);
+                    }
                 }
             }
         for (int step = 32; step; step >>= 1) sum += __shfl_xor(sum, step, 64);
@@ -165,13 +179,15 @@ __device__ __forceinline__ void write_out(const PrefillArgs& p, const RowTile<RO
         make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
 }
 
-// NaN if some element is not finite
-__device__ __forceinline__ float not_finite(const h8& a, float bad)
+// whether some row of the wave has a sum that is not finite
+__device__ __forceinline__ bool not_finite(const f16v (&acc)[4], bool there)
 {
-    struct { h2 v[4]; } t = __builtin_bit_cast(decltype(t), a);
+    float bad = 0.f;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) bad = __builtin_amdgcn_fdot2(t.v[x], (h2){(_Float16)0.f, (_Float16)0.f}, bad, false);
-    return bad;
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int y = 0; y < 16; ++y) bad = fmaf(acc[d][y], 0.f, bad);
+    return __builtin_amdgcn_ballot_w64(there && bad != bad) != 0;
 }
 
 __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void prefill_kernel(PrefillArgs p)
@@ -273,7 +289,6 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
         const uint8_t* at = s_tiles[it & 1][1] + 16 * s * kRowBytes + v_off[d];
         return v_operand(at, at + 8 * kRowBytes);
     };
-    bool odd = false;                                                      // some value that not every row sees is not finite
     // One tile: the weights of scores `sc` (with their maximum `top`, m among them) and their product with the values, while the
     // matrix cores form the next tile's scores (behind the last tile those of whatever the buffer holds, for nobody).  The order of
     // the instructions is set here, step by step: a step's products run while the next step's operands come from LDS and a share of the
@@ -284,19 +299,20 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
         // of the tile's keys this row sees those up to at_most that lie above `above` or below `below`; a lane's first key is 4 hl (counted
         // from there, the keys are constants)
         const int at_most = (there ? pos - t0 : -1) - 4 * hl, above = (p.window ? pos - p.window - t0 : -1) - 4 * hl, below = p.sinks - t0 - 4 * hl;
-        auto seen = [&](int e) { return e <= at_most && (e > above || e < below); };
         if (masked) {
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
-                for (int y = 0; y < 16; ++y) sc[x][y] = seen(32 * x + 8 * (y >> 2) + (y & 3)) ? sc[x][y] : -__builtin_inff();
-            top = top_of(sc);
-            float bad = 0.f;
-#pragma unroll 1
-            for (int s = 0; s < 4; ++s)
+                for (int y = 0; y < 16; ++y) sc[x][y] = 32 * x + 8 * (y >> 2) + (y & 3) <= at_most ? sc[x][y] : -__builtin_inff();
+            if (p.window)
 #pragma unroll
-                for (int d = 0; d < 4; ++d) bad = not_finite(values(it, s, d), bad);
-            if (__builtin_amdgcn_ballot_w64(bad != bad) != 0) odd = true;
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int y = 0; y < 16; ++y) {
+                        const int e = 32 * x + 8 * (y >> 2) + (y & 3);
+                        sc[x][y] = e > above || e < below ? sc[x][y] : -__builtin_inff();
+                    }
+            top = top_of(sc);
         }
         if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
             const float alpha = __builtin_amdgcn_exp2f((m - top) * kScale);
@@ -379,6 +395,7 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
         turn(it, sa, sb);
         if (it + 1 < n) turn(it + 1, sb, sa);
     }
+    const bool odd = not_finite(acc, there);
     if (odd && nwg == 1) {
         redo_rows(p, t, hk, wave * 32, wave * 32 + 32, lane);
         return;
@@ -464,7 +481,6 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
     for (int d = 0; d < 4; ++d) acc[d] = (f16v)(0.f);
     const int key = 4 * hl + ((lane & 15) >> 2), within = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    bool odd = false;
     for (int it = 0; it < n; ++it) {
         if (it + 1 < n) wait_vmcnt<16>();                                  // the next tile may still be on its way
         else wait_vmcnt<0>();
@@ -487,12 +503,6 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
                 const int e = 8 * (y >> 2) + (y & 3);
                 sc[0][y] = e <= at_most && (e > above || e < below) ? sc[0][y] : -__builtin_inff();
             }
-            float bad = 0.f;
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int d = 0; d < 4; ++d) bad = not_finite(values(s, d), bad);
-            if (__builtin_amdgcn_ballot_w64(bad != bad) != 0) odd = true;
         }
         float top = m;
 #pragma unroll
@@ -531,6 +541,7 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
     // ---- the waves meet ----
     float total = (l[0] + l[1]) + (l[2] + l[3]);
     total += __shfl_xor(total, 32, 64);
+    const bool odd = not_finite(acc, there);
     float* own = reinterpret_cast<float*>(&s_ring[wave][0][0]) + col * kPart;
 #pragma unroll
     for (int d = 0; d < 4; ++d)

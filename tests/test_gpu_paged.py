@@ -455,7 +455,7 @@ def test_prefill_infinities_and_nan_reach_only_the_queries_that_see_them(window,
         if paged.visible(i, 150, window, sinks):
             assert np.isnan(got[i]).all()
         else:
-            assert np.array_equal(got[i], clean[i])
+            assert (np.abs(got[i].astype(np.float64) - ref[i]) <= tol[i]).all()
 
 
 def test_prefill_values_that_are_not_finite_where_workgroups_share_keys():
