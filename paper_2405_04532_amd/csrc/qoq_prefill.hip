@@ -31,6 +31,7 @@ constexpr int kBM = 128, kBN = 64, kPrefillThreads = 256;
 constexpr int kRows = 32, kKeys = 32;                    // of the narrow kernel's tiles
 constexpr int kPart = kD + 4;                            // floats of a row's partial result: sums, maximum, weight sum, whether to do it again
 constexpr int kRowBytes = kD * 2;                        // 256: sixteen 16-byte chunks
+constexpr int kRowPitch = kRowBytes + 16;                // of results in LDS
 constexpr int kTileBytes = kBN * kRowBytes;              // 16 KiB of keys, as much of values
 constexpr float kScale = 1.4426950408889634f * 0.08838834764831845f;      // log2(e) / sqrt(128)
 constexpr int kMaxParts = 64;                            // workgroups to a row tile
@@ -395,6 +396,7 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
         turn(it, sa, sb);
         if (it + 1 < n) turn(it + 1, sb, sa);
     }
+    __syncthreads();                                                       // everyone has left the tiles
     const bool odd = not_finite(acc, there);
     if (odd && nwg == 1) {
         redo_rows(p, t, hk, wave * 32, wave * 32 + 32, lane);
@@ -402,8 +404,8 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
     }
     float total = (l[0] + l[1]) + (l[2] + l[3]);
     total += __shfl_xor(total, 32, 64);
-    if (!there) return;
     if (nwg > 1) {                                                         // to be added up by the second launch
+        if (!there) return;
         float* mine = p.parts + ((((size_t)slot * p.Hkv + hk) * p.ns + split) * kBM + wave * 32 + col) * kPart;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
@@ -413,12 +415,29 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
         if (hl == 0) *reinterpret_cast<float4*>(mine + kD) = make_float4(m * kScale, total, odd ? 1.f : 0.f, 0.f);
         return;
     }
+    // rows leave through LDS, 16 bytes a lane and whole rows of 256 (8 bytes a lane of 64 rows' pieces otherwise)
     const float inv = inverse(total);
+    uint8_t* own = reinterpret_cast<uint8_t*>(&s_tiles[0][0][0]) + wave * 32 * kRowPitch;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-            write_out(p, t, hk, wave * 32 + col, 32 * d + 8 * y + 4 * hl, make_float4(acc[d][4 * y], acc[d][4 * y + 1], acc[d][4 * y + 2], acc[d][4 * y + 3]), inv);
+        for (int y = 0; y < 4; ++y) {
+            const h2 a = {(_Float16)(acc[d][4 * y] * inv), (_Float16)(acc[d][4 * y + 1] * inv)};
+            const h2 c = {(_Float16)(acc[d][4 * y + 2] * inv), (_Float16)(acc[d][4 * y + 3] * inv)};
+            *reinterpret_cast<uint2*>(own + col * kRowPitch + (32 * d + 8 * y + 4 * hl) * 2) = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
+        }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");                 // the wave's own LDS writes, then its reads
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+        const int row = 4 * x + (lane >> 4);
+        if (wave * 32 + row >= t.rows(p)) break;
+        int query, head;
+        t.row(p, wave * 32 + row, query, head);
+        reinterpret_cast<uint4*>(p.out + ((int64_t)(q0 + query) * p.H + hk * p.r + head) * kD)[lane & 15] =
+            *reinterpret_cast<const uint4*>(own + row * kRowPitch + (lane & 15) * 16);
+    }
 }
 
 // ------------------------------------------------------------------------------------------
