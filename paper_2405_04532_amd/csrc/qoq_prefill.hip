@@ -73,14 +73,20 @@ struct RowTile {
 
     __device__ __forceinline__ bool find(const PrefillArgs& p, uint32_t slot, int lane)
     {
-        const int b = count_before(p.B, lane, [&](int i) { return (int64_t)p.cu_q[i] * p.r / ROWS + i <= (int64_t)slot; });
-        if (b >= p.B) return false;
+        // 64 sequences' bounds in flight at once, a lane each
+        auto before = [&](int end, int i) { return (int64_t)end * p.r / ROWS + i <= (int64_t)slot; };
+        const int lo = near_before(p.B, lane, [&](int i) { return before(p.cu_q[i], i); }), held = min(p.B - lo, 64);
+        const int ends_q = lane < held ? p.cu_q[lo + lane + 1] : 0, ends_k = lane < held ? p.cu_k[lo + lane + 1] : 0;
+        const int begin_q = p.cu_q[lo], begin_k = p.cu_k[lo];
+        const int c = __popcll(__builtin_amdgcn_ballot_w64(lane < held && before(ends_q, lo + lane + 1)));
+        if (c >= held) return false;
         auto bounded = [](int v, int most) { return min(max(v, 0), most); };
-        q0 = bounded(p.cu_q[b], p.M);
-        k0 = bounded(p.cu_k[b], p.Mk);
-        Tq = bounded(p.cu_q[b + 1], p.M) - q0;
-        Tk = max(bounded(p.cu_k[b + 1], p.Mk) - k0, 0);
-        const int64_t tile = (int64_t)slot - ((int64_t)p.cu_q[b] * p.r / ROWS + b);
+        const int at_q = c ? __builtin_amdgcn_readlane(ends_q, c - 1) : begin_q, at_k = c ? __builtin_amdgcn_readlane(ends_k, c - 1) : begin_k;
+        q0 = bounded(at_q, p.M);
+        k0 = bounded(at_k, p.Mk);
+        Tq = bounded(__builtin_amdgcn_readlane(ends_q, c), p.M) - q0;
+        Tk = max(bounded(__builtin_amdgcn_readlane(ends_k, c), p.Mk) - k0, 0);
+        const int64_t tile = (int64_t)slot - ((int64_t)at_q * p.r / ROWS + lo + c);
         if (Tq <= 0 || tile < 0 || tile * ROWS >= (int64_t)Tq * p.r) return false;
         first = (int)(tile * ROWS);                      // below 2^31
         lo_pos = Tk - Tq + first / p.r;

@@ -409,6 +409,17 @@ def test_prefill_more_queries_than_tokens_and_rows_of_no_sequence():
     assert not api.attention_prefill(q, none, none, _ints([0, 80]), _ints([0, 0])).any()
 
 
+@pytest.mark.parametrize("B", [1, 64, 65, 200])
+def test_prefill_of_many_sequences(B):
+    """More sequences than the lanes of a wave, empty ones among them; queries in front of the first row of the first sequence."""
+    new, held = [(5 * b) % 4 for b in range(B - 1)] + [3], [(11 * b) % 90 for b in range(B)]
+    q, k, v, cu_q, cu_k = _prompts(new, held, 4, 2, 113)
+    ws = api.new_workspace(api.attention_prefill_workspace_bytes(len(q), len(k), B, 4, 2), DEV)
+    for room in (None, ws):
+        out = api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), window=40, sinks=2, workspace=room)
+        _check_prefill(out, q, k, v, cu_q, cu_k, 40, 2)
+
+
 def test_prefill_strided_slices():
     H, Hkv, M = 8, 2, 150
     qkv = torch.cat((_heads(M, H, 101, 4), _heads(M, Hkv, 102), _heads(M, Hkv, 103, 4)), dim=1)
