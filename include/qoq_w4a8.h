@@ -280,7 +280,7 @@ int qoq_kv4_unpack(const void* cache, int64_t B, int64_t Hkv, int64_t S_max, int
  *     y = x gamma / sqrt(mean(x^2) + eps)          per head, where q_gamma / k_gamma [128] FP16 are given (else y = x)
  *     (a, b) -> (a cos - b sin, b cos + a sin)      the pairs (i, i + rot/2) of y's first `rot` elements, or (2i, 2i + 1)
  *                                                   with `interleaved`; cos = angles[p][i], sin = angles[p][rot/2 + i]
- *   evaluated in FP64 and rounded once to FP16: q_out, k_out; k_out and v are quantized exactly as qoq_kv4_append does and
+ *   evaluated in FP64 and converted to FP32 and that to FP16: q_out, k_out; k_out and v are quantized exactly as qoq_kv4_append does and
  *   written into the pages of their positions (positions outside [0, 64 width) are dropped).
  *   angles    [angle_rows, rot] FP32; rot = 0 with NULL: no rotation; else a multiple of 16 up to 128.  Positions outside
  *             [0, angle_rows) take the nearest row.

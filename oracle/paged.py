@@ -12,7 +12,8 @@ PAGE = 64
 
 def turn_heads(x_fp16, gamma_fp16, eps, angles, positions, interleaved):
     """x_fp16 [M, heads, D], one position per row -> the same in FP16: x gamma / sqrt(mean(x^2) + eps) where gamma is given, then the
-    rotation by angles [rows, rot] float32 (cosines, sines; None: none), in float64, rounded once."""
+    rotation by angles [rows, rot] float32 (cosines, sines; None: none), in float64, converted to float32 and that to
+    float16."""
     y = np.asarray(x_fp16, dtype=np.float16).astype(np.float64)
     if gamma_fp16 is not None:
         y = y / np.sqrt((y * y).mean(axis=-1, keepdims=True) + eps) * np.asarray(gamma_fp16, dtype=np.float16).astype(np.float64)
@@ -26,7 +27,7 @@ def turn_heads(x_fp16, gamma_fp16, eps, angles, positions, interleaved):
     if gamma_fp16 is None and angles is None:
         return np.asarray(x_fp16, dtype=np.float16)
     with np.errstate(over="ignore"):
-        return y.astype(np.float16)
+        return y.astype(np.float32).astype(np.float16)
 
 
 def rows_of(cu, starts, M):

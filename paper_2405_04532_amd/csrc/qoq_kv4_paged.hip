@@ -20,7 +20,7 @@ namespace {
 // are exchanges inside the row.
 //   y = x gamma r,  r = 1 / sqrt(mean(x^2) + eps)   (with gamma);   pairs (a, b) -> (a cos - b sin, b cos + a sin)
 // x gamma is exact in FP32 (two 11-bit numbers), its product with the FP32 cosine exact in FP64, whose multiply-add runs at
-// FP32's rate here, so everything behind x gamma is FP64 and the result the FP64 evaluation rounded once to FP16.
+// FP32's rate here, so everything behind x gamma is FP64 up to the conversion to FP16.
 // ------------------------------------------------------------------------------------------
 struct AppendArgs {
     const __half *q, *k, *v;                     // token rows, their strides in elements
@@ -41,25 +41,16 @@ struct AppendArgs {
     uint32_t q_items, q_groups, q_heads;         // waves for queries: groups of q_heads heads per four rows
 };
 
-// Numbers as FP16, rounded once: through FP32 unless that could be a midpoint of two FP16 numbers (its last 12 bits are then zero).
-// There the FP32 number is cut off instead and its last bit set where something was: no midpoint, and on the right side of it.
+// FP64 to FP16 through FP32, as programs convert (there is no direct instruction): within 1/2 + 2^-14 of a step, and the bits of a
+// plain FP64 evaluation that is converted so.  One rounding instead costs a look for midpoints at every element, and one key in 16000
+// is then another neighbour of such a midpoint than theirs, which now and then moves a 4-bit code by one.
 __device__ __forceinline__ uint4 halves_of(const double (&y)[8])
 {
     float f[8];
-    uint32_t least = 0xFFFu;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         f[e] = (float)y[e];
-        least = min(least, (uint32_t)__float_as_int(f[e]) & 0xFFFu);
-    }
-    if (least == 0) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const double back = f[e];
-            uint32_t bits = __float_as_uint(f[e]);
-            bits -= fabs(back) > fabs(y[e]) ? 1u : 0u;
-            f[e] = __uint_as_float(bits | (back != y[e] ? 1u : 0u));
-        }
+        asm("" : "+v"(f[e]));                                              // else the two conversions become one in software
     }
     uint32_t o[4];
 #pragma unroll

@@ -151,9 +151,9 @@ def test_append_drops_what_has_no_place_and_leaves_other_rows():
     assert api.kv4_paged_gather(pool, table, _ints([0, 0, 0, 0]), None, 0, Hkv)[0].shape == (0, Hkv, D)
 
 
-def test_append_rounds_once():
+def test_append_rounding():
     """Results at and next to midpoints of FP16 numbers, subnormal and overflowing ones, infinities and NaN: the float64 evaluation
-    rounded once."""
+    by way of float32."""
     M, H = 64, 4
     g = torch.Generator().manual_seed(8)
     x = (torch.randn(M, H, D, generator=g) * torch.exp2(torch.randint(-24, 16, (M, H, 1), generator=g).float())).half()
