@@ -304,7 +304,8 @@ int qoq_kv4_unpack(const void* cache, int64_t B, int64_t Hkv, int64_t S_max, int
  *   zero row.  Infinities and NaN in keys and values reach the queries that see them, and no others.
  *   out [M, H, 128] FP16 contiguous; workspace as above, of qoq_attention_prefill_workspace_bytes(...) bytes.
  * Limits: D = 128; B <= 1048576, Hkv <= 1024, M and Mk <= 16777216, width <= 262144, pages <= 2^31 - 1, window and sinks >= 0; in decode
- * H / Hkv <= 16.  Errors as above. */
+ * H / Hkv <= 16.  Calls whose rows, sequences and heads come to 2^24 workgroups or more are refused as QOQ_ERR_HIP (decode: B Hkv;
+ * the others: a sequence takes a workgroup for each KV head even if it is empty).  Errors as above. */
 size_t qoq_kv4_pool_bytes(int64_t pages, int64_t Hkv, int64_t D);
 int qoq_qk_rope_kv4_append(const void* q_fp16, int64_t q_stride, const void* k_fp16, int64_t k_stride, const void* v_fp16, int64_t v_stride,
                            const void* q_gamma_fp16, const void* k_gamma_fp16, double eps, const float* angles, int64_t angle_rows,

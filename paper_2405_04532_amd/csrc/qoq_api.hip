@@ -487,7 +487,7 @@ int qoq_kv4_paged_gather(const void* pool, int64_t pages, const int32_t* block_t
 
 static bool paged_decode_ok(int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t width, int64_t window, int64_t sinks)
 {
-    return paged_ok(B, Hkv, D, 1, width) && H > 0 && H % Hkv == 0 && H / Hkv <= 16 && window_ok(window, sinks) && B * Hkv < (int64_t)1 << 31;
+    return paged_ok(B, Hkv, D, 1, width) && H > 0 && H % Hkv == 0 && H / Hkv <= 16 && window_ok(window, sinks);
 }
 
 size_t qoq_kv4_paged_attention_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t width, int64_t window, int64_t sinks)

@@ -785,7 +785,7 @@ hipError_t launch_rope_append(const RopeAppend& a, hipStream_t s)
     p.kv_heads = heads_to_a_wave(quads, a.Hkv);
     p.kv_groups = (uint32_t)((a.Hkv + p.kv_heads - 1) / p.kv_heads);
     const int64_t kv_items = slots * p.kv_groups, q_items = p.q ? quads * p.q_groups : 0;
-    if (kv_items + q_items >= (int64_t)1 << 31) return hipErrorInvalidValue;
+    if (kv_items + q_items > 4 * kMaxGrid) return hipErrorInvalidValue;
     p.kv_items = (uint32_t)kv_items; p.q_items = (uint32_t)q_items;
     auto* kernel = a.rot == kD ? (a.interleaved ? rope_append_kernel<true, true> : rope_append_kernel<false, true>)
                                : (a.interleaved ? rope_append_kernel<true, false> : rope_append_kernel<false, false>);
@@ -797,7 +797,7 @@ hipError_t launch_paged_gather(const uint8_t* pool, int64_t pages, const int32_t
                                const int32_t* starts, int64_t M, int64_t B, int64_t Hkv, void* k_out, void* v_out, hipStream_t s)
 {
     const int64_t items = (M / 16 + 2 * B) * Hkv;
-    if (items >= (int64_t)1 << 31) return hipErrorInvalidValue;
+    if (items > 4 * kMaxGrid) return hipErrorInvalidValue;
     paged_gather_kernel<<<(unsigned)((items + 3) / 4), 256, 0, s>>>(pool, table, cu, starts, static_cast<__half*>(k_out), static_cast<__half*>(v_out),
                                                                      (uint32_t)pages, (int)width, (int)M, (int)B, (int)Hkv, (uint32_t)items);
     return hipGetLastError();
@@ -839,6 +839,7 @@ hipError_t launch_paged_decode(const void* q, int64_t q_stride, const uint8_t* p
     p.parts = workspace ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes) : nullptr;
     const int ns = workspace ? paged_splits(B, Hkv, width, window, sinks) : 1;
     const bool nt = B * Hkv * most_seen(width, window, sinks) / kPageTokens * kPageBytes >= (int64_t)24 << 20;
+    if (B * Hkv > kMaxGrid) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(B * Hkv), (unsigned)ns);
     const int PK = p.R <= 8 ? 2 : 1;
     const size_t lds = std::max((size_t)kWaves * PK * p.R * kPartial * sizeof(float), (kMaxSplits + 1) * kMaxRatio * sizeof(float) + 64 * kWaves * sizeof(float4));

@@ -698,7 +698,7 @@ hipError_t launch_prefill(const Prefill& a, hipStream_t s)
     p.M = (int)a.M; p.Mk = (int)a.Mk; p.B = (int)a.B; p.H = (int)a.H; p.Hkv = (int)a.Hkv; p.r = (int)(a.H / a.Hkv);
     p.window = (int)a.window; p.sinks = a.window ? (int)a.sinks : 0;
     const Plan plan = prefill_plan(a.M, a.Mk, a.B, a.H, a.Hkv, a.window, a.sinks);
-    if (plan.tiles >= (int64_t)1 << 31) return hipErrorInvalidValue;
+    if (plan.tiles > kMaxGrid) return hipErrorInvalidValue;
     p.slots = (uint32_t)(plan.tiles / a.Hkv);
     p.ns = a.workspace ? plan.ns : 1;
     p.parts = p.ns > 1 ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + kCounterBytes) : nullptr;

@@ -9,6 +9,8 @@
 
 namespace qoq {
 
+constexpr int64_t kMaxGrid = (1 << 24) - 1;                 // workgroups of 256 threads: a grid's dimension has less than 2^32 threads
+
 // Number of b in 1 .. B for which before(b) holds, a condition that is true up to some b and false from there on: a search by the
 // 64 lanes of a wave, no round of loads for up to 64 sequences, one up to 4096, until the number lies in lo .. lo + 63, the result.  It
 // lies in 0 .. B whatever before() says.

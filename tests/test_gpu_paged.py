@@ -363,7 +363,7 @@ def _check_prefill(out, q, k, v, cu_q, cu_k, window, sinks, rows=None):
         assert not have[blind].any()
 
 
-@pytest.mark.parametrize("H,Hkv", [(2, 2), (4, 1), (7, 1), (6, 2), (40, 1)])
+@pytest.mark.parametrize("H,Hkv", [(2, 2), (4, 1), (7, 1), (6, 2), (40, 1), (64, 1)])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (40, 0), (100, 5), (64, 70)])
 def test_prefill(H, Hkv, window, sinks):
     new, held = [1, 0, 33, 64, 130, 3], [0, 5, 0, 1, 70, 200]
@@ -609,3 +609,210 @@ def test_another_stream_and_refusals_of_the_binding():
     for bad in (dict(rows=-1), dict(Hkv=0), dict(k_out=k[:5]), dict(cu=c.long()), dict(starts=_ints([0, 0]))):
         with pytest.raises((TypeError, ValueError, api.QoqError)):
             api.kv4_paged_gather(**{**dict(pool=pool, block_table=table, cu=c, starts=None, rows=T, Hkv=Hkv), **bad})
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# Graphs, streams, far offsets
+# ------------------------------------------------------------------------------------------------------------------
+def test_a_graph_of_a_prompt_and_a_token():
+    """Append, gather, a long prompt's and a few rows' attention and a decode step in one graph with one workspace, replayed with
+    other inputs in the same tensors and eager calls in the same workspace between; every replay against the eager calls."""
+    H, Hkv, window, sinks = 8, 2, 0, 0
+    held, new, width = 4100, 512, 73
+    total = held + new
+    pool, table, pages, cu, _, _ = _filled([total], Hkv, width, 301)
+    angles = api.rope_angles(width * PAGE, device=DEV)
+    cu_new, cu_few, cu_all, starts, lens = _ints([0, new]), _ints([0, 20]), _ints([0, total]), _ints([held]), _ints([total])
+    needs = [api.attention_prefill_workspace_bytes(m, total, 1, H, Hkv) for m in (new, 20)] + [api.kv4_paged_attention_workspace_bytes(1, H, Hkv, width)]
+    assert min(needs) > api.GEMM_COUNTER_BYTES                             # all three share keys between workgroups
+    ws = api.new_workspace(max(needs), DEV)
+    x = torch.empty((new, H + 2 * Hkv, D), dtype=torch.float16, device=DEV)
+    q, k = torch.empty((new, H, D), dtype=torch.float16, device=DEV), torch.empty((total, Hkv, D), dtype=torch.float16, device=DEV)
+    v, outs = torch.empty_like(k), [torch.empty((m, H, D), dtype=torch.float16, device=DEV) for m in (new, 20, 1)]
+
+    def step():
+        api.qk_rope_kv4_append(x[:, :H], x[:, H:H + Hkv], x[:, H + Hkv:], pool, table, cu_new, starts, angles, q_out=q)
+        api.kv4_paged_gather(pool, table, cu_all, None, total, Hkv, k, v)
+        api.attention_prefill(q, k, v, cu_new, cu_all, window, sinks, out=outs[0], workspace=ws)
+        api.attention_prefill(q[-20:], k, v, cu_few, cu_all, window, sinks, out=outs[1], workspace=ws)
+        api.kv4_paged_attention_decode(q[-1:], pool, table, lens, Hkv, window, sinks, out=outs[2], workspace=ws)
+
+    fill = lambda seed: x.copy_(torch.cat((_heads(new, H, seed), _heads(new, Hkv, seed + 1), _heads(new, Hkv, seed + 2, 4)), dim=1))      # noqa: E731
+    want = []
+    for seed in (310, 320, 330):
+        fill(seed)
+        step()
+        want.append([t.clone() for t in (q, k, v, *outs)])
+    _check_prefill(outs[0], q, k, v, [0, new], [0, total], window, sinks, rows=20)
+    _check_prefill(outs[1], q[-20:], k, v, [0, 20], [0, total], window, sinks)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for i in (0, 1, 2, 1, 0):
+        fill((310, 320, 330)[i])
+        for t in (q, k, v, *outs):
+            t.fill_(7.0)
+        graph.replay()
+        for have, exp in zip((q, k, v, *outs), want[i]):
+            assert _same(have, exp)
+        torch.cuda.synchronize()
+        few = api.attention_prefill(q[:3], k, v, _ints([0, 3]), cu_all, window, sinks, workspace=ws)
+        _check_prefill(few, q[:3], k, v, [0, 3], [0, total], window, sinks)
+    assert not ws[:api.GEMM_COUNTER_BYTES].any()
+
+
+def test_two_streams_at_once():
+    """Calls that overlap in time, each with a workspace of its own, on the same cache."""
+    H, Hkv, lens = 8, 2, [3000, 1700]
+    width = 48
+    pool, table, pages, cu, kh, vh = _filled(lens, Hkv, width, 341)
+    k, v = (torch.from_numpy(t.astype(np.float16)).to(DEV) for t in (kh, vh))
+    seq, cu_k, cu_q = _ints(lens), _ints(cu), _ints([0, 9, 12])
+    q, few = wl.make_queries(2, H, D, 343, DEV), _heads(12, H, 344, 4)
+    sizes = [api.kv4_paged_attention_workspace_bytes(2, H, Hkv, width), api.attention_prefill_workspace_bytes(12, sum(lens), 2, H, Hkv)]
+    assert min(sizes) > 0
+    streams, spaces = [torch.cuda.Stream() for _ in range(2)], [api.new_workspace(max(sizes), DEV) for _ in range(2)]
+    want = (api.kv4_paged_attention_decode(q, pool, table, seq, Hkv, workspace=spaces[0]), api.attention_prefill(few, k, v, cu_q, cu_k, workspace=spaces[0]))
+    _check_decode(want[0], q, kh, vh, cu, lens, 0, 0)
+    _check_prefill(want[1], few, k, v, [0, 9, 12], cu, 0, 0)
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for stream, ws, kept in zip(streams, spaces, got):
+            with torch.cuda.stream(stream):
+                kept.append((api.kv4_paged_attention_decode(q, pool, table, seq, Hkv, workspace=ws), api.attention_prefill(few, k, v, cu_q, cu_k, workspace=ws)))
+    torch.cuda.synchronize()
+    for a, b in got[0] + got[1]:
+        assert _same(a, want[0]) and _same(b, want[1])
+
+
+def test_pages_shared_by_sequences():
+    """Sequences with a common beginning name the same pages; a sequence may name a page more than once."""
+    H, Hkv, width = 8, 2, 6
+    pool, table, pages, cu, kh, vh = _filled([256, 100], Hkv, width, 351)
+    t = table.clone()
+    t[1, 2:4] = table[1, :2]                                               # 128 tokens of the first, then the second's 100
+    t[1, :2] = table[0, :2]
+    t[0, 4] = t[0, 1]                                                      # and the first goes on with its own second page
+    lens = [320, 228]
+    q = wl.make_queries(2, H, D, 353, DEV)
+    pick = np.concatenate((np.arange(256), np.arange(64, 128), np.arange(128), 256 + np.arange(100)))
+    out = api.kv4_paged_attention_decode(q, pool, t, _ints(lens), Hkv)
+    _check_decode(out, q, kh[pick], vh[pick], [0, 320, 548], lens, 0, 0)
+    gk, gv = api.kv4_paged_gather(pool, t, _ints([0, 320, 548]), None, 548, Hkv)
+    assert _same(gk, kh[pick].astype(np.float16)) and _same(gv, vh[pick].astype(np.float16))
+
+
+def test_pages_past_four_gigabytes():
+    """The last pages of a pool of more than 2^32 bytes hold, return and serve what the first ones of a small pool do."""
+    H, Hkv, lens = 8, 8, [200, 65]
+    small, table, pages, cu, kh, vh = _filled(lens, Hkv, 4, 361)
+    many = (1 << 32) // (Hkv * 8704) + 100
+    far = torch.where(table >= 0, many - 1 - table, table)
+    pool = torch.empty(many * Hkv * 8704, dtype=torch.uint8, device=DEV)
+    M = sum(lens)
+    q, k, v = _heads(M, H, 363, 4), _heads(M, Hkv, 364), _heads(M, Hkv, 365, 4)
+    angles = api.rope_angles(256, device=DEV)
+    got, one = [], wl.make_queries(2, H, D, 366, DEV)
+    for p, t in ((small, table), (pool, far)):
+        turned, _ = api.qk_rope_kv4_append(q, k, v, p, t, _ints(cu), None, angles)
+        got.append((turned, *api.kv4_paged_gather(p, t, _ints(cu), None, M, Hkv), api.kv4_paged_attention_decode(one, p, t, _ints(lens), Hkv)))
+    for a, b in zip(*got):
+        assert _same(a, b)
+
+
+def test_rows_past_four_gigabytes():
+    """The last rows of tensors of more than 2^32 bytes, and rows that lie the largest stride apart."""
+    H, Hkv, n = 8, 2, 600
+    q, k, v, _, _ = _prompts([n], [0], H, Hkv, 371)
+    want = api.attention_prefill(q, k, v, _ints([0, n]), _ints([0, n]))
+    M = (1 << 32) // (H * D * 2) + 1000
+    big_q, out = torch.empty((M, H, D), dtype=torch.float16, device=DEV), torch.empty((M, H, D), dtype=torch.float16, device=DEV)
+    big_q[-n:] = q
+    out[0], out[-n - 1] = 3.0, 4.0
+    api.attention_prefill(big_q, k, v, _ints([M - n, M]), _ints([0, n]), out=out)
+    # (a grid for so many rows takes 128 of them to a workgroup: other tiles, the same bound)
+    _check_prefill(out[-n:], q, k, v, [0, n], [0, n], 0, 0, rows=40)
+    assert bool((out[0] == 3).all()) and bool((out[-n - 1] == 4).all())
+    angles = api.rope_angles(n, device=DEV)
+    pool, table = api.kv4_new_pool(10, Hkv, DEV), _ints([[2, 0, 1, 9, 8, 7, 4, 3, 6, 5]])
+    turned, _ = api.qk_rope_kv4_append(q, k, v, pool, table, _ints([0, n]), None, angles)
+    kv = torch.zeros((M, 2 * Hkv, D), dtype=torch.float16, device=DEV)
+    kv[-n:, :Hkv], kv[-n:, Hkv:] = k, v
+    other = torch.zeros_like(pool)
+    api.qk_rope_kv4_append(big_q, kv[:, :Hkv], kv[:, Hkv:], other, table, _ints([M - n, M]), None, angles, q_out=big_q)
+    assert _same(big_q[-n:], turned)
+    gk, gv = (t.view(-1)[:M * Hkv * D].view(M, Hkv, D) for t in (out, kv))
+    api.kv4_paged_gather(other, table, _ints([M - n, M]), None, M, Hkv, gk, gv)
+    ek, ev = api.kv4_paged_gather(pool, table, _ints([0, n]), None, n, Hkv)
+    assert _same(gk[-n:], ek) and _same(gv[-n:], ev)
+    del big_q, out, kv, gk, gv
+    wide = torch.empty((n, 1 << 22), dtype=torch.float16, device=DEV)
+    qs, ks, vs = wide[:, :H * D].view(n, H, D), wide[:, H * D:(H + Hkv) * D].view(n, Hkv, D), wide[:, -Hkv * D:].view(n, Hkv, D)
+    qs.copy_(q), ks.copy_(k), vs.copy_(v)
+    assert _same(api.attention_prefill(qs, ks, vs, _ints([0, n]), _ints([0, n])), want)
+    many = _heads(n, 64, 373, 4)                                           # 128 rows to a workgroup
+    assert _same(api.attention_prefill(many, ks, vs, _ints([0, n]), _ints([0, n])), api.attention_prefill(many, k, v, _ints([0, n]), _ints([0, n])))
+    pool.zero_()
+    assert _same(api.qk_rope_kv4_append(qs, ks, vs, pool, table, _ints([0, n]), None, angles)[0], turned)
+    assert _same(api.kv4_paged_gather(pool, table, _ints([0, n]), None, n, Hkv)[0], ek)
+
+
+def test_longest_sequence():
+    """2^24 tokens, the most a table of 262144 pages holds, all in one page named again and again: each of its 64 tokens has the same
+    weight as alone.  Each of 256 waves adds up 2^16 of them: 2^16 roundings of 2^-24 at most for the products, 2^13 for the weights, of
+    which a lane has 4 of a chunk's 32, all relative to the sums of magnitudes."""
+    H, Hkv, width = 4, 1, 1 << 18
+    pool, table, pages, cu, kh, vh = _filled([64], Hkv, 1, 381)
+    long = table[:, :1].repeat(1, width).contiguous()
+    q = wl.make_queries(1, H, D, 383, DEV)
+    ref, spread = paged.attention(q.cpu().numpy().astype(np.float64), kh, vh, [63])
+    tol, _ = _bound(q.cpu().numpy().astype(np.float64), kh, ref, spread, 64)
+    tol = tol + (2.0 ** 16 + 2.0 ** 13) * 2.0 ** -24 * spread + 64 * 15 * 2.0 ** -25 + 2.0 ** -25
+    ws = api.new_workspace(api.kv4_paged_attention_workspace_bytes(1, H, Hkv, width), DEV)
+    for length in (1 << 24, (1 << 31) - 1):                                # (more than the table holds: as many as it does)
+        out = api.kv4_paged_attention_decode(q, pool, long, _ints([length]), Hkv, workspace=ws)
+        assert (np.abs(out.cpu().numpy().astype(np.float64) - ref) <= tol).all()
+    # through a window, behind the first tokens: the page's last 40 and first 5 tokens
+    out = api.kv4_paged_attention_decode(q, pool, long, _ints([1 << 24]), Hkv, window=40, sinks=5, workspace=ws)
+    see = np.array([t >= 24 or t < 5 for t in range(64)])
+    ref, spread = paged.attention(q.cpu().numpy().astype(np.float64), kh, vh, [63], held=see)
+    tol, _ = _bound(q.cpu().numpy().astype(np.float64), kh, ref, spread, 64)
+    assert (np.abs(out.cpu().numpy().astype(np.float64) - ref) <= tol + 64 * 15 * 2.0 ** -25 + 2.0 ** -25).all()
+    # the last token appended by its position
+    k, v = _heads(1, Hkv, 385), _heads(1, Hkv, 386, 4)
+    api.kv4_paged_append(pool, k, v, long, _ints([0, 1]), _ints([(1 << 24) - 1]))
+    gk, gv = api.kv4_paged_gather(pool, long, _ints([0, 2]), _ints([(1 << 24) - 1]), 2, Hkv)
+    assert _same(gk[:1], paged.quantized(k.cpu().numpy()).astype(np.float16)) and not gk[1].any() and not gv[1].any()
+
+
+def test_prompt_attention_behind_millions_of_tokens():
+    """Keys of more than 2^32 bytes: three queries behind 2^24 - 5 tokens, whose keys are zero but for some at both ends and at
+    2^32 bytes; zero keys have one weight and zero values, so that the result has a plain form."""
+    n = (1 << 24) - 2
+    k, v = torch.zeros((n, 1, D), dtype=torch.float16, device=DEV), torch.zeros((n, 1, D), dtype=torch.float16, device=DEV)
+    at = np.concatenate((np.arange(5), (1 << 24) // 2 + np.arange(-4, 5), (1 << 24) - 300 + np.arange(6), np.arange(n - 6, n)))
+    some_k, some_v = _heads(len(at), 1, 391), _heads(len(at), 1, 392, 4)
+    q = (_heads(3, 2, 393, 4) * 4).contiguous()
+    k[torch.from_numpy(at).to(DEV)], v[torch.from_numpy(at).to(DEV)] = some_k, some_v
+    kd, vd, qd = (t.cpu().numpy().astype(np.float64) for t in (some_k, some_v, q))
+    ws = api.new_workspace(api.attention_prefill_workspace_bytes(3, n, 1, 2, 1), DEV)
+    for space in (ws, None):
+        got = api.attention_prefill(q, k, v, _ints([0, 3]), _ints([0, n]), workspace=space).cpu().numpy().astype(np.float64)
+        for i in range(3):
+            see = at <= n - 3 + i
+            for h in range(2):
+                s = kd[see, 0] @ qd[i, h] / np.sqrt(D)
+                top = max(s.max(), 0.0)
+                p = np.exp(s - top)
+                total = p.sum() + (n - 2 + i - see.sum()) * np.exp(-top)
+                ref, spread = p @ vd[see, 0] / total, p @ np.abs(vd[see, 0]) / total
+                e = 130 * 2.0 ** -24 * float((np.abs(kd[:, 0]) @ np.abs(qd[i, h])).max()) / np.sqrt(D)
+                # the zero keys' weights are one number, whose rounding does not average out: 2^-11 of it, or below FP16's normal numbers
+                # 2^-25 of the largest weight; and without a workspace a lane adds up its share of 2^17 tiles in four sums, two
+                # additions each: 2^18 half steps of 2^-24
+                loss = n * 2.0 ** -25 / total + 2.0 ** 18 * 2.0 ** -24
+                tol = 2 * 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2 * e + 2.0 ** -20 + loss) * spread + len(at) * 2.0 ** -25 * np.abs(vd).max()
+                assert (np.abs(got[i, h] - ref) <= tol).all(), (i, h)
