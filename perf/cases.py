@@ -5,13 +5,13 @@ Four kinds of work, all through the public functions of paper_2405_04532_amd.api
   linear   FP16 activations through one quantized layer: the activation quantizer and the W4A8 GEMM
   decode   one generation step of one decoder layer: the fused producers and the quantizer, the layer's GEMMs, one token
            per sequence appended to the 4-bit KV cache, and attention over the cache
-  prefill  the same layer over whole prompts (attention over a prompt is not part of this framework: its result is an
-           input here)
+  prefill  the same layer over whole prompts (what attention over the prompt gives is an input here; perf/operators.py
+           measures it, with the paged cache and the rotation)
   load     one layer's FP16 weights on their way to the packed form: as they are, rotated, or with the input channels
            reordered by the salience that calibration activations give them
 
-Rotary embedding and residual additions are the calling program's own, so queries, keys, values and the residual stream
-are inputs.  Weights and activations are synthetic: normal values with 1% of outlier channels, the structure that the
+Queries, keys, values and the residual stream are inputs: rotary embedding has its own measurement there, and residual
+additions are the calling program's own.  Weights and activations are synthetic: normal values with 1% of outlier channels, the structure that the
 method is built for.  Token counts, widths, batch sizes and contexts are spread over what these models are served with:
 1 to 4096 tokens in a call, 1 to 64 sequences, contexts of 64 to 8192 tokens.
 """
