@@ -21,6 +21,8 @@ namespace {
 //   y = x gamma r,  r = 1 / sqrt(mean(x^2) + eps)   (with gamma);   pairs (a, b) -> (a cos - b sin, b cos + a sin)
 // x gamma is exact in FP32 (two 11-bit numbers), its product with the FP32 cosine exact in FP64, whose multiply-add runs at
 // FP32's rate here, so everything behind x gamma is FP64 up to the conversion to FP16.
+// Bound by memory: a wave keeps two KV heads' or four queries' loads in flight and looks its rows and angles up once for up to eight heads.
+// 5 x 1733 tokens of 64 / 8 heads 53 us, 5.0 TB/s (a large copy: 5.2), with norms 60; one token of 32 / 32 heads 4.1, 64 of 32 / 8 with norms 5.2.
 // ------------------------------------------------------------------------------------------
 struct AppendArgs {
     const __half *q, *k, *v;                     // token rows, their strides in elements
@@ -269,7 +271,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs p)
 }
 
 // ------------------------------------------------------------------------------------------
-// Tokens of the cache back as FP16, (code - z) s rounded once: one wave per aligned 16 positions of a sequence and KV head.
+// Tokens of the cache back as FP16, (code - z) s rounded once: one wave per aligned 16 positions of a sequence and KV head, all its loads
+// at once, keys and values stored in whole rows.  Bound by the stores: 6 x 6000 tokens of 8 heads 23-30 us, 4.7-6 TB/s; 389 tokens of 32 heads 4.7.
 // ------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint2 values_of(uint32_t c4, float z, float s)     // four codes in the low 16 bits
 {
@@ -351,14 +354,19 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(const uint8_t* __rest
 // `ns` workgroups stand by for each (sequence, KV head); nwg of them attend, as many as give each wave at least `deal` chunks, and
 // their waves take the chunks in turn.  Unnormalised sums, maxima and weight sums meet in the workspace; the last workgroup to
 // arrive adds them up, in the order of the workgroups whichever arrives when, and leaves the counter at zero.
+//
+// Bound by memory where there are pairs enough, 64 x 1024 tokens of 32 heads 38.6 us (5.5 TB/s); else by the trips to memory one after the
+// other: table, page, a wave's chunks, and the join's (parts out, counter, parts in: about 4 us); 8192 tokens of 8 KV heads 10.6 us, 40 tokens 3.9.
 // ------------------------------------------------------------------------------------------
 constexpr int kPartial = kD + 4;                         // floats per head: 128 sums, the maximum, the weight sum (rows of 16 bytes)
 constexpr int kChunk = 32;                               // tokens per chunk: two tiles of 16 (divides the page)
 constexpr int kMaxRatio = 16;                            // query heads per KV head: the columns of one matrix instruction
 constexpr int kWaves = 4;                                // of a workgroup
-constexpr int kAlone = 5;                                // chunks per wave up to which one workgroup attends alone
-constexpr int kInFlight = 8;                            // sums of a thread of the join
-constexpr int kMaxSplits = 64;                          // workgroups to a (sequence, KV head): the lanes of a wave
+// Chunks per wave up to which one workgroup attends alone: the join costs as much.  8 x 300 tokens of 64 / 8 heads 5.4 us alone, 8.1 shared;
+// 1000 tokens of 8 or 32 KV heads 8.8 alone, 7.5 and 8.0 shared.
+constexpr int kAlone = 5;
+constexpr int kInFlight = 8;                             // sums of a thread of the join
+constexpr int kMaxSplits = 64;                           // workgroups to a (sequence, KV head): the lanes of a wave
 
 struct DecodeTail {                                      // arguments that are not needed at once
     const __half* q;
@@ -438,6 +446,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
     const int n_first = min((sinks + kChunk - 1) / kChunk, chunks);        // chunks of the sinks
     const int gap = max(lo / kChunk - n_first, 0);                         // chunks behind them that nothing sees
     const int n = chunks - gap;                                            // the list: i < n_first ? i : i + gap
+    // more workgroups shorten the waves' chains and lengthen the join: chunks to a wave grow with the root of their number
+    // (8192 tokens of 8 KV heads 10.6 us; 1 to a wave 12.5, 6 11.2; 32000 of one KV head 22.9; 1 to a wave 27.5)
     const int deal = max(2, (int)(__builtin_sqrtf((float)n) * 0.25f));
     const int nwg = n <= kAlone * kWaves ? 1 : min(ns, (n + kWaves * deal - 1) / (kWaves * deal));
     if (split >= nwg) return;
@@ -803,7 +813,8 @@ hipError_t launch_paged_gather(const uint8_t* pool, int64_t pages, const int32_t
     return hipGetLastError();
 }
 
-// Workgroups that stand by for each (sequence, KV head), and the tokens that a query can see at most
+// Workgroups that stand by for each (sequence, KV head), and the tokens that a query can see at most.  Two for each compute unit: with three
+// 37 x 700 tokens of 64 / 8 heads 12.3 us, 9.9 with two, 4 x 8192 of 32 / 8 14.0 and 13.3, 16 x 32000 through a window of 4096 19.4 and 18.9.
 static int64_t most_seen(int64_t width, int64_t window, int64_t sinks)
 {
     const int64_t S = width * kPageTokens;
@@ -838,9 +849,14 @@ hipError_t launch_paged_decode(const void* q, int64_t q_stride, const uint8_t* p
     p.counters = static_cast<int*>(workspace);
     p.parts = workspace ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes) : nullptr;
     const int ns = workspace ? paged_splits(B, Hkv, width, window, sinks) : 1;
+    // Codes past the caches where a call reads more than stays in them: 16 x 32000 tokens of 8 KV heads through a window of 4096 (71 MB) 18.5 us,
+    // 20.0 through them, 64 x 4000 (279 MB) 39 and 44; level at 27 and 36 MB, slower where the memory-side cache still holds a call's codes
+    // (64 x 300 of 32 heads, three caches in turn, 17.5 and 16.5; nine in turn 18.0 and 18.9).
     const bool nt = B * Hkv * most_seen(width, window, sinks) / kPageTokens * kPageBytes >= (int64_t)24 << 20;
     if (B * Hkv > kMaxGrid) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(B * Hkv), (unsigned)ns);
+    // Up to eight heads to a KV head, two tiles of tokens share the columns: half of the softmax's instructions for more code.  64 x 4000 tokens of
+    // 32 / 8 heads 39.0 us, a tile at a time 39.8, 16 x 8192 26.2 and 27.0; short sequences lose 0.2.
     const int PK = p.R <= 8 ? 2 : 1;
     const size_t lds = std::max((size_t)kWaves * PK * p.R * kPartial * sizeof(float), (kMaxSplits + 1) * kMaxRatio * sizeof(float) + 64 * kWaves * sizeof(float4));
     auto* kernel = PK == 2 ? (nt ? paged_decode_kernel<2, true> : paged_decode_kernel<2, false>)
