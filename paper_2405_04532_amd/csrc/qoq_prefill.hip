@@ -667,7 +667,7 @@ static int64_t row_tiles(int64_t M, int64_t B, int64_t H, int64_t Hkv, int64_t r
 // keys.  Measured, narrow and wide: 32 / 8 heads, 20 tokens behind 3000 15.0 and 17.7 us, 200 behind 4000 45 and 36, 300 behind 2000 48 and 32; 200 alone
 // 8.8 and 13.3; 32 / 32 heads, 256 alone 9.0 and 15.2, 512 18.4 and 21.5; 32 / 8 heads, 800 alone 34 and 23.
 // The keys of wide tiles are shared while there are less than two for each compute unit: 512 behind 4000 88 us whole, 60 shared; not where a
-// workgroup is through them before a second launch pays: 800 alone 23 whole, 28 shared.
+// workgroup is through them before a second launch pays: 800 alone 23 whole, 28 shared, 1024 alone of 32 / 32 heads 28 and 38.
 struct Plan { bool narrow; int ns; int64_t tiles; };
 static Plan prefill_plan(int64_t M, int64_t Mk, int64_t B, int64_t H, int64_t Hkv, int64_t window, int64_t sinks)
 {
