@@ -7,24 +7,21 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "qoq_ragged_search.h"
+
 namespace qoq {
 
 constexpr int64_t kMaxGrid = (1 << 24) - 1;                 // workgroups of 256 threads: a grid's dimension has less than 2^32 threads
 
 // Number of b in 1 .. B for which before(b) holds, a condition that is true up to some b and false from there on: a search by the
-// 64 lanes of a wave, no round of loads for up to 64 sequences, one up to 4096, until the number lies in lo .. lo + 63, the result.  It
-// lies in 0 .. B whatever before() says.
+// 64 lanes of a wave, no round of loads for up to 64 sequences, one up to 4096.  The result is an `lo` in 0 .. B (whatever before() says) such that
+// the number is lo plus the count of lanes below B - lo for which before(lo + lane + 1) holds; a count of 64 means that the number is B.
 template <class F>
 __device__ __forceinline__ int near_before(int B, int lane, F&& before)
 {
-    int lo = 0, n = B;                                       // the number lies in lo .. lo + n
-    while (n > 64) {
-        const int step = (n + 63) / 64, at = lo + (lane + 1) * step;
-        const int c = __popcll(__builtin_amdgcn_ballot_w64(at <= lo + n && before(at)));
-        n = min(step - 1, n - c * step);
-        lo += c * step;
-    }
-    return lo;
+    LaneSearch s{0, B};
+    while (!s.near(B)) s.narrow(__popcll(__builtin_amdgcn_ballot_w64(s.asks(lane) && before(s.candidate(lane)))));
+    return s.lo;
 }
 template <class F>
 __device__ __forceinline__ int count_before(int B, int lane, F&& before)

@@ -816,3 +816,43 @@ def test_prompt_attention_behind_millions_of_tokens():
                 loss = n * 2.0 ** -25 / total + 2.0 ** 18 * 2.0 ** -24
                 tol = 2 * 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2 * e + 2.0 ** -20 + loss) * spread + len(at) * 2.0 ** -25 * np.abs(vd).max()
                 assert (np.abs(got[i, h] - ref) <= tol).all(), (i, h)
+
+
+@pytest.mark.parametrize("B", [4096, 4097, 4160, 4161, 262208, 262209, 266304, 266305])
+def test_every_sequence_of_a_large_batch_is_found(B):
+    """One token per sequence, and so many sequences that 64 lanes look for one in two or three rounds, on both sides of where the last
+    round's candidates fill a wave: every sequence's codes, cached numbers and attention (one key, weight 1: its value's bits)."""
+    pages, width = -(-B // PAGE), 1
+    table = (torch.arange(B, dtype=torch.int32, device=DEV) // PAGE)[:, None].contiguous()      # 64 sequences to a page, each at its own place
+    starts = torch.arange(B, dtype=torch.int32, device=DEV) % PAGE
+    cu = torch.arange(B + 1, dtype=torch.int32, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(B)
+    q, k, v = (torch.randn((B, 1, D), generator=g, device=DEV, dtype=torch.float16) for _ in range(3))
+    pool = api.kv4_new_pool(pages, 1, DEV)
+    qo, ko = torch.full_like(q, 9.0), torch.full_like(k, 9.0)
+    angles = torch.cat((torch.ones(PAGE, 64), torch.zeros(PAGE, 64)), dim=1).to(DEV)             # no turn
+    api.qk_rope_kv4_append(q, k, v, pool, table, cu, starts, angles, q_out=qo, k_out=ko)
+    assert torch.equal(qo, q) and torch.equal(ko, k)
+    # the same tokens as one sequence's prompt: the pages of the pool in their order
+    alone = api.kv4_new_pool(pages, 1, DEV)
+    order = torch.arange(pages, dtype=torch.int32, device=DEV)[None]
+    api.kv4_paged_append(alone, k, v, order, _ints([0, B]))
+    assert torch.equal(pool, alone)
+    gk, gv = torch.full_like(k, 9.0), torch.full_like(v, 9.0)
+    api.kv4_paged_gather(pool, table, cu, starts, B, 1, gk, gv)
+    ek, ev = api.kv4_paged_gather(alone, order, _ints([0, B]), None, B, 1)
+    assert torch.equal(gk, ek) and torch.equal(gv, ev)
+    out = torch.full_like(q, 9.0)
+    api.attention_prefill(q, k, v, cu, cu, out=out)
+    assert torch.equal(out, v)
+
+
+@pytest.mark.parametrize("B", [4097, 4160])
+def test_prefill_of_thousands_of_ragged_sequences(B):
+    """Lengths from none to six, some behind cached tokens, and outputs that no sequence owns left as they were."""
+    new, held = [(5 * b) % 7 for b in range(B)], [(11 * b) % 9 for b in range(B)]
+    q, k, v, cu_q, cu_k = _prompts(new, held, 4, 2, 117, behind=3)
+    out = torch.full_like(q, 9.0)
+    api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), window=5, sinks=1, out=out)
+    assert bool((out[-3:] == 9).all())
+    _check_prefill(out, q, k, v, cu_q, cu_k, 5, 1)
