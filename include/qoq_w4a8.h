@@ -234,7 +234,8 @@ int qoq_hadamard_rotate(const void* src_fp16, int64_t rows, int64_t K, int64_t b
  * qoq_kv4_attention_decode: one new query token per sequence,
  *   out[b, h, :] = softmax_t( q[b, h, :] . K^[b, floor(h / r), t, :] / sqrt(D) ) V^[b, floor(h / r), t, :],
  *   t < seq_lens[b], r = H / Hkv an integer in 1 .. 16; K^, V^ the dequantized cache.  Products take FP16 operands
- *   (the softmax weight times the value scale is rounded to FP16 for that), sums and the softmax are FP32, one
+ *   (the softmax weight, at most about 1, times the value scale is rounded to FP16 for that: 2^-11 of itself, or 2^-25 where that is more,
+ *   which tokens of small values and small weights lose bits by; the paged form below does not), sums and the softmax are FP32, one
  *   rounding to FP16 at the end.  seq_lens[b] is clamped to [0, S_max]; an empty
  *   sequence gives a zero row.
  *   q_fp16 [B, H, D] FP16; seq_lens [B] INT32 device; out_fp16 [B, H, D] FP16 (written)
@@ -291,7 +292,8 @@ int qoq_kv4_unpack(const void* cache, int64_t B, int64_t Hkv, int64_t S_max, int
  *   sequence b, (code - z) s rounded once; zeros where it lies on no page.  For a prompt that goes on behind cached tokens.
  * qoq_kv4_paged_attention_decode: qoq_kv4_attention_decode over pages, q [B, H, 128] with a stride, out [B, H, 128] contiguous; of
  *   the seq_lens[b] tokens (clamped to [0, 64 width]) those t with  t >= seq_lens[b] - window  or  t < sinks  are seen; window = 0:
- *   all.  A query that sees nothing gives a zero row.
+ *   all.  A query that sees nothing gives a zero row.  Weight times value scale is rounded to FP16 relative to the largest there is:
+ *   2^-11 of itself, or 2^-39 of the largest weight times the largest scale where that is more.
  *   workspace  NULL, or at least qoq_kv4_paged_attention_workspace_bytes(...) bytes (0: none is needed), 16-byte aligned, zero-filled
  *              once with qoq_gemm_workspace_prepare, as for qoq_w4a8_gemm, whose workspace may be the same one: calls of both kinds
  *              and any shapes may take turns in it on one stream; calls that overlap in time need workspaces of their own.

@@ -348,17 +348,20 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(const uint8_t* __rest
 
 // ------------------------------------------------------------------------------------------
 // Decode attention over pages.  The arithmetic of a chunk of 32 tokens is that of the contiguous cache's kernel (qoq_kv4.hip): both
-// products on the matrix cores, codes unpacked in registers, softmax in place.
+// products on the matrix cores, codes unpacked in registers, softmax in place; but the weights' reference follows the values' scales too.
 //
 // What a sequence's query sees is a list of chunks: those of the sinks, then those of the window (without a window all of them).
 // `ns` workgroups stand by for each (sequence, KV head); nwg of them attend, as many as give each wave at least `deal` chunks, and
-// their waves take the chunks in turn.  Unnormalised sums, maxima and weight sums meet in the workspace; the last workgroup to
+// their waves take the chunks in turn.  Unnormalised sums, references and weight sums meet in the workspace; the last workgroup to
 // arrive adds them up, in the order of the workgroups whichever arrives when, and leaves the counter at zero.
+//
+// The second product's operand is weight x value scale in FP16: off by 2^-11 of itself, or by 2^-39 of the largest weight x scale where that is
+// more (a lane's largest weight times its largest scale, of four or eight tokens at a time).
 //
 // Bound by memory where there are pairs enough, 64 x 1024 tokens of 32 heads 38.6 us (5.5 TB/s); else by the trips to memory one after the
 // other: table, page, a wave's chunks, and the join's (parts out, counter, parts in: about 4 us); 8192 tokens of 8 KV heads 10.6 us, 40 tokens 3.9.
 // ------------------------------------------------------------------------------------------
-constexpr int kPartial = kD + 4;                         // floats per head: 128 sums, the maximum, the weight sum (rows of 16 bytes)
+constexpr int kPartial = kD + 4;                         // floats per head: 128 sums, their reference, the weight sum (rows of 16 bytes)
 constexpr int kChunk = 32;                               // tokens per chunk: two tiles of 16 (divides the page)
 constexpr int kMaxRatio = 16;                            // query heads per KV head: the columns of one matrix instruction
 constexpr int kWaves = 4;                                // of a workgroup
@@ -380,6 +383,7 @@ struct DecodeTail {                                      // arguments that are n
 // pages are addressed by a base in scalar registers, which comes out of the block table, and a lane's offset
 typedef const __attribute__((address_space(1))) uint8_t* global_bytes;
 typedef const __attribute__((address_space(1))) u32x4* global_u32x4;
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float4 load_part(const float* at)
 {
@@ -479,7 +483,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
         }
     }
 
-    float m = -1e29f, l = 0.f;                           // of this lane's column, over the tokens it has seen
+    // of this lane's column, over the tokens it has seen: the reference that scores are taken from before they become weights, and the weights'
+    // sum.  It follows the largest (score + exponent of the value's scale): weight x scale, which is rounded to FP16 for the matrix cores, then has
+    // its largest numbers below 2^15 whatever the values' size, and 29 binades lie between those and the first that loses bits.  (37 x 700 10.4 us
+    // without the scales, 10.5 with them, 64 x 4000 39.1 and 39.3, 8192 tokens 11.0 and 11.0.)
+    float m = -1e29f, l = 0.f;
     f4 acc[8];                                           // acc[4u + j][x]: element d = 16 kb + 4x + 64u + j of the column
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = (f4){0.f, 0.f, 0.f, 0.f};
@@ -541,17 +549,28 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
 #pragma unroll
             for (int tt = 0; tt < NS; ++tt) sc[tt] = d[tt];
         }
-        float m_new = m;
+        uint32_t pw[NS][4];                              // parameters of the values of the tokens whose scores this lane keeps
+#pragma unroll
+        for (int tt = 0; tt < NS; ++tt) {
+            const uint4 a = PK == 2 && second ? cur.vp[1] : cur.vp[tt];
+            pw[tt][0] = a.x; pw[tt][1] = a.y; pw[tt][2] = a.z; pw[tt][3] = a.w;
+        }
+        float top = -1e30f;
+        us2 largest = {0, 0};
 #pragma unroll
         for (int tt = 0; tt < NS; ++tt) {
             const uint32_t sw[4] = {cur.ks[tt].x, cur.ks[tt].y, cur.ks[tt].z, cur.ks[tt].w};
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 sc[tt][x] = fmaf(sc[tt][x], (float)half_of(sw[x]) * kScale, bias[tt][x]);
-                m_new = fmaxf(m_new, sc[tt][x]);
+                top = fmaxf(top, sc[tt][x]);
+                largest = __builtin_elementwise_max(largest, __builtin_bit_cast(us2, pw[tt][x]));
             }
         }
-        m_new = max_other_half(max_other_row(m_new));    // the four k-blocks of a column agree on the maximum
+        // the largest scale is below 2^(its exponent's bits - 14), so with this reference weight x scale stays below 2^15
+        const float exponent = (float)((largest.x >> 10) & 31u);
+        // the four k-blocks of a column agree on the reference
+        const float m_new = max_other_half(max_other_row(fmaxf(m, top + (exponent - 29.f))));
         if (__builtin_amdgcn_ballot_w64(m_new != m) != 0) {                  // rare once a few chunks have been seen
             const float alpha = __builtin_amdgcn_exp2f(m - m_new);
             m = m_new;
@@ -562,13 +581,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
         uint32_t bw[2][2];                               // B operand: softmax weight * value scale, tokens 4 kb .. of both tiles
 #pragma unroll
         for (int tt = 0; tt < NS; ++tt) {
-            const uint32_t pw[2][4] = {{cur.vp[0].x, cur.vp[0].y, cur.vp[0].z, cur.vp[0].w}, {cur.vp[1].x, cur.vp[1].y, cur.vp[1].z, cur.vp[1].w}};
             float wf[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 const float pr = __builtin_amdgcn_exp2f(sc[tt][x] - m);
                 l += pr;
-                wf[x] = pr * (float)half_of(PK == 2 ? (second ? pw[1][x] : pw[0][x]) : pw[tt][x]);
+                wf[x] = pr * (float)half_of(pw[tt][x]);
             }
             const uint32_t b_lo = __builtin_bit_cast(uint32_t, (h2){(_Float16)wf[0], (_Float16)wf[1]});
             const uint32_t b_hi = __builtin_bit_cast(uint32_t, (h2){(_Float16)wf[2], (_Float16)wf[3]});
@@ -582,10 +600,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
         h2 cz[2][2], cz16[2][2];
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
-            const uint32_t pw[4] = {cur.vp[tt].x, cur.vp[tt].y, cur.vp[tt].z, cur.vp[tt].w};
+            const uint32_t zw[4] = {cur.vp[tt].x, cur.vp[tt].y, cur.vp[tt].z, cur.vp[tt].w};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                cz[tt][h] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(pw[2 * h + 1], pw[2 * h], 0x07060302u));
+                cz[tt][h] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(zw[2 * h + 1], zw[2 * h], 0x07060302u));
                 cz16[tt][h] = cz[tt][h] + k960;
             }
         }
@@ -690,7 +708,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
     // The join: `groups` groups of n4 threads take the workgroups' sums in turn, kInFlight in flight beside the
     // maxima; the groups' own sums meet in LDS.
     const float* parts = p.parts + (size_t)bh * ns * R * kPartial;
-    float* s_factor = s_part;                            // [nwg][R]: 2^(maximum - the largest)
+    float* s_factor = s_part;                            // [nwg][R]: 2^(reference - the largest)
     float* s_den = s_factor + kMaxSplits * kMaxRatio;    // [R]
     float4* s_sum = reinterpret_cast<float4*>(s_den + kMaxRatio);          // [groups][n4]
     const int groups = max(1, 64 * kWaves / n4);
@@ -706,7 +724,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
             if (s0 + i * groups < nwg) a[i] = load_part(at + (size_t)(s0 + i * groups) * R * kPartial);
         }
     };
-    unsigned long long ml[kMaxRatio / kWaves];           // a wave per head, a lane per workgroup: maximum and weight sum
+    unsigned long long ml[kMaxRatio / kWaves];           // a wave per head, a lane per workgroup: reference and weight sum
 #pragma unroll
     for (int i = 0; i < kMaxRatio / kWaves; ++i)
         ml[i] = __hip_atomic_load(reinterpret_cast<unsigned long long*>(const_cast<float*>(parts) + ((size_t)min(lane, nwg - 1) * R + min(wave + i * kWaves, R - 1)) * kPartial + kD),

@@ -856,3 +856,65 @@ def test_prefill_of_thousands_of_ragged_sequences(B):
     api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), window=5, sinks=1, out=out)
     assert bool((out[-3:] == 9).all())
     _check_prefill(out, q, k, v, cu_q, cu_k, 5, 1)
+
+
+def _chosen(lens, k, v, width, seed):
+    """A pool with these keys and values: [tokens, Hkv, 128] FP16 of the sequences one after the other."""
+    table, pages = _tables(lens, width, seed)
+    cu = np.concatenate(([0], np.cumsum(lens)))
+    pool = torch.full((pages * k.shape[1] * 8704,), 0xFF, dtype=torch.uint8, device=DEV)
+    api.kv4_paged_append(pool, k, v, table, _ints(cu))
+    return pool, table, cu, paged.quantized(k.cpu().numpy()), paged.quantized(v.cpu().numpy())
+
+
+@pytest.mark.parametrize("H,Hkv", [(2, 2), (8, 1), (16, 1)])
+@pytest.mark.parametrize("ahead", [2.8, 8.3, 10.4, 17.0])
+@pytest.mark.parametrize("size,first", [(0.1, 1.0), (2.0 ** -10, 1.0), (2.0 ** -13, 1.0), (2.0 ** -16, 1.0), (1.0, 2.0 ** -9), (2.0 ** -8, 2.0 ** 9), (1.5e4, 1.0)])
+def test_decode_of_light_tokens(H, Hkv, ahead, size, first):
+    """A first token whose score is `ahead` above those of a long flat tail (natural logarithm), values of `size`, the first token's
+    `first` times that: the light tokens' weights times the scale of their values, however small, keep their share.
+    A product of weight and scale is rounded to FP16 as a multiple of a power of two: half a step is 2^-11 of it or, below FP16's normal numbers,
+    2^-25 of that power, which lies 2^14 below the largest weight times the largest scale, or lower (scales below 2^-15 count as
+    that).  So n tokens of codes up to 15 lose 15 n 2^-39 max(scale, 2^-15) at most, against weights whose sum is at least the largest of them."""
+    L, width, lens = 3000, 48, [3000, 700, 65]
+    n = sum(lens)
+    g = torch.Generator().manual_seed(int(ahead * 10) + H)
+    base = torch.randn(1, Hkv, D, generator=g)
+    q = (base.repeat_interleave(H // Hkv, 1) * (1 + 0.05 * torch.randn(len(lens), H, 1, generator=g))).half()
+    k = 0.02 * torch.randn(n, Hkv, D, generator=g)
+    v = (size * torch.randn(n, Hkv, D, generator=g)).clamp(-6e4, 6e4)       # (FP16 numbers)
+    cu = np.concatenate(([0], np.cumsum(lens)))
+    for at in cu[:-1]:
+        k[at] = base[0] * (ahead * np.sqrt(D) / (base[0] ** 2).sum(-1, keepdim=True))
+        v[at] = v[at] * first
+    pool, table, cu, kh, vh = _chosen(lens, k.half().to(DEV), v.half().to(DEV), width, 51)
+    scale = float(kv4.kv4_quantize(v.half().numpy())[1].astype(np.float64).max())
+    ws = api.new_workspace(api.kv4_paged_attention_workspace_bytes(3, H, Hkv, width), DEV)
+    for window, sinks, room in ((0, 0, ws), (0, 0, None), (600, 4, None)):
+        got = api.kv4_paged_attention_decode(q.to(DEV), pool, table, _ints(lens), Hkv, window, sinks, workspace=room).cpu().numpy().astype(np.float64)
+        for b, n_b in enumerate(lens):
+            kb, vb, qb = kh[cu[b]:cu[b] + n_b], vh[cu[b]:cu[b] + n_b], q[b:b + 1].numpy().astype(np.float64)
+            ref, spread = paged.attention(qb, kb, vb, [n_b - 1], window, sinks)
+            tol, _ = _bound(qb, kb, ref, spread, n_b)
+            tol = tol[0] + 15 * n_b * 2.0 ** -39 * max(scale, 2.0 ** -15) + 2.0 ** -25
+            assert (np.abs(got[b] - ref[0]) <= tol).all(), (b, window, float((np.abs(got[b] - ref[0]) / tol).max()))
+
+
+def test_decode_of_values_of_every_size():
+    """Values whose sizes change from token to token over all of FP16, up to its largest numbers: nothing overflows on the way."""
+    H, Hkv, lens, width = 8, 1, [2000, 33], 32
+    g = torch.Generator().manual_seed(77)
+    n = sum(lens)
+    q, k = torch.randn(2, H, D, generator=g).half(), torch.randn(n, Hkv, D, generator=g).half()
+    v = (torch.randn(n, Hkv, D, generator=g).clamp(-1.9, 1.9) * torch.exp2(torch.randint(-20, 16, (n, Hkv, 1), generator=g).float())).half()
+    pool, table, cu, kh, vh = _chosen(lens, k.to(DEV), v.to(DEV), width, 53)
+    assert bool(torch.isfinite(v).all()) and float(v.abs().max()) > 6e4
+    scale = float(kv4.kv4_quantize(v.numpy())[1].astype(np.float64).max())
+    ws = api.new_workspace(api.kv4_paged_attention_workspace_bytes(2, H, Hkv, width), DEV)
+    for room in (ws, None):
+        got = api.kv4_paged_attention_decode(q.to(DEV), pool, table, _ints(lens), Hkv, workspace=room).cpu().numpy().astype(np.float64)
+        for b, n_b in enumerate(lens):
+            kb, vb, qb = kh[cu[b]:cu[b] + n_b], vh[cu[b]:cu[b] + n_b], q[b:b + 1].numpy().astype(np.float64)
+            ref, spread = paged.attention(qb, kb, vb, [n_b - 1])
+            tol, _ = _bound(qb, kb, ref, spread, n_b)
+            assert (np.abs(got[b] - ref[0]) <= tol[0] + 15 * n_b * 2.0 ** -39 * scale + 2.0 ** -25).all(), b
