@@ -10,9 +10,11 @@
 //                                                       row are the lane's own but for one exchange between the halves
 //   O[d][row]   += sum_key v[key][d] p[key][row]       p's registers are the operand as they stand: the order of the keys in
 //                                                       the sum is free, and v is read transposed from LDS in that order
-// Softmax in base 2, FP32; the weights are rounded to FP16 for the second product (2^-11 relative, each on its own), sums stay FP32.
-// The running maximum is raised only when a score passes it by more than kSlack: weights then reach 2^kSlack, their FP16 numbers
-// have the same relative precision there, and the sums' 64 registers are rarely rescaled.
+// Softmax in base 2, FP32; the weights are rounded to FP16 for the second product, sums stay FP32.  They are taken relative to a reference
+// that lies 2^kLead below a row's largest score when it is set, and is raised only when a score passes it by more than another
+// 2^kSlack, so that the sums' 64 registers are rarely rescaled: the largest weight is between 2^7 and 2^15, and each is off by 2^-11 of
+// itself or, below FP16's normal numbers, by 2^-25, which is 2^-32 of the largest at most.  (Without the lead the second bound is 2^-25; times were level,
+// 3 x 4001 520 to 521 us, 256 alone 8.55 and 8.65.)
 // Bound by the matrix cores on large batches, 3 x 4001 tokens of 64 / 8 heads 502 us, 947 TFLOP/s (a large product of the library's: 1145), two
 // workgroups to a compute unit; by a workgroup's own chain of key tiles on short ones, 1024 tokens of 32 heads 25 us: 3.7 to the
 // first tile, then 1.2 to 1.4 for each of the last rows' 16.  A ring of four tiles was no faster (31), nor are weights spread over both products (27.5).
@@ -32,7 +34,7 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBM = 128, kBN = 64, kPrefillThreads = 256;
 constexpr int kRows = 32, kKeys = 32;                    // of the narrow kernel's tiles
-constexpr int kPart = kD + 4;                            // floats of a row's partial result: sums, maximum, weight sum, whether to do it again
+constexpr int kPart = kD + 4;                            // floats of a row's partial result: sums, reference, weight sum, whether to do it again
 constexpr int kRowBytes = kD * 2;                        // 256: sixteen 16-byte chunks
 constexpr int kRowPitch = kRowBytes + 16;                // of results in LDS
 constexpr int kTileBytes = kBN * kRowBytes;              // 16 KiB of keys, as much of values
@@ -40,7 +42,7 @@ constexpr float kScale = 1.4426950408889634f * 0.08838834764831845f;      // log
 constexpr int kMaxParts = 64;                            // workgroups to a row tile
 constexpr int kWideDeal = 8;                            // key tiles that a workgroup is given before another one attends
 constexpr int kNarrowDeal = 2;                          // key tiles that a wave is given before another workgroup attends
-constexpr float kSlack = 8.f / kScale;                   // in units of the scores
+constexpr float kLead = 7.f / kScale, kSlack = 8.f / kScale;              // in units of the scores
 
 struct PrefillArgs {
     const __half *q, *k, *v;
@@ -324,9 +326,9 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
                     }
             top = top_of(sc);
         }
-        if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
-            const float alpha = __builtin_amdgcn_exp2f((m - top) * kScale);
-            m = top;
+        if (__builtin_amdgcn_ballot_w64(top > m + (kLead + kSlack)) != 0) {
+            const float raised = fmaxf(m, top - kLead), alpha = __builtin_amdgcn_exp2f((m - raised) * kScale);
+            m = raised;
 #pragma unroll
             for (int x = 0; x < 4; ++x) l[x] *= alpha;
 #pragma unroll
@@ -452,7 +454,7 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
 // ------------------------------------------------------------------------------------------
 // Few rows.  A workgroup takes 32 rows, and its four waves take key tiles of 32 in turn, each through a ring of its own in LDS (two tiles of
 // keys and values), without meeting; p.ns workgroups stand by for a row tile, of which as many attend as get kNarrowDeal key tiles a
-// wave.  Sums, maxima and weight sums of the waves meet in LDS, those of the workgroups in the workspace, added up by a second launch.
+// wave.  Sums, references and weight sums of the waves meet in LDS, those of the workgroups in the workspace, added up by a second launch.
 // ------------------------------------------------------------------------------------------
 constexpr int kRing = 2 * kKeys * kRowBytes;             // a key tile's keys and values
 
@@ -536,9 +538,9 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
         for (int y = 0; y < 16; ++y) top = fmaxf(top, sc[0][y]);
         top = max_other_half(top);
-        if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
-            const float alpha = __builtin_amdgcn_exp2f((m - top) * kScale);
-            m = top;
+        if (__builtin_amdgcn_ballot_w64(top > m + (kLead + kSlack)) != 0) {
+            const float raised = fmaxf(m, top - kLead), alpha = __builtin_amdgcn_exp2f((m - raised) * kScale);
+            m = raised;
 #pragma unroll
             for (int x = 0; x < 4; ++x) l[x] *= alpha;
 #pragma unroll

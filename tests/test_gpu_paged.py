@@ -918,3 +918,49 @@ def test_decode_of_values_of_every_size():
             ref, spread = paged.attention(qb, kb, vb, [n_b - 1])
             tol, _ = _bound(qb, kb, ref, spread, n_b)
             assert (np.abs(got[b] - ref[0]) <= tol[0] + 15 * n_b * 2.0 ** -39 * scale + 2.0 ** -25).all(), b
+
+
+@pytest.mark.parametrize("H,Hkv,new,held", [(2, 1, 5, 6000), (4, 1, 700, 5300), (2, 2, 40, 0)])
+@pytest.mark.parametrize("ahead", [9.0, 12.5, 17.0])
+def test_prefill_of_light_tokens(H, Hkv, new, held, ahead):
+    """A first token whose score is `ahead` above those of all others (natural logarithm), which are alike, and whose values are zero: the others' weights
+    keep their share.  A weight is off by 2^-11 of itself or, below FP16's normal numbers, by 2^-25 where the largest of the row is at least
+    2^7: n 2^-32 max|v|."""
+    T = new + held
+    g = torch.Generator().manual_seed(int(10 * ahead))
+    base = torch.randn(1, Hkv, D, generator=g)
+    q = (base.repeat_interleave(H // Hkv, 1) * (1 + 0.02 * torch.randn(new, H, 1, generator=g))).half().to(DEV)
+    k, v = torch.zeros(T, Hkv, D, dtype=torch.float16, device=DEV), torch.randn(T, Hkv, D, generator=g).abs().half().to(DEV)
+    k[0] = (base[0] * (ahead * np.sqrt(D) / (base[0] ** 2).sum(-1, keepdim=True))).half().to(DEV)
+    v[0] = 0
+    cu_q, cu_k = [0, new], [0, T]
+    ws = api.new_workspace(api.attention_prefill_workspace_bytes(new, T, 1, H, Hkv), DEV)
+    pick = np.unique(np.concatenate((np.arange(min(new, 5)), np.linspace(0, new - 1, 20).astype(int))))
+    qd, kd, vd = (t.cpu().numpy().astype(np.float64) for t in (q, k, v))
+    ref, spread = paged.attention(qd[pick], kd, vd, held + pick)
+    tol, _ = _bound(qd[pick], kd, ref, spread, T)
+    tol = tol + T * 2.0 ** -32 * vd.max() + 2.0 ** -25
+    for room in (ws, None):
+        got = api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k), workspace=room).cpu().numpy().astype(np.float64)[pick]
+        assert (np.abs(got - ref) <= tol).all(), float((np.abs(got - ref) / tol).max())
+
+
+def test_prefill_of_a_million_light_tokens():
+    """Tokens whose weights are below FP16's normal numbers and make up a fifth of the sum: what the products take and what the weights' sum
+    takes are the same numbers.  The tokens are alike, so their roundings do not average out: 2^-25 of at least 2^7 each, and a lane
+    adds up its 2^13 tiles with the workspace, 2^15 without, in four sums of two additions a tile."""
+    n, ahead = 1 << 20, 15.3
+    g = torch.Generator().manual_seed(5)
+    q = torch.randn(1, 1, D, generator=g).half().to(DEV)
+    k, v = torch.zeros(n, 1, D, dtype=torch.float16, device=DEV), torch.full((n, 1, D), 0.5, dtype=torch.float16, device=DEV)
+    k[0], v[0] = q[0] * (ahead * np.sqrt(D) / float((q.float() ** 2).sum())), 0
+    score = float((q.double() * k[0].double()).sum()) / np.sqrt(D)
+    tail = (n - 1) * np.exp(-score)
+    ref = 0.5 * tail / (1 + tail)
+    assert 0.1 < tail < 0.4
+    ws = api.new_workspace(api.attention_prefill_workspace_bytes(1, n, 1, 1, 1), DEV)
+    e = 130 * 2.0 ** -24 * float((q.double().abs() * k[0].double().abs()).sum()) / np.sqrt(D)
+    for room, tiles in ((ws, 1 << 13), (None, 1 << 15)):
+        got = api.attention_prefill(q, k, v, _ints([0, 1]), _ints([0, n]), workspace=room).double().cpu().numpy()
+        tol = 2.0 ** -11 * ref + (2 * 2.0 ** -11 + 2 * e + 2.0 ** -20 + 2 * tiles * 2.0 ** -24) * ref + n * 2.0 ** -32 * 0.5
+        assert (np.abs(got - ref) <= tol).all(), (float(np.abs(got - ref).max()), tol)
