@@ -304,7 +304,7 @@ int qoq_kv4_unpack(const void* cache, int64_t B, int64_t Hkv, int64_t S_max, int
  *     out[i, h] = softmax_t(q[i, h] . k[t, h / r] / sqrt(128)) v[t, h / r],  r = H / Hkv <= 64
  *   FP32 softmax and sums, weights rounded to FP16 for the second product (2^-11 of itself, or 2^-32 of the row's largest where that is
  *   more), one rounding at the end.  A query that sees nothing gives a
- *   zero row.  Infinities and NaN in keys and values reach the queries that see them, and no others.
+ *   zero row, one whose scores are all minus infinity NaN.  Infinities and NaN in keys and values reach the queries that see them, and no others.
  *   out [M, H, 128] FP16 contiguous; workspace as above, of qoq_attention_prefill_workspace_bytes(...) bytes.
  * Limits: D = 128; B <= 1048576, Hkv <= 1024, M and Mk <= 16777216, width <= 262144, pages <= 2^31 - 1, window and sinks >= 0; in decode
  * H / Hkv <= 16.  Calls whose rows, sequences and heads come to 2^24 workgroups or more are refused as QOQ_ERR_HIP (decode: B Hkv;

@@ -120,7 +120,9 @@ __device__ __forceinline__ int attending(const PrefillArgs& p, const RowTile<ROW
     return min(p.ns, max(1, (t.n + deal - 1) / deal));
 }
 
-__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }       // a row that sees nothing is zero (NaN stays)
+// What a row's sums are multiplied by.  A row in front of position 0 sees nothing and is zero.  From there on it sees a key, and its largest
+// weight is at least 1 unless all of its scores are minus infinity: its sums are zero and it is 0 / 0.
+__device__ __forceinline__ float factor(float inv, int pos) { return pos < 0 ? 0.f : inv; }
 
 // A zero weight times infinity or NaN is NaN, in rows that do not see that value.  So where a wave's results are not all finite, rows `begin` ..
 // `end` - 1 of its tile are done again, one after the other, with the keys they see and no others: 64 scores at a time, a lane each,
@@ -174,7 +176,7 @@ __device__ void redo_rows(const PrefillArgs& p, const RowTile<ROWS, BN>& t, int 
                 }
             }
         for (int step = 32; step; step >>= 1) sum += __shfl_xor(sum, step, 64);
-        const float inv = inverse(sum);
+        const float inv = factor(1.f / sum, pos);
         const h2 pair = {(_Float16)(o0 * inv), (_Float16)(o1 * inv)};
         reinterpret_cast<uint32_t*>(p.out + ((int64_t)(t.q0 + query) * p.H + hk * p.r + head) * kD)[lane] = __builtin_bit_cast(uint32_t, pair);
     }
@@ -186,6 +188,7 @@ __device__ __forceinline__ void write_out(const PrefillArgs& p, const RowTile<RO
 {
     int query, head;
     t.row(p, x, query, head);
+    inv = factor(inv, t.Tk - t.Tq + query);
     const h2 a = {(_Float16)(num.x * inv), (_Float16)(num.y * inv)}, c = {(_Float16)(num.z * inv), (_Float16)(num.w * inv)};
     *reinterpret_cast<uint2*>(p.out + ((int64_t)(t.q0 + query) * p.H + hk * p.r + head) * kD + d) =
         make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
@@ -427,7 +430,7 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
         return;
     }
     // rows leave through LDS, 16 bytes a lane and whole rows of 256 (8 bytes a lane of 64 rows' pieces otherwise)
-    const float inv = inverse(total);
+    const float inv = factor(1.f / total, pos);
     uint8_t* own = reinterpret_cast<uint8_t*>(&s_tiles[0][0][0]) + wave * 32 * kRowPitch;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -607,7 +610,7 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
             *reinterpret_cast<float4*>(part + row * kPart + d) = num;
             if (d == 0) *reinterpret_cast<float4*>(part + row * kPart + kD) = make_float4(most, sum, redo ? 1.f : 0.f, 0.f);
         } else if (!redo) {
-            write_out(p, t, hk, row, d, num, inverse(sum));
+            write_out(p, t, hk, row, d, num, 1.f / sum);
         }
     }
     // (a wave's `odd` stands at all of its rows, so every thread that has a row knows)
@@ -656,7 +659,7 @@ __global__ __launch_bounds__(kPrefillThreads) void prefill_combine_kernel(Prefil
                 redo |= ml[s].z != 0.f;
             }
     }
-    if (there && !redo) write_out(p, t, hk, row, d, num, inverse(sum));
+    if (there && !redo) write_out(p, t, hk, row, d, num, 1.f / sum);
     if (__builtin_amdgcn_ballot_w64(there && redo) != 0) redo_rows(p, t, hk, blockIdx.y * 8 + wave * 2, blockIdx.y * 8 + wave * 2 + 2, lane);
 }
 

@@ -964,3 +964,24 @@ def test_prefill_of_a_million_light_tokens():
         got = api.attention_prefill(q, k, v, _ints([0, 1]), _ints([0, n]), workspace=room).double().cpu().numpy()
         tol = 2.0 ** -11 * ref + (2 * 2.0 ** -11 + 2 * e + 2.0 ** -20 + 2 * tiles * 2.0 ** -24) * ref + n * 2.0 ** -32 * 0.5
         assert (np.abs(got - ref) <= tol).all(), (float(np.abs(got - ref).max()), tol)
+
+
+@pytest.mark.parametrize("new,held", [(40, 0), (5, 4000), (700, 4100)])
+def test_prefill_of_queries_whose_scores_are_all_minus_infinity(new, held):
+    """Keys with an infinity that a query turns into a score of minus infinity have no weight; where it sees nothing else, the softmax is
+    0 / 0 and its row NaN, and not that of a query that sees nothing."""
+    H, Hkv, T = 2, 1, new + held
+    q, k, v, _, _ = _prompts([new], [held], H, Hkv, 121)
+    q[:, :, 3] = torch.where(torch.arange(new, device=DEV)[:, None] % 2 == 0, -1.0, 1.0)
+    some = 7                                                               # queries up to this one see nothing but such keys
+    k[:held + some + 1, 0, 3] = float("inf")
+    ws = api.new_workspace(api.attention_prefill_workspace_bytes(new, T, 1, H, Hkv), DEV)
+    for window, sinks in ((0, 0), (5, 2)):
+        for room in (ws, None):
+            got = api.attention_prefill(q, k, v, _ints([0, new]), _ints([0, T]), window=window, sinks=sinks, workspace=room).cpu().numpy()
+            # (even rows: minus infinity; odd ones: infinity, NaN as soon as one is seen)
+            assert np.isnan(got[:min(some + 1, new)]).all(), (window, room is None)
+    qs, ks = q.clone(), k.clone()
+    qs[:, :, 3], cu_q, cu_k = -1.0, [0, 3, new], [0, 0, T]                 # and three queries of a sequence without tokens
+    out = api.attention_prefill(qs, ks, v, _ints(cu_q), _ints(cu_k))
+    assert not out[:3].any() and bool(torch.isnan(out[3:3 + max(some + 1 - 3, 0)]).all())
