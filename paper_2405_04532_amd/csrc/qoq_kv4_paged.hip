@@ -135,8 +135,8 @@ struct Turn {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const double a = x[2 * e], b = x[2 * e + 1];
-                y[2 * e] = fma(a, c[e], -(b * s[e]));
-                y[2 * e + 1] = fma(b, c[e], a * s[e]);
+                y[2 * e] = turned ? fma(a, c[e], -(b * s[e])) : a;         // (0 times a neighbour's infinity is no zero)
+                y[2 * e + 1] = turned ? fma(b, c[e], a * s[e]) : b;
             }
         } else {
             uint32_t pw[4];

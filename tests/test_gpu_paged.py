@@ -985,3 +985,18 @@ def test_prefill_of_queries_whose_scores_are_all_minus_infinity(new, held):
     qs[:, :, 3], cu_q, cu_k = -1.0, [0, 3, new], [0, 0, T]                 # and three queries of a sequence without tokens
     out = api.attention_prefill(qs, ks, v, _ints(cu_q), _ints(cu_k))
     assert not out[:3].any() and bool(torch.isnan(out[3:3 + max(some + 1 - 3, 0)]).all())
+
+
+@pytest.mark.parametrize("near", [False, True])
+def test_infinities_outside_the_turned_part_stay_where_they_are(near):
+    """A norm divides a head with an infinity by infinity: NaN there and, among the elements that are not turned, zeros beside it."""
+    M, H, rot = 5, 2, 32
+    q, kv = _heads(M, H, 25), torch.zeros(M, 1, D, dtype=torch.float16, device=DEV)
+    q[1, 0, 70], q[2, 1, 101], q[3, 0, 5], q[3, 1, 32] = float("inf"), -float("inf"), float("inf"), float("inf")
+    gamma, angles = 1 + 0.1 * _heads(1, 1, 26)[0, 0], api.rope_angles(M, rot, device=DEV)
+    pool, table = api.kv4_new_pool(1, 1, DEV), _ints([[0]])
+    for g in (gamma, None):
+        out, _ = api.qk_rope_kv4_append(q, kv, kv, pool, table, _ints([0, M]), None, angles, q_gamma=g, interleaved=near)
+        with np.errstate(invalid="ignore"):
+            want = paged.turn_heads(q.cpu().numpy(), None if g is None else g.cpu().numpy(), 1e-6, angles.cpu().numpy(), np.arange(M), near)
+        assert np.array_equal(out.cpu().numpy(), want, equal_nan=True)
