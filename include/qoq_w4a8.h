@@ -298,7 +298,8 @@ int qoq_kv4_unpack(const void* cache, int64_t B, int64_t Hkv, int64_t S_max, int
  *              once with qoq_gemm_workspace_prepare, as for qoq_w4a8_gemm, whose workspace may be the same one: calls of both kinds
  *              and any shapes may take turns in it on one stream; calls that overlap in time need workspaces of their own.
  *              Without one, a sequence is not shared by several workgroups.  The sums are the same ones in every call on the
- *              same inputs, whichever workgroup ends last.
+ *              same inputs, whichever workgroup ends last.  The bytes neither grow nor fall with the batch; no shape needs more
+ *              than 4587520, and none of prompt attention's more than 34865152, so that one workspace of those serves every call.
  * qoq_attention_prefill: causal attention over FP16 keys and values; a sequence's Tq queries (cu_q, M rows) are the last of its Tk
  *   tokens (cu_k, Mk rows): query i has position p = Tk - Tq + i and sees t <= p with  t > p - window  or  t < sinks  (window = 0: all);
  *     out[i, h] = softmax_t(q[i, h] . k[t, h / r] / sqrt(128)) v[t, h / r],  r = H / Hkv <= 64

@@ -341,6 +341,7 @@ def kv4_unpack(cache, B, Hkv, S_max, D=128):
 # The KV4 cache in pages of a pool, and attention over prompts
 # ---------------------------------------------------------------------------------------
 KV4_PAGE = 64                     # tokens of a page
+ATTENTION_WORKSPACE_MAX = 34865152    # bytes that no call of paged decode or prompt attention exceeds, whatever its shape
 
 
 def kv4_pool_bytes(pages, Hkv, D=128):
@@ -383,6 +384,7 @@ def kv4_paged_gather(pool, block_table, cu, starts, rows, Hkv, k_out=None, v_out
 
 
 def kv4_paged_attention_workspace_bytes(B, H, Hkv, width, window=0, sinks=0, D=128):
+    """Bytes of this shape's call, 0 if it needs none; not monotone in the batch, at most ATTENTION_WORKSPACE_MAX for any shape."""
     return int(lib().qoq_kv4_paged_attention_workspace_bytes(B, H, Hkv, D, width, window, sinks))
 
 
@@ -394,6 +396,7 @@ def kv4_paged_attention_decode(q, pool, block_table, seq_lens, Hkv, window=0, si
 
 
 def attention_prefill_workspace_bytes(M, Mk, B, H, Hkv, window=0, sinks=0, D=128):
+    """Bytes of this shape's call, 0 if it needs none; not monotone in the rows, at most ATTENTION_WORKSPACE_MAX for any shape."""
     return int(lib().qoq_attention_prefill_workspace_bytes(M, Mk, B, H, Hkv, D, window, sinks))
 
 

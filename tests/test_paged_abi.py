@@ -1,5 +1,8 @@
 """Refusals of the paged calls, on the CPU: nothing here reaches a device."""
 import ctypes
+import math
+import os
+import random
 
 import pytest
 import torch
@@ -112,3 +115,22 @@ def test_angles():
     i, pos = torch.arange(32, dtype=torch.float64), 69
     want = pos * 500000.0 ** (-2 * i / 64)
     assert bool(((t[pos, :32] - want.cos()).abs() <= 2 ** -24).all()) and bool(((t[pos, 32:] - want.sin()).abs() <= 2 ** -24).all())
+
+
+def test_one_workspace_serves_every_shape(L):
+    """The bytes of a call are not monotone in its sizes (a larger batch may need none), but bounded: for any shape by what the header and the
+    binding state, and there are shapes that need just that."""
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "qoq_w4a8.h")).read()
+    most = {"decode": 0, "prompt": 0}
+    rng = random.Random(1)
+    log = lambda hi: int(2 ** rng.uniform(0, math.log2(hi + 1)))           # noqa: E731
+    for _ in range(20000):
+        Hkv, window, sinks = log(1024), rng.choice((0, log(1 << 20))), log(100)
+        most["decode"] = max(most["decode"], api.kv4_paged_attention_workspace_bytes(log(1 << 20), Hkv * rng.randint(1, 16), Hkv, log(1 << 18), window, sinks))
+        most["prompt"] = max(most["prompt"], api.attention_prefill_workspace_bytes(log(1 << 24), log(1 << 24), log(2000), Hkv * rng.randint(1, 64), Hkv, window, sinks))
+    full = {"decode": api.kv4_paged_attention_workspace_bytes(128, 32, 2, 1 << 18),
+            "prompt": api.attention_prefill_workspace_bytes(12, 14000000, 4, 784, 16, 30000, 1)}
+    assert full == {"decode": 4587520, "prompt": api.ATTENTION_WORKSPACE_MAX}
+    assert all(most[x] <= full[x] and str(full[x]) in text for x in full)
+    # a batch that needs none, and one of its parts that does
+    assert api.kv4_paged_attention_workspace_bytes(128, 32, 8, 128) == 0 < api.kv4_paged_attention_workspace_bytes(16, 32, 8, 128)
