@@ -1000,3 +1000,24 @@ def test_infinities_outside_the_turned_part_stay_where_they_are(near):
         with np.errstate(invalid="ignore"):
             want = paged.turn_heads(q.cpu().numpy(), None if g is None else g.cpu().numpy(), 1e-6, angles.cpu().numpy(), np.arange(M), near)
         assert np.array_equal(out.cpu().numpy(), want, equal_nan=True)
+
+
+@pytest.mark.parametrize("empty", [62, 63, 64, 65, 300])
+def test_long_runs_of_empty_sequences(empty):
+    """More sequences without rows between two neighbouring rows than a wave has lanes; in front of the first row and behind the last."""
+    new = [0] * empty + [1] + [0] * empty + [1, 1] + [0] * (2 * empty) + [2, 0, 1] + [0] * empty + [9] + [0] * empty
+    B, M = len(new), sum(new)
+    starts, held = [(17 * b) % 50 for b in range(B)], [(5 * b) % 3 for b in range(B)]
+    cu = np.concatenate(([0], np.cumsum(new)))
+    table, pages = _tables([64] * B, 1, 9)
+    q, k, v = _heads(M, 4, 131), _heads(M, 2, 132), _heads(M, 2, 133, 4)
+    angles = api.rope_angles(64, device=DEV)
+    pool = api.kv4_new_pool(pages, 2, DEV)
+    qo, ko = api.qk_rope_kv4_append(q, k, v, pool, table, _ints(cu), _ints(starts), angles, want_k=True)
+    seq, pos = paged.rows_of(cu, starts, M)
+    want_k = paged.turn_heads(k.cpu().numpy(), None, 0, angles.cpu().numpy(), pos, False)
+    assert _same(qo, paged.turn_heads(q.cpu().numpy(), None, 0, angles.cpu().numpy(), pos, False)) and _same(ko, want_k)
+    gk, gv = api.kv4_paged_gather(pool, table, _ints(cu), _ints(starts), M, 2)
+    assert _same(gk, paged.quantized(want_k).astype(np.float16)) and _same(gv, paged.quantized(v.cpu().numpy()).astype(np.float16))
+    q, k, v, cu_q, cu_k = _prompts(new, held, 4, 2, 135)
+    _check_prefill(api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k)), q, k, v, cu_q, cu_k, 0, 0)
