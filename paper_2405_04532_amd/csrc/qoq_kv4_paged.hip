@@ -351,15 +351,15 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(const uint8_t* __rest
 // products on the matrix cores, codes unpacked in registers, softmax in place; but the weights' reference follows the values' scales too.
 //
 // What a sequence's query sees is a list of chunks: those of the sinks, then those of the window (without a window all of them).
-// `ns` workgroups stand by for each (sequence, KV head); nwg of them attend, as many as give each wave at least `deal` chunks, and
-// their waves take the chunks in turn.  Unnormalised sums, references and weight sums meet in the workspace; the last workgroup to
+// `ns` workgroups stand by for each (sequence, KV head); nwg of them attend, as few as leave each wave `deal` chunks
+// at most (all of them if that is not enough), and their waves take the chunks in turn.  Unnormalised sums, references and weight sums meet in the workspace; the last workgroup to
 // arrive adds them up, in the order of the workgroups whichever arrives when, and leaves the counter at zero.
 //
 // The second product's operand is weight x value scale in FP16: off by 2^-11 of itself, or by 2^-39 of the largest weight x scale where that is
 // more (a lane's largest weight times its largest scale, of four or eight tokens at a time).
 //
-// Bound by memory where there are pairs enough, 64 x 1024 tokens of 32 heads 38.6 us (5.5 TB/s); else by the trips to memory one after the
-// other: table, page, a wave's chunks, and the join's (parts out, counter, parts in: about 4 us); 8192 tokens of 8 KV heads 10.6 us, 40 tokens 3.9.
+// Bound by memory where there are pairs enough, 64 x 1024 tokens of 32 heads 39 us (5.4 TB/s); else by the trips to memory one after the
+// other: table, page, a wave's chunks, and the join's (parts out, counter, parts in: about 4 us); 8192 tokens of 8 KV heads 10.7 us, 40 tokens 4.0.
 // ------------------------------------------------------------------------------------------
 constexpr int kPartial = kD + 4;                         // floats per head: 128 sums, their reference, the weight sum (rows of 16 bytes)
 constexpr int kChunk = 32;                               // tokens per chunk: two tiles of 16 (divides the page)
@@ -832,7 +832,9 @@ hipError_t launch_paged_gather(const uint8_t* pool, int64_t pages, const int32_t
 }
 
 // Workgroups that stand by for each (sequence, KV head), and the tokens that a query can see at most.  Two for each compute unit: with three
-// 37 x 700 tokens of 64 / 8 heads 12.3 us, 9.9 with two, 4 x 8192 of 32 / 8 14.0 and 13.3, 16 x 32000 through a window of 4096 19.4 and 18.9.
+// 37 x 700 tokens of 64 / 8 heads 12.3 us, 9.9 with two (its 296 pairs then have one each), 4 x 8192 of 32 / 8 14.0 and 13.3, 16 x 32000 through a window of 4096 19.4 and 18.9.
+// Lengths are not known here: this rule, and whether codes pass by the caches below, go by the table's width or the window.  Tables of 512 pages a sequence where 5 are
+// used were no slower: 8 x 300 of 64 / 8 heads 5.9 us with either, 64 x 300 of 32 heads 21.3 and 23.1, 4 x 4000 of 32 / 8 11.6 and 11.8.
 static int64_t most_seen(int64_t width, int64_t window, int64_t sinks)
 {
     const int64_t S = width * kPageTokens;

@@ -15,8 +15,9 @@
 // 2^kSlack, so that the sums' 64 registers are rarely rescaled: the largest weight is between 2^7 and 2^15, and each is off by 2^-11 of
 // itself or, below FP16's normal numbers, by 2^-25, which is 2^-32 of the largest at most.  (Without the lead the second bound is 2^-25; times were level,
 // 3 x 4001 520 to 521 us, 256 alone 8.55 and 8.65.)
-// Bound by the matrix cores on large batches, 3 x 4001 tokens of 64 / 8 heads 502 us, 947 TFLOP/s (a large product of the library's: 1145), two
-// workgroups to a compute unit; by a workgroup's own chain of key tiles on short ones, 1024 tokens of 32 heads 25 us: 3.7 to the
+// Large batches, 3 x 4001 tokens of 64 / 8 heads 510 us, 933 TFLOP/s (a large product of the library's: 1145), two workgroups to a compute unit, are
+// bound by instructions: of the cycles matrix instructions take 55% and vector ones 47%, hardly at once, and the clock falls to
+// 1.7 GHz under them (2.3 on one short prompt).  Short ones are bound by a workgroup's own chain of key tiles, 1024 tokens of 32 heads 25 us: 3.7 to the
 // first tile, then 1.2 to 1.4 for each of the last rows' 16.  A ring of four tiles was no faster (31), nor are weights spread over both products (27.5).
 #include <algorithm>
 #include <type_traits>
