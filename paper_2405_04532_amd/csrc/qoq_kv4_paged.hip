@@ -568,9 +568,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
             }
         }
         // the largest scale is below 2^(its exponent's bits - 14), so with this reference weight x scale stays below 2^15
-        const float exponent = (float)((largest.x >> 10) & 31u);
+        // (where FP32 no longer holds a score's units, the sum would be rounded by more than there is room: the score itself)
+        const float below = fabsf(top) < 0x1p23f ? (float)((largest.x >> 10) & 31u) - 29.f : 0.f;
         // the four k-blocks of a column agree on the reference
-        const float m_new = max_other_half(max_other_row(fmaxf(m, top + (exponent - 29.f))));
+        const float m_new = max_other_half(max_other_row(fmaxf(m, top + below)));
         if (__builtin_amdgcn_ballot_w64(m_new != m) != 0) {                  // rare once a few chunks have been seen
             const float alpha = __builtin_amdgcn_exp2f(m - m_new);
             m = m_new;

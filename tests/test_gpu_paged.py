@@ -1021,3 +1021,29 @@ def test_long_runs_of_empty_sequences(empty):
     assert _same(gk, paged.quantized(want_k).astype(np.float16)) and _same(gv, paged.quantized(v.cpu().numpy()).astype(np.float16))
     q, k, v, cu_q, cu_k = _prompts(new, held, 4, 2, 135)
     _check_prefill(api.attention_prefill(q, k, v, _ints(cu_q), _ints(cu_k)), q, k, v, cu_q, cu_k, 0, 0)
+
+
+@pytest.mark.parametrize("H,Hkv", [(2, 2), (8, 1), (16, 1)])
+@pytest.mark.parametrize("size", [300.0, 1000.0, 2000.0, 2400.0, 3300.0, 4100.0, 9000.0, 30000.0])
+def test_decode_of_the_largest_scores(H, Hkv, size):
+    """Scores up to 10^10, far past where FP32 holds their units: one token ahead of all others is alone in the result, and tokens of
+    one score share it evenly.  (Equal scores are the same sums and so the same numbers; a product and the result are rounded.)"""
+    lens, width = [40, 333, 1500, 64], 24
+    g = torch.Generator().manual_seed(int(size) + H)
+    n, sign = sum(lens), torch.where(torch.rand(Hkv, D, generator=g) < 0.5, -1.0, 1.0)
+    q = (size * sign).repeat_interleave(H // Hkv, 0)[None].repeat(4, 1, 1)
+    k = (-size * sign)[None].repeat(n, 1, 1)
+    v = torch.randn(n, Hkv, D, generator=g) * torch.exp2(3 * torch.rand(n, Hkv, 1, generator=g))
+    cu = np.concatenate(([0], np.cumsum(lens)))
+    ahead = [39, 7, 1000, None]                                            # in each sequence; in the last one all are alike
+    for b, t in enumerate(ahead):
+        if t is not None:
+            k[cu[b] + t] *= -1
+    pool, table, cu, _, vh = _chosen(lens, k.half().to(DEV), v.half().to(DEV), width, 57)
+    ws = api.new_workspace(api.kv4_paged_attention_workspace_bytes(4, H, Hkv, width), DEV)
+    for room in (ws, None):
+        got = api.kv4_paged_attention_decode(q.half().to(DEV), pool, table, _ints(lens), Hkv, workspace=room).cpu().numpy().astype(np.float64)
+        for b, t in enumerate(ahead):
+            vb = np.repeat(vh[cu[b]:cu[b + 1]], H // Hkv, axis=1)
+            ref, spread = (vb[t], np.abs(vb[t])) if t is not None else (vb.mean(axis=0), np.abs(vb).mean(axis=0))
+            assert (np.abs(got[b] - ref) <= 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2.0 ** -20) * spread + 2.0 ** -25).all(), b
