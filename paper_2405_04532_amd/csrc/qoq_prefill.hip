@@ -11,8 +11,8 @@
 //   O[d][row]   += sum_key v[key][d] p[key][row]       p's registers are the operand as they stand: the order of the keys in
 //                                                       the sum is free, and v is read transposed from LDS in that order
 // Softmax in base 2, FP32; the weights are rounded to FP16 for the second product, sums stay FP32.  They are taken relative to a reference
-// that lies 2^kLead below a row's largest score when it is set, and is raised only when a score passes it by more than another
-// 2^kSlack, so that the sums' 64 registers are rarely rescaled: the largest weight is between 2^7 and 2^15, and each is off by 2^-11 of
+// that lies 2^7 (kLead) below a row's largest score when it is set, and is raised only when a score passes it by more than another
+// 2^8 (kSlack), so that the sums' 64 registers are rarely rescaled: the largest weight is between 2^7 and 2^15, and each is off by 2^-11 of
 // itself or, below FP16's normal numbers, by 2^-25, which is 2^-32 of the largest at most.  (Without the lead the second bound is 2^-25; times were level,
 // 3 x 4001 520 to 521 us, 256 alone 8.55 and 8.65.)
 // Large batches, 3 x 4001 tokens of 64 / 8 heads 510 us, 933 TFLOP/s (a large product of the library's: 1145), two workgroups to a compute unit, are
@@ -125,9 +125,10 @@ __device__ __forceinline__ int attending(const PrefillArgs& p, const RowTile<ROW
 // weight is at least 1 unless all of its scores are minus infinity: its sums are zero and it is 0 / 0.
 __device__ __forceinline__ float factor(float inv, int pos) { return pos < 0 ? 0.f : inv; }
 
-// A zero weight times infinity or NaN is NaN, in rows that do not see that value.  So where a wave's results are not all finite, rows `begin` ..
-// `end` - 1 of its tile are done again, one after the other, with the keys they see and no others: 64 scores at a time, a lane each,
-// then two elements of the values a lane.  (Slow: for inputs that are broken already.)
+// A zero weight times infinity or NaN is NaN, in rows that do not see that value, and scores past 2^24 can leave a row without weights.  So
+// where a wave's results are not all finite, or a row's weights are gone, rows `begin` .. `end` - 1 of its tile are done again, one after the
+// other, with the keys they see and no others: 64 scores at a time, a lane each, then two elements of the values a lane.  (Slow: for inputs
+// that are broken already, or next to it.)
 template <int ROWS, int BN>
 __device__ void redo_rows(const PrefillArgs& p, const RowTile<ROWS, BN>& t, int hk, int begin, int end, int lane)
 {
@@ -195,10 +196,12 @@ __device__ __forceinline__ void write_out(const PrefillArgs& p, const RowTile<RO
         make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
 }
 
-// whether some row of the wave has a sum that is not finite
-__device__ __forceinline__ bool not_finite(const f16v (&acc)[4], bool there)
+// Whether some row of the wave has to be done again: a sum is not finite, or the weights' is small although a score was seen (it is 2^7 at
+// least but for rounding).  The product of the reference and kScale is rounded, which is a factor that a row's weights have in common; past
+// 2^24 it is not small, and they can overflow or vanish.
+__device__ __forceinline__ bool to_redo(const f16v (&acc)[4], float m, float total, bool there)
 {
-    float bad = 0.f;
+    float bad = total < 0x1p-14f && m > -1e29f ? __builtin_nanf("") : 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -412,13 +415,13 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
         if (it + 1 < n) turn(it + 1, sb, sa);
     }
     __syncthreads();                                                       // everyone has left the tiles
-    const bool odd = not_finite(acc, there);
+    float total = (l[0] + l[1]) + (l[2] + l[3]);
+    total += __shfl_xor(total, 32, 64);
+    const bool odd = to_redo(acc, m, total, there);
     if (odd && nwg == 1) {
         redo_rows(p, t, hk, wave * 32, wave * 32 + 32, lane);
         return;
     }
-    float total = (l[0] + l[1]) + (l[2] + l[3]);
-    total += __shfl_xor(total, 32, 64);
     if (nwg > 1) {                                                         // to be added up by the second launch
         if (!there) return;
         float* mine = p.parts + ((((size_t)slot * p.Hkv + hk) * p.ns + split) * kBM + wave * 32 + col) * kPart;
@@ -575,7 +578,7 @@ __global__ __launch_bounds__(kPrefillThreads) __attribute__((amdgpu_waves_per_eu
     // ---- the waves meet ----
     float total = (l[0] + l[1]) + (l[2] + l[3]);
     total += __shfl_xor(total, 32, 64);
-    const bool odd = not_finite(acc, there);
+    const bool odd = to_redo(acc, m, total, there);
     float* own = reinterpret_cast<float*>(&s_ring[wave][0][0]) + col * kPart;
 #pragma unroll
     for (int d = 0; d < 4; ++d)

@@ -1047,3 +1047,24 @@ def test_decode_of_the_largest_scores(H, Hkv, size):
             vb = np.repeat(vh[cu[b]:cu[b + 1]], H // Hkv, axis=1)
             ref, spread = (vb[t], np.abs(vb[t])) if t is not None else (vb.mean(axis=0), np.abs(vb).mean(axis=0))
             assert (np.abs(got[b] - ref) <= 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2.0 ** -20) * spread + 2.0 ** -25).all(), b
+
+
+@pytest.mark.parametrize("H,Hkv,T", [(2, 1, 100), (8, 2, 900), (4, 4, 1300)])
+@pytest.mark.parametrize("size", [300.0, 1000.0, 2000.0, 2400.0, 3300.0, 4100.0, 9000.0, 30000.0])
+def test_prefill_of_the_largest_scores(H, Hkv, T, size):
+    """The same of prompts: queries in front of a token that is ahead see tokens of one score, those behind it that token alone."""
+    g = torch.Generator().manual_seed(int(size) + T)
+    sign = torch.where(torch.rand(Hkv, D, generator=g) < 0.5, -1.0, 1.0)
+    q = (size * sign).repeat_interleave(H // Hkv, 0)[None].repeat(T, 1, 1).half().to(DEV)
+    k, at = (-size * sign)[None].repeat(T, 1, 1), T // 2 + 3
+    k[at] *= -1
+    v = (torch.randn(T, Hkv, D, generator=g) * torch.exp2(3 * torch.rand(T, Hkv, 1, generator=g))).half().to(DEV)
+    vd = v.cpu().numpy().astype(np.float64)
+    steps = np.arange(1, T + 1)[:, None, None]
+    ref, spread = np.cumsum(vd, axis=0) / steps, np.cumsum(np.abs(vd), axis=0) / steps
+    ref[at:], spread[at:] = vd[at], np.abs(vd[at])
+    ref, spread = np.repeat(ref, H // Hkv, axis=1), np.repeat(spread, H // Hkv, axis=1)
+    ws = api.new_workspace(api.attention_prefill_workspace_bytes(T, T, 1, H, Hkv), DEV)
+    for room in (ws, None):
+        got = api.attention_prefill(q, k.half().to(DEV), v, _ints([0, T]), _ints([0, T]), workspace=room).cpu().numpy().astype(np.float64)
+        assert (np.abs(got - ref) <= 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2.0 ** -20) * spread + 2.0 ** -25).all()
