@@ -293,7 +293,7 @@ int qoq_kv4_unpack(const void* cache, int64_t B, int64_t Hkv, int64_t S_max, int
  * qoq_kv4_paged_attention_decode: qoq_kv4_attention_decode over pages, q [B, H, 128] with a stride, out [B, H, 128] contiguous; of
  *   the seq_lens[b] tokens (clamped to [0, 64 width]) those t with  t >= seq_lens[b] - window  or  t < sinks  are seen; window = 0:
  *   all.  A query that sees nothing gives a zero row.  Weight times value scale is rounded to FP16 relative to the largest there is:
- *   2^-11 of itself, or 2^-39 of the largest weight times the largest scale where that is more.
+ *   2^-11 of itself, or (scores within 5e6) 2^-39 of the largest weight times the largest scale where that is more.
  *   workspace  NULL, or at least qoq_kv4_paged_attention_workspace_bytes(...) bytes (0: none is needed), 16-byte aligned, zero-filled
  *              once with qoq_gemm_workspace_prepare, as for qoq_w4a8_gemm, whose workspace may be the same one: calls of both kinds
  *              and any shapes may take turns in it on one stream; calls that overlap in time need workspaces of their own.
@@ -303,8 +303,8 @@ int qoq_kv4_unpack(const void* cache, int64_t B, int64_t Hkv, int64_t S_max, int
  * qoq_attention_prefill: causal attention over FP16 keys and values; a sequence's Tq queries (cu_q, M rows) are the last of its Tk
  *   tokens (cu_k, Mk rows): query i has position p = Tk - Tq + i and sees t <= p with  t > p - window  or  t < sinks  (window = 0: all);
  *     out[i, h] = softmax_t(q[i, h] . k[t, h / r] / sqrt(128)) v[t, h / r],  r = H / Hkv <= 64
- *   FP32 softmax and sums, weights rounded to FP16 for the second product (2^-11 of itself, or 2^-32 of the row's largest where that is
- *   more), one rounding at the end.  A query that sees nothing gives a
+ *   FP32 softmax and sums, weights rounded to FP16 for the second product (2^-11 of itself, or, scores within 5e6,
+ *   2^-32 of the row's largest where that is more), one rounding at the end.  A query that sees nothing gives a
  *   zero row, one whose scores are all minus infinity NaN.  Infinities and NaN in keys and values reach the queries that see them, and no others.
  *   out [M, H, 128] FP16 contiguous; workspace as above, of qoq_attention_prefill_workspace_bytes(...) bytes.
  * Limits: D = 128; B <= 1048576, Hkv <= 1024, M and Mk <= 16777216, width <= 262144, pages <= 2^31 - 1, window and sinks >= 0; in decode

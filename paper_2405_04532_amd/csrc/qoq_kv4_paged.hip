@@ -485,8 +485,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
 
     // of this lane's column, over the tokens it has seen: the reference that scores are taken from before they become weights, and the weights'
     // sum.  It follows the largest (score + exponent of the value's scale): weight x scale, which is rounded to FP16 for the matrix cores, then has
-    // its largest numbers below 2^15 whatever the values' size, and 29 binades lie between those and the first that loses bits.  (37 x 700 10.4 us
-    // without the scales, 10.5 with them, 64 x 4000 39.1 and 39.3, 8192 tokens 11.0 and 11.0.)
+    // its largest numbers below 2^15 whatever the values' size, and 29 binades lie between those and the first that loses bits.  (37 x 700 10.2 us
+    // without the scales, 10.5 with them, 64 x 4000 39.3 and 39.6, 8192 tokens 10.8 and 10.9.)
     float m = -1e29f, l = 0.f;
     f4 acc[8];                                           // acc[4u + j][x]: element d = 16 kb + 4x + 64u + j of the column
 #pragma unroll
