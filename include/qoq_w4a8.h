@@ -327,6 +327,60 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
                           const int32_t* cu_q, const int32_t* cu_k, int64_t M, int64_t Mk, int64_t B, int64_t H, int64_t Hkv, int64_t D,
                           int64_t window, int64_t sinks, void* out_fp16, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- A decode step of many requests ---------------------------------------------------------------------------
+ * Requests that share a long prompt, each with an adapter of its own, whose answers are scored: what such a step runs beside
+ * the calls above.
+ *
+ * qoq_kv4_shared_attention_decode: qoq_kv4_paged_attention_decode (without a window) of B sequences, of which those of a group g,
+ *   group_cu[g] .. group_cu[g + 1] - 1, share their first prefix_lens[g] tokens.  Those are read from the pages that the block table names
+ *   for the group's FIRST sequence, once for the group; the tokens behind them from each sequence's own pages.  Where the entries of a
+ *   group name the same pages in front of the prefix's end (which need not be a page's end: the page in which it ends may be the
+ *   first sequence's own, and hold other tokens' copies in the others), the result is the same as of the call without groups, but for
+ *   the order of sums.  The first sequence may itself be empty, its entries have to name the prefix's pages all the same.
+ *     group_cu     [groups + 1] INT32, device, ascending; sequences in front of the first and behind the last share nothing
+ *     prefix_lens  [groups] INT32, device, clamped to [0, 64 width]; a sequence that is shorter sees its seq_lens[b] tokens of it
+ *     groups = 0: the pointers may be NULL.  Descending or overlapping groups give unspecified results and touch nothing else.
+ *   workspace  required, qoq_kv4_shared_attention_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant on entry and exit (it may
+ *              be a GEMM workspace's part behind the counters, or any scratch); calls that overlap in time need workspaces of their own.
+ * qoq_lora_add: out[m] = base[m] + scales[a] (x[m] A_a^T) B_a^T for the rows m of adapter a, out[m] = base[m] for those of none.
+ *   base [M, N], x [M, K], out [M, N] FP16 with row strides in elements (multiples of 8), so that they may be slices of a fused projection's;
+ *   out may be base (with its stride), but not overlap base, x, a or b otherwise.  a [adapters, rank, K], b [adapters, N, rank] FP16 contiguous;
+ *   scales [adapters] FP32, or NULL: ones.  An adapter of a smaller rank is padded with zeros.  Sums are FP32; x A^T enters the
+ *   second product to 2^-22 of itself, or 2^-39 of the largest of its 64 ranks where that is more; one rounding at the end.
+ *   plan  of qoq_lora_plan for the same M and adapters: which rows are whose, worked out once and used by every projection of a step (and
+ *         by calls on other streams that are ordered behind it).  A plan of another M or number of adapters, or none: nothing is written.
+ *   workspace  required, qoq_lora_workspace_bytes(...) bytes, 16-byte aligned, zero-filled once with qoq_gemm_workspace_prepare, as for
+ *              qoq_w4a8_gemm, whose workspace may be the same one.
+ * qoq_lora_plan: row_adapter [M] INT32, device: the adapter of each row; any value outside [0, adapters) is none.  Opaque, qoq_lora_plan_bytes
+ *   bytes, 16-byte aligned.
+ * qoq_token_logprobs: per row of logits [M, V], FP16 or FP32 (dtype), with a row stride in elements (any, at least V):
+ *     logprob[m] = x[t] - log sum_j exp(x[j]),  t = tokens[m];   entropy[m] = -sum_j p_j log p_j
+ *     rank[m]    = 1 + the number of tokens in front of t in the order of the logits, equal ones by index
+ *     top_ids, top_logprobs [M, top]: the first `top` (at most 32, at most V) in that order
+ *   Sums are FP32, held relative to the row's largest.  Logits of minus infinity (a masked vocabulary) have probability 0 and logprob minus
+ *   infinity.  A token outside [0, V): logprob NaN, rank 0.  A row that holds a NaN or plus infinity, or minus infinity only: all of its
+ *   results NaN, rank 0, top_ids -1.  tokens may be NULL with logprob and rank; logprob, rank and entropy may be NULL.
+ *   workspace  NULL, or qoq_token_logprobs_workspace_bytes(...) bytes (0: none is needed), zero-filled once as above, shared in turns as above;
+ *              without one a row is not shared by several workgroups.
+ * Limits: groups <= 1048576; rank % 8 == 0, rank <= 512, N % 8 == 0, K % 8 == 0, N and K <= 4194304, adapters <= 4096, M <= 1048576 (adapters);
+ * V <= 16777216, M <= 16777216 (logits; 2^24 workgroups or more: QOQ_ERR_HIP); the rest as for the paged decode.  Errors as above. */
+typedef enum { QOQ_FP16 = 0, QOQ_FP32 = 1 } qoq_dtype;
+size_t qoq_kv4_shared_attention_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t width, int64_t groups);
+int qoq_kv4_shared_attention_decode(const void* q_fp16, int64_t q_stride, const void* pool, int64_t pages, const int32_t* block_table,
+                                    int64_t width, const int32_t* seq_lens, const int32_t* group_cu, const int32_t* prefix_lens, int64_t groups,
+                                    int64_t B, int64_t H, int64_t Hkv, int64_t D, void* out_fp16, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+size_t qoq_lora_plan_bytes(int64_t M, int64_t adapters);
+int qoq_lora_plan(const int32_t* row_adapter, int64_t M, int64_t adapters, void* plan, size_t plan_bytes, void* stream);
+size_t qoq_lora_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t rank, int64_t adapters);
+int qoq_lora_add(const void* base_fp16, int64_t base_stride, const void* x_fp16, int64_t x_stride, const void* a_fp16, const void* b_fp16,
+                 const float* scales, const void* plan, size_t plan_bytes, int64_t M, int64_t N, int64_t K, int64_t rank, int64_t adapters,
+                 void* out_fp16, int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream);
+size_t qoq_token_logprobs_workspace_bytes(int dtype, int64_t M, int64_t V, int64_t top);
+int qoq_token_logprobs(const void* logits, int dtype, int64_t stride, const int32_t* tokens, int64_t M, int64_t V, int64_t top, float* logprob,
+                       int32_t* rank, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
 /* Test/tuning hook: force the GEMM launch configuration instead of the built-in heuristic.
  * tile_m: 0 = auto; 16, 32, 64 = streaming kernel with that many tokens per tile; 65 = 64 tokens,
  * two adjacent blocks per workgroup in lockstep (N % 128 == 0; else as 64); 66 = four blocks in lockstep

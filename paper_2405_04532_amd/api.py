@@ -101,6 +101,17 @@ _SIGNATURES = {
     "qoq_attention_prefill_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 8),
     "qoq_attention_prefill": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_void_p] * 2 + [ctypes.c_int64] * 8 +
                               [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "qoq_kv4_shared_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 6),
+    "qoq_kv4_shared_attention_decode": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_void_p] * 3 + [ctypes.c_int64] * 5 +
+                                        [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "qoq_lora_plan_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 2),
+    "qoq_lora_plan": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "qoq_lora_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 5),
+    "qoq_lora_add": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64] * 2 + [ctypes.c_void_p] * 4 + [ctypes.c_size_t] + [ctypes.c_int64] * 5 +
+                     [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "qoq_token_logprobs_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int] + [ctypes.c_int64] * 3),
+    "qoq_token_logprobs": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p] + [ctypes.c_int64] * 3 +
+                           [ctypes.c_void_p] * 6 + [ctypes.c_size_t, ctypes.c_void_p]),
 }
 
 EXPORTS = tuple(_SIGNATURES)
@@ -405,6 +416,50 @@ def attention_prefill(q, k, v, cu_q, cu_k, window=0, sinks=0, out=None, workspac
     the last of its tokens.  A query sees the last `window` tokens up to its own (0: all) and the first `sinks`.  With a
     `workspace` (new_workspace of attention_prefill_workspace_bytes) several workgroups may share the keys of few queries."""
     return (_native or _load_native()).attention_prefill(q, k, v, cu_q, cu_k, window, sinks, out, workspace)
+
+
+# ---------------------------------------------------------------------------------------
+# A decode step of many requests: shared prefixes, adapters, log probabilities
+# ---------------------------------------------------------------------------------------
+def kv4_shared_attention_workspace_bytes(B, H, Hkv, width, groups, D=128):
+    return int(lib().qoq_kv4_shared_attention_workspace_bytes(B, H, Hkv, D, width, groups))
+
+
+def kv4_shared_attention_decode(q, pool, block_table, seq_lens, group_cu, prefix_lens, Hkv, out=None, workspace=None):
+    """kv4_paged_attention_decode of a batch whose sequences group_cu[g] .. group_cu[g + 1] - 1 share their first prefix_lens[g] tokens:
+    those are read once, from the pages of the group's first sequence, those behind them from each sequence's own.
+    group_cu [groups + 1], prefix_lens [groups] INT32.  The `workspace` (uint8 tensor of kv4_shared_attention_workspace_bytes, any
+    contents) is allocated if None."""
+    return (_native or _load_native()).kv4_shared_attention_decode(q, pool, block_table, seq_lens, group_cu, prefix_lens, Hkv, out, workspace)
+
+
+def lora_plan(row_adapter, adapters, out=None):
+    """The plan of lora_add for a batch: row_adapter [M] INT32 names the adapter of each row, outside [0, adapters) none.  Worked out once and
+    used for every projection of a step."""
+    return (_native or _load_native()).lora_plan(row_adapter, adapters, out)
+
+
+def lora_workspace_bytes(M, N, K, rank, adapters):
+    return int(lib().qoq_lora_workspace_bytes(M, N, K, rank, adapters))
+
+
+def lora_add(base, x, a, b, plan, scales=None, out=None, workspace=None):
+    """base + scales[i] (x a[i]^T) b[i]^T per row with its adapter i, base where it has none: base [M, N] (the shared projection's
+    output), x [M, K], a [adapters, rank, K], b [adapters, N, rank] FP16, scales [adapters] FP32 or None.  Rows may be strided; out may be
+    base.  `plan` is lora_plan's for these rows.  The `workspace` (new_workspace of lora_workspace_bytes) is made if None."""
+    return (_native or _load_native()).lora_add(base, x, a, b, plan, scales, out, workspace)
+
+
+def token_logprobs_workspace_bytes(M, V, top=0, dtype=torch.float16):
+    return int(lib().qoq_token_logprobs_workspace_bytes(int(dtype == torch.float32), M, V, top))
+
+
+def token_logprobs(logits, tokens=None, top=0, workspace=None):
+    """Of each row of logits [M, V], FP16 or FP32: log probability and rank (1: the most likely) of the token that `tokens` [M] INT32 names,
+    the entropy, and the `top` (at most 32) most likely tokens with their log probabilities, equal logits by index; returns
+    (logprob [M] FP32 | None, rank [M] INT32 | None, entropy [M] FP32, top_ids [M, top] INT32 | None, top_logprobs [M, top] FP32 | None).
+    With a `workspace` (new_workspace of token_logprobs_workspace_bytes) several workgroups may share a row."""
+    return (_native or _load_native()).token_logprobs(logits, tokens, top, workspace)
 
 
 # ---------------------------------------------------------------------------------------

@@ -549,6 +549,111 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
     return qoq::launch_prefill(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QOQ_OK : QOQ_ERR_HIP;
 }
 
+// ---- a decode step of many requests -------------------------------------------------------------------------
+static bool shared_decode_ok(int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t width, int64_t groups)
+{
+    return paged_decode_ok(B, H, Hkv, D, width, 0, 0) && groups >= 0 && groups <= (1 << 20);
+}
+
+size_t qoq_kv4_shared_attention_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t width, int64_t groups)
+{
+    return shared_decode_ok(B, H, Hkv, D, width, groups) ? qoq::shared_decode_workspace_bytes(B, H, Hkv, width, groups) : 0;
+}
+
+int qoq_kv4_shared_attention_decode(const void* q_fp16, int64_t q_stride, const void* pool, int64_t pages, const int32_t* block_table,
+                                    int64_t width, const int32_t* seq_lens, const int32_t* group_cu, const int32_t* prefix_lens, int64_t groups,
+                                    int64_t B, int64_t H, int64_t Hkv, int64_t D, void* out_fp16, void* workspace, size_t workspace_bytes,
+                                    void* stream)
+{
+    if (!paged_ok(B, Hkv, D, pages, width) || !shared_decode_ok(B, H, Hkv, D, width, groups) || !stride_ok(q_stride, H)) return QOQ_ERR_SHAPE;
+    if (B == 0) return QOQ_OK;
+    if (!q_fp16 || !pool || !block_table || !seq_lens || !out_fp16 || (groups && (!group_cu || !prefix_lens))) return QOQ_ERR_NULL;
+    if (!aligned16(q_fp16) || !aligned16(pool) || !aligned16(out_fp16) || !aligned16(workspace) || !aligned4(block_table) || !aligned4(seq_lens) ||
+        !aligned4(group_cu) || !aligned4(prefix_lens))
+        return QOQ_ERR_ALIGN;
+    if (!workspace || workspace_bytes < qoq::shared_decode_workspace_bytes(B, H, Hkv, width, groups)) return QOQ_ERR_WORKSPACE;
+    if (!arch_ok()) return QOQ_ERR_ARCH;
+    return qoq::launch_shared_decode(q_fp16, q_stride, static_cast<const uint8_t*>(pool), pages, block_table, width, seq_lens, group_cu, prefix_lens,
+                                     B, groups, H, Hkv, out_fp16, workspace, static_cast<hipStream_t>(stream)) == hipSuccess ? QOQ_OK : QOQ_ERR_HIP;
+}
+
+static bool lora_plan_ok(int64_t M, int64_t adapters) { return M >= 0 && M <= (1 << 20) && adapters > 0 && adapters <= qoq::lora_max_adapters(); }
+static bool lora_ok(int64_t M, int64_t N, int64_t K, int64_t rank, int64_t adapters)
+{
+    return lora_plan_ok(M, adapters) && N > 0 && N % 8 == 0 && N <= (1 << 22) && K > 0 && K % 8 == 0 && K <= (1 << 22) && rank > 0 &&
+           rank % 8 == 0 && rank <= 512;
+}
+
+size_t qoq_lora_plan_bytes(int64_t M, int64_t adapters) { return lora_plan_ok(M, adapters) ? qoq::lora_plan_bytes(M, adapters) : 0; }
+
+int qoq_lora_plan(const int32_t* row_adapter, int64_t M, int64_t adapters, void* plan, size_t plan_bytes, void* stream)
+{
+    if (!lora_plan_ok(M, adapters)) return QOQ_ERR_SHAPE;
+    if (!plan || (M && !row_adapter)) return QOQ_ERR_NULL;
+    if (!aligned16(plan) || !aligned4(row_adapter)) return QOQ_ERR_ALIGN;
+    if (plan_bytes < qoq::lora_plan_bytes(M, adapters)) return QOQ_ERR_WORKSPACE;
+    if (!arch_ok()) return QOQ_ERR_ARCH;
+    return qoq::launch_lora_plan(row_adapter, M, adapters, plan, static_cast<hipStream_t>(stream)) == hipSuccess ? QOQ_OK : QOQ_ERR_HIP;
+}
+
+size_t qoq_lora_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t rank, int64_t adapters)
+{
+    return lora_ok(M, N, K, rank, adapters) ? qoq::lora_workspace_bytes(M, N, K, rank, adapters) : 0;
+}
+
+int qoq_lora_add(const void* base_fp16, int64_t base_stride, const void* x_fp16, int64_t x_stride, const void* a_fp16, const void* b_fp16,
+                 const float* scales, const void* plan, size_t plan_bytes, int64_t M, int64_t N, int64_t K, int64_t rank, int64_t adapters,
+                 void* out_fp16, int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream)
+{
+    auto rows = [](int64_t stride, int64_t n) { return stride >= n && stride % 8 == 0 && stride <= (1 << 24); };
+    if (!lora_ok(M, N, K, rank, adapters) || !rows(base_stride, N) || !rows(x_stride, K) || !rows(out_stride, N)) return QOQ_ERR_SHAPE;
+    if (base_fp16 && base_fp16 == out_fp16 && base_stride != out_stride) return QOQ_ERR_SHAPE;
+    if (M == 0) return QOQ_OK;
+    if (!base_fp16 || !x_fp16 || !a_fp16 || !b_fp16 || !plan || !out_fp16) return QOQ_ERR_NULL;
+    if (!aligned16(base_fp16) || !aligned16(x_fp16) || !aligned16(a_fp16) || !aligned16(b_fp16) || !aligned16(plan) || !aligned16(out_fp16) ||
+        !aligned16(workspace) || !aligned4(scales))
+        return QOQ_ERR_ALIGN;
+    if (plan_bytes < qoq::lora_plan_bytes(M, adapters) || !workspace || workspace_bytes < qoq::lora_workspace_bytes(M, N, K, rank, adapters))
+        return QOQ_ERR_WORKSPACE;
+    if (!arch_ok()) return QOQ_ERR_ARCH;
+    qoq::LoraAdd l{};
+    l.base = base_fp16; l.x = x_fp16; l.a = a_fp16; l.b = b_fp16; l.scales = scales; l.plan = plan; l.out = out_fp16; l.workspace = workspace;
+    l.base_stride = base_stride; l.x_stride = x_stride; l.out_stride = out_stride;
+    l.M = M; l.N = N; l.K = K; l.rank = rank; l.adapters = adapters;
+    return qoq::launch_lora_add(l, static_cast<hipStream_t>(stream)) == hipSuccess ? QOQ_OK : QOQ_ERR_HIP;
+}
+
+static bool logprobs_ok(int dtype, int64_t M, int64_t V, int64_t top)
+{
+    return (dtype == QOQ_FP16 || dtype == QOQ_FP32) && rows_ok(M) && V > 0 && V <= (1 << 24) && top >= 0 && top <= 32 && top <= V;
+}
+
+size_t qoq_token_logprobs_workspace_bytes(int dtype, int64_t M, int64_t V, int64_t top)
+{
+    return logprobs_ok(dtype, M, V, top) ? qoq::logprobs_workspace_bytes(M, V, top, dtype == QOQ_FP32) : 0;
+}
+
+int qoq_token_logprobs(const void* logits, int dtype, int64_t stride, const int32_t* tokens, int64_t M, int64_t V, int64_t top, float* logprob,
+                       int32_t* rank, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!logprobs_ok(dtype, M, V, top) || stride < V || stride > ((int64_t)1 << 32)) return QOQ_ERR_SHAPE;
+    if (M == 0) return QOQ_OK;
+    if (!logits || (top && (!top_ids || !top_logprobs)) || (!tokens && (logprob || rank))) return QOQ_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(logits) % (dtype == QOQ_FP32 ? 4 : 2) || !aligned16(workspace) || !aligned4(tokens) || !aligned4(logprob) ||
+        !aligned4(rank) || !aligned4(entropy) || !aligned4(top_ids) || !aligned4(top_logprobs))
+        return QOQ_ERR_ALIGN;
+    const size_t need = qoq::logprobs_workspace_bytes(M, V, top, dtype == QOQ_FP32);
+    if (workspace && workspace_bytes < need) return QOQ_ERR_WORKSPACE;
+    if (!arch_ok()) return QOQ_ERR_ARCH;
+    qoq::TokenLogprobs a{};
+    a.logits = logits; a.wide = dtype == QOQ_FP32; a.stride = stride; a.tokens = tokens;
+    a.M = M; a.V = V; a.top = top;
+    a.logprob = logprob; a.rank = rank; a.entropy = entropy;
+    a.top_ids = top_ids; a.top_logprobs = top_logprobs;
+    a.workspace = need ? workspace : nullptr;
+    return qoq::launch_logprobs(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QOQ_OK : QOQ_ERR_HIP;
+}
+
 int qoq_w4a8_gemm(const int8_t* qx, const void* sx_fp16, const int32_t* rowsum, const void* packed, int64_t M,
                   int64_t N, int64_t K, int mode, void* out_fp16, void* workspace, size_t workspace_bytes,
                   void* stream)

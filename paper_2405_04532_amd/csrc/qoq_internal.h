@@ -117,6 +117,46 @@ struct Prefill {
 size_t prefill_workspace_bytes(int64_t M, int64_t Mk, int64_t B, int64_t H, int64_t Hkv, int64_t window, int64_t sinks);
 hipError_t launch_prefill(const Prefill& a, hipStream_t s);
 
+// qoq_kv4_shared.hip: decode attention over pages for a batch whose sequences share prefixes.
+size_t shared_decode_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t width, int64_t G);
+hipError_t launch_shared_decode(const void* q, int64_t q_stride, const uint8_t* pool, int64_t pages, const int32_t* table, int64_t width,
+                                const int32_t* seq_lens, const int32_t* group_cu, const int32_t* prefix_lens, int64_t B, int64_t G, int64_t H,
+                                int64_t Hkv, void* out, void* workspace, hipStream_t s);
+
+// qoq_lora.hip: low-rank adapters of many requests beside a projection.
+struct LoraAdd {
+    const void* base;                    // FP16 [M, N] with a row stride
+    const void* x;                       // FP16 [M, K] with a row stride
+    const void *a, *b;                   // FP16 [adapters, rank, K], [adapters, N, rank]
+    const float* scales;                 // [adapters], or null
+    const void* plan;
+    void* out;                           // may be base
+    void* workspace;
+    int64_t base_stride, x_stride, out_stride, M, N, K, rank, adapters;
+};
+int64_t lora_max_adapters();
+size_t lora_plan_bytes(int64_t M, int64_t adapters);
+hipError_t launch_lora_plan(const int32_t* row_adapter, int64_t M, int64_t adapters, void* plan, hipStream_t s);
+size_t lora_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t rank, int64_t adapters);
+hipError_t launch_lora_add(const LoraAdd& l, hipStream_t s);
+
+// qoq_logprobs.hip: log probabilities of given tokens, entropy, the most likely tokens.
+struct TokenLogprobs {
+    const void* logits;                  // FP16 or (wide) FP32 [M, V] with a row stride
+    int wide;
+    int64_t stride;
+    const int32_t* tokens;               // or null
+    int64_t M, V, top;
+    float* logprob;                      // or null
+    int32_t* rank;                       // or null
+    float* entropy;                      // or null
+    int32_t* top_ids;
+    float* top_logprobs;
+    void* workspace;                     // or null: one workgroup to a row
+};
+size_t logprobs_workspace_bytes(int64_t M, int64_t V, int64_t top, int wide);
+hipError_t launch_logprobs(const TokenLogprobs& a, hipStream_t s);
+
 // Launch configuration the library picks for a problem (also sizes the workspace).
 struct GemmTuning { int tile_m, split_k; };  // 0 = let the heuristic decide
 // eight_waves = false: a plan without those kernels, whose k-slices take more workspace, and without 48-token tiles in place of

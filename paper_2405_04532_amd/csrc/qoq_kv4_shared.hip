@@ -1,0 +1,512 @@
+// Decode attention over the paged 4-bit cache for a batch whose sequences share prefixes: one query token for each sequence,
+//   out[b, h] = softmax_t( q[b, h] . K^[t] / sqrt(D) ) V^[t],  t < L_b,
+// where tokens t < P_g of a sequence of group g lie in the pages of the group's first sequence, the others in its own.
+//
+// The columns of a matrix instruction are 16 query vectors; over a sequence's own tokens those are the heads of a KV head, over a
+// prefix the heads of all the group's sequences.  So a wave takes 16 CT columns through a chunk of 32 tokens whose codes it unpacks once: a
+// prefix is read, and unpacked, once for 16 CT / R sequences, and a workgroup for as many columns of the same KV head finds it in the L2 of its
+// chiplet (workgroups of one KV head are 8 apart where the heads are a multiple of 8).
+//
+// One launch attends, with workgroups for both kinds of work side by side, each writing unnormalised sums, references and weight sums of
+// its range of tokens; a second one joins those of each head.  The arithmetic of a chunk and the weights' reference are those of the
+// paged decode kernel (qoq_kv4_paged.hip).
+#include <algorithm>
+
+#include "qoq_gemm_common.h"
+#include "qoq_kv4_common.h"
+#include "qoq_workspace.h"
+
+namespace qoq {
+namespace {
+
+constexpr int kPartial = kD + 4;                         // floats of a part: 128 sums, their reference, the weight sum (rows of 16 bytes)
+constexpr int kChunk = 32;                               // tokens: two tiles of 16 (divides the page)
+constexpr int kWaves = 4;                                // of a workgroup
+constexpr int kMaxParts = 64;                            // of a prefix, and of a sequence's own tokens
+constexpr int kColumnTiles = 2;                          // of 16 columns for each wave, over a prefix
+constexpr int kPrefixColumns = 16 * kColumnTiles;
+
+struct SharedArgs {
+    const uint8_t* pool;
+    const int32_t *table, *seq_lens, *cu, *prefix_lens;
+    const __half* q;
+    float* parts;                                        // [B][H][prefix_parts + own_parts][kPartial]
+    __half* out;
+    int64_t q_stride;
+    uint32_t pages;
+    int width, B, G, Hkv, R, prefix_parts, own_parts;
+    uint32_t prefix_blocks;
+};
+
+typedef const __attribute__((address_space(1))) uint8_t* global_bytes;
+typedef const __attribute__((address_space(1))) u32x4* global_u32x4;
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+
+// Workgroups that attend to `chunks` chunks, of the `parts` that stand by: as few as leave each wave two, if there are that many.
+__device__ __forceinline__ int attending(int chunks, int parts) { return min(parts, (chunks + 2 * kWaves - 1) / (2 * kWaves)); }
+
+// Group of sequence b with a prefix: its prefix's tokens (0: none).  The 64 lanes look together.
+__device__ __forceinline__ int prefix_of(const SharedArgs& p, int b, int lane)
+{
+    for (int g0 = 0; g0 < p.G; g0 += 64) {
+        const int g = g0 + lane;
+        int n = 0;
+        bool in = false;
+        if (g < p.G) {
+            in = p.cu[g] <= b && b < p.cu[g + 1];
+            n = min(max(p.prefix_lens[g], 0), p.width * kPageTokens);
+        }
+        const unsigned long long who = __builtin_amdgcn_ballot_w64(in);
+        if (who) return __builtin_amdgcn_readfirstlane(__shfl(n, __builtin_ctzll(who), 64));
+    }
+    return 0;
+}
+
+struct Work {
+    const int32_t* pages_of;                             // the block table's row
+    int hk, lo, hi;                                      // KV head; tokens lo .. hi - 1
+    int part, parts;                                     // this workgroup among those that attend
+    int first, column0, columns;                         // column c is head (column0 + c) % R of sequence first + (column0 + c) / R
+    int slot;                                            // of the parts
+    int total_slots;
+};
+
+// One workgroup's range of tokens for up to 16 CT columns.  PK = 2: two tiles of tokens share the columns of a matrix instruction (at most
+// eight columns).  LIMITS: columns may end in front of `hi`, each at its sequence's length.
+template <int CT, int PK, bool LIMITS>
+__device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float* s_part)
+{
+    constexpr int NS = 2 / PK;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r16 = lane & 15, kb = lane >> 4;
+    const bool second = PK == 2 && r16 >= 8;
+    const int R = p.R;
+
+    struct Chunk {
+        uint4 kc[2];        // keys: token r16 of the tile, elements 32 kb ..
+        uint4 vc[2];        // values: this lane's 16 bytes of the tile
+        uint32_t kz[2];     // (s, z) of token r16 (zero point for unpacking)
+        uint4 ks[NS];       // (s, z) of tokens 4 kb .. 4 kb + 3 (scales of the scores this lane keeps)
+        uint4 vp[2];        // (s, z) of tokens 4 kb .. 4 kb + 3 of the values
+    };
+    uint32_t off_kc = (uint32_t)(r16 * (kD / 2) + kb * 16), off_kz = (uint32_t)(kCodeBytes + r16 * 4);
+    uint32_t off_ks = (uint32_t)(kCodeBytes + kb * 16 + (second ? 64 : 0)), off_vc = (uint32_t)(kHalfPage + lane * 16);
+    uint32_t off_vp = (uint32_t)(kHalfPage + kCodeBytes + kb * 16);
+    auto words = [](global_bytes at) __attribute__((always_inline)) { return __builtin_bit_cast(uint4, *(global_u32x4)at); };
+    auto load_chunk = [&](Chunk& c, int chunk, uint32_t id) __attribute__((always_inline)) {
+        const uint32_t held = id < p.pages ? id : 0;                     // (no page: any, and nothing of it counts)
+        const auto page = (global_bytes)(uintptr_t)to_sgpr(p.pool + ((int64_t)held * p.Hkv + k.hk) * kPageBytes);
+        const int tin = (chunk & 1) * kChunk;
+        const auto codes = page + tin * (kD / 2), prm = page + tin * 4;
+        asm("" : "+v"(off_kc), "+v"(off_kz), "+v"(off_ks), "+v"(off_vc), "+v"(off_vp));
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            c.kc[tt] = words(codes + tt * 1024 + off_kc);
+            c.kz[tt] = *(const __attribute__((address_space(1))) uint32_t*)(prm + tt * 64 + off_kz);
+            if (tt < NS) c.ks[tt] = words(prm + tt * 64 + off_ks);
+        }
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            c.vc[tt] = words(codes + tt * 1024 + off_vc);
+            c.vp[tt] = words(prm + tt * 64 + off_vp);
+        }
+    };
+
+    const int c0 = k.lo / kChunk, n = (k.hi + kChunk - 1) / kChunk - c0;   // the chunks
+    const int i0 = k.part * kWaves + wave, stride = k.parts * kWaves;
+    const int n_iter = i0 < n ? (n - i0 + stride - 1) / stride : 0;
+    auto chunk_of = [&](int it) __attribute__((always_inline)) {           // of the wave's it-th turn, or its last
+        return __builtin_amdgcn_readfirstlane(c0 + min(i0 + max(min(it, n_iter - 1), 0) * stride, n - 1));
+    };
+    auto page_of = [&](int it) __attribute__((always_inline)) { return (uint32_t)k.pages_of[chunk_of(it) >> 1]; };
+    Chunk A, Bf;
+    uint32_t id_a = page_of(0), id_b = page_of(1);
+    load_chunk(A, chunk_of(0), id_a);
+
+    // B operand of S = K q^T: a lane's column of each tile (none: zeros), k-block kb = elements 32 kb ..
+    uint4 qv[CT][4];
+    int limit[CT];
+    int least = k.hi, most = LIMITS ? 0 : k.hi;          // of the columns' limits: what lies behind all of them need not have been written
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        const int column = c * 16 + (PK == 2 ? r16 & 7 : r16), held = k.column0 + min(column, k.columns - 1), b = k.first + held / R;
+        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_stride + (int64_t)(k.hk * R + held % R) * kD + kb * 32);
+        const uint32_t some = column < k.columns ? ~0u : 0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint4 t = src[e];
+            qv[c][e] = make_uint4(t.x & some, t.y & some, t.z & some, t.w & some);
+        }
+        limit[c] = k.hi;
+        if (LIMITS) {
+            limit[c] = min(max(p.seq_lens[b], 0), k.hi);
+            least = min(least, limit[c]);
+            most = max(most, limit[c]);
+        }
+    }
+    if (LIMITS) {
+#pragma unroll
+        for (int o = 8; o; o >>= 1) {
+            least = min(least, __shfl_xor(least, o, 64));
+            most = max(most, __shfl_xor(most, o, 64));
+        }
+        least = __builtin_amdgcn_readfirstlane(least);
+        most = __builtin_amdgcn_readfirstlane(most);
+    }
+
+    // of a lane's columns, over the tokens they have seen: the reference that scores are taken from before they become weights, and the weights' sum
+    float m[CT], l[CT];
+    f4 acc[CT][8];                                       // acc[.][4u + j][x]: element d = 16 kb + 4x + 64u + j of the column
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        m[c] = -1e29f; l[c] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[c][i] = (f4){0.f, 0.f, 0.f, 0.f};
+    }
+    const float kScale = 1.4426950408889634f * 0.08838834764831845f;      // log2(e) / sqrt(128)
+    const h2 k960 = {(_Float16)960.0f, (_Float16)960.0f};
+
+    auto process = [&](Chunk& cur, int it, uint32_t id) __attribute__((always_inline)) {
+        const int chunk = chunk_of(it), t0 = chunk * kChunk;
+        // A chunk of which not every token is seen by all: parameters of tokens that none sees are whatever the cache holds and must not
+        // enter the arithmetic; what a column does not see gets a score of -1e30, whose weight is 0 against any maximum (which starts at
+        // -1e29), and a value scale of zero.
+        const bool partly = !(id < p.pages && t0 >= k.lo && t0 + kChunk <= least);
+        const int lo = k.lo, hi = id < p.pages ? most : 0;
+        if (partly) {
+            auto held = [&](int t) { return t >= lo && t < hi; };
+            auto kept = [&](uint4 v, int t, uint32_t none) {               // parameters of tokens t .. t + 3
+                return make_uint4(held(t) ? v.x : none, held(t + 1) ? v.y : none, held(t + 2) ? v.z : none, held(t + 3) ? v.w : none);
+            };
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                cur.kz[tt] = held(t0 + tt * 16 + r16) ? cur.kz[tt] : 0xE4000000u;                 // -(1024 + 0)
+                cur.vp[tt] = kept(cur.vp[tt], t0 + tt * 16 + 4 * kb, 0xE4000000u);
+            }
+        }
+        f4 d[CT][2];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            const uint32_t kz = cur.kz[tt];
+            const h2 c = __builtin_bit_cast(h2, __builtin_amdgcn_perm(kz, kz, 0x07060706u));   // high half in both halves
+            const h2 c16 = c + k960;
+            const uint32_t kw[4] = {cur.kc[tt].x, cur.kc[tt].y, cur.kc[tt].z, cur.kc[tt].w};
+#pragma unroll
+            for (int i = 0; i < CT; ++i) d[i][tt] = (f4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                h2 kh[4];
+                unpack4(kw[w], c, c16, kh);              // kh[j] = elements 8w + 2j, 8w + 2j + 1 of this lane's 32
+                const h8 k8 = join(kh[0], kh[1], kh[2], kh[3]);
+#pragma unroll
+                for (int i = 0; i < CT; ++i) d[i][tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k8, __builtin_bit_cast(h8, qv[i][w]), d[i][tt], 0, 0, 0);
+            }
+        }
+        h8 b8[CT];                                       // B operand: softmax weight * value scale, tokens 4 kb .. of both tiles
+#pragma unroll
+        for (int i = 0; i < CT; ++i) {
+            float sc[NS][4];                             // [x] = token 4 kb + x of the lane's tile (of both tiles with PK = 1)
+            uint32_t pw[NS][4];                          // parameters of the values of these tokens
+#pragma unroll
+            for (int tt = 0; tt < NS; ++tt) {
+                const uint4 a = PK == 2 && second ? cur.vp[1] : cur.vp[tt];
+                pw[tt][0] = a.x; pw[tt][1] = a.y; pw[tt][2] = a.z; pw[tt][3] = a.w;
+                const uint32_t sw[4] = {cur.ks[tt].x, cur.ks[tt].y, cur.ks[tt].z, cur.ks[tt].w};
+#pragma unroll
+                for (int x = 0; x < 4; ++x) sc[tt][x] = (PK == 2 && second ? d[i][1][x] : d[i][tt][x]) * ((float)half_of(sw[x]) * kScale);
+            }
+            if (partly) {
+                const int end = min(hi, limit[i]);
+#pragma unroll
+                for (int tt = 0; tt < NS; ++tt)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int t = t0 + (second ? 16 : 0) + tt * 16 + 4 * kb + x;
+                        if (!(t >= lo && t < end)) { sc[tt][x] = -1e30f; pw[tt][x] = 0; }
+                    }
+            }
+            float top = -1e30f;
+            us2 largest = {0, 0};
+#pragma unroll
+            for (int tt = 0; tt < NS; ++tt)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    top = fmaxf(top, sc[tt][x]);
+                    largest = __builtin_elementwise_max(largest, __builtin_bit_cast(us2, pw[tt][x]));
+                }
+            // the largest scale is below 2^(its exponent's bits - 14), so with this reference weight x scale stays below 2^15
+            // (where FP32 no longer holds a score's units, the sum would be rounded by more than there is room: the score itself)
+            const float below = fabsf(top) < 0x1p23f ? (float)((largest.x >> 10) & 31u) - 29.f : 0.f;
+            // the four k-blocks of a column agree on the reference
+            const float m_new = max_other_half(max_other_row(fmaxf(m[i], top + below)));
+            if (__builtin_amdgcn_ballot_w64(m_new != m[i]) != 0) {           // rare once a few chunks have been seen
+                const float alpha = __builtin_amdgcn_exp2f(m[i] - m_new);
+                m[i] = m_new;
+                l[i] *= alpha;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[i][e] *= alpha;
+            }
+            uint32_t bw[2][2];
+#pragma unroll
+            for (int tt = 0; tt < NS; ++tt) {
+                float wf[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const float pr = __builtin_amdgcn_exp2f(sc[tt][x] - m[i]);
+                    l[i] += pr;
+                    wf[x] = pr * (float)half_of(pw[tt][x]);
+                }
+                const uint32_t b_lo = __builtin_bit_cast(uint32_t, (h2){(_Float16)wf[0], (_Float16)wf[1]});
+                const uint32_t b_hi = __builtin_bit_cast(uint32_t, (h2){(_Float16)wf[2], (_Float16)wf[3]});
+                if (PK == 2) {                           // a column takes part with its own tile only
+                    bw[0][0] = second ? 0u : b_lo; bw[0][1] = second ? 0u : b_hi;
+                    bw[1][0] = second ? b_lo : 0u; bw[1][1] = second ? b_hi : 0u;
+                } else {
+                    bw[tt][0] = b_lo; bw[tt][1] = b_hi;
+                }
+            }
+            b8[i] = join(__builtin_bit_cast(h2, bw[0][0]), __builtin_bit_cast(h2, bw[0][1]), __builtin_bit_cast(h2, bw[1][0]), __builtin_bit_cast(h2, bw[1][1]));
+        }
+        h2 cz[2][2], cz16[2][2];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            const uint32_t zw[4] = {cur.vp[tt].x, cur.vp[tt].y, cur.vp[tt].z, cur.vp[tt].w};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                cz[tt][h] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(zw[2 * h + 1], zw[2 * h], 0x07060302u));
+                cz16[tt][h] = cz[tt][h] + k960;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {                    // (one half of the elements after the other: registers)
+            __builtin_amdgcn_sched_barrier(0);
+            h2 vh[2][2][4];                              // [tile][h][j]: (token 4 kb + 2h, + 1) of element 4 (r16 + 16 u) + j
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                const uint32_t vw[4] = {cur.vc[tt].x, cur.vc[tt].y, cur.vc[tt].z, cur.vc[tt].w};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) unpack4(vw[2 * u + h], cz[tt][h], cz16[tt][h], vh[tt][h]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const h8 v8 = join(vh[0][0][j], vh[0][1][j], vh[1][0][j], vh[1][1][j]);
+#pragma unroll
+                for (int i = 0; i < CT; ++i) acc[i][4 * u + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v8, b8[i], acc[i][4 * u + j], 0, 0, 0);
+            }
+        }
+    };
+
+    int it = 0;
+    for (; it + 2 < n_iter; it += 2) {
+        load_chunk(Bf, chunk_of(it + 1), id_b);
+        const uint32_t now = id_a;
+        id_a = page_of(it + 2);
+        process(A, it, now);
+        load_chunk(A, chunk_of(it + 2), id_a);
+        const uint32_t then = id_b;
+        id_b = page_of(it + 3);
+        process(Bf, it + 1, then);
+    }
+    if (it + 2 == n_iter) {
+        load_chunk(Bf, chunk_of(it + 1), id_b);
+        process(A, it, id_a);
+        process(Bf, it + 1, id_b);
+    } else if (n_iter > 0) {
+        process(A, it, id_a);
+    }
+
+    // ---- the partial results of the waves (and of the column halves) meet in LDS, a column tile at a time: [wave, half][16 / PK][kPartial] ----
+    constexpr int N = kWaves * PK, W = 16 / PK;
+#pragma unroll
+    for (int i = 0; i < CT; ++i) {
+        const int columns = min(k.columns - i * 16, W);
+        if (columns <= 0) break;
+        if (i) __syncthreads();
+        l[i] += __shfl_xor(l[i], 16, 64);
+        l[i] += __shfl_xor(l[i], 32, 64);
+        const int column = PK == 2 ? r16 & 7 : r16;
+        float* mine = s_part + ((wave * PK + (second ? 1 : 0)) * W + column) * kPartial;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                *reinterpret_cast<float4*>(mine + 16 * kb + 4 * x + 64 * u) = make_float4(acc[i][4 * u][x], acc[i][4 * u + 1][x], acc[i][4 * u + 2][x], acc[i][4 * u + 3][x]);
+        if (kb == 0) *reinterpret_cast<float2*>(mine + kD) = make_float2(m[i], l[i]);
+        __syncthreads();
+        for (int x = threadIdx.x; x < columns * (kD / 4); x += 64 * kWaves) {
+            const int at = x / (kD / 4), d = x % (kD / 4) * 4;
+            const float* part = s_part + at * kPartial;
+            float mm = -1e29f;
+#pragma unroll
+            for (int e = 0; e < N; ++e) mm = fmaxf(mm, part[e * W * kPartial + kD]);
+            float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+            float den = 0.f;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float2 ml = *reinterpret_cast<const float2*>(part + e * W * kPartial + kD);
+                const float4 a = *reinterpret_cast<const float4*>(part + e * W * kPartial + d);
+                const float f = __builtin_amdgcn_exp2f(ml.x - mm);
+                num.x = fmaf(a.x, f, num.x); num.y = fmaf(a.y, f, num.y); num.z = fmaf(a.z, f, num.z); num.w = fmaf(a.w, f, num.w);
+                den = fmaf(ml.y, f, den);
+            }
+            const int held = k.column0 + i * 16 + at;
+            const int64_t row = ((int64_t)(k.first + held / R) * p.Hkv + k.hk) * R + held % R;
+            float* to = p.parts + (row * k.total_slots + k.slot) * kPartial;
+            *reinterpret_cast<float4*>(to + d) = num;
+            if (d == 0) *reinterpret_cast<float4*>(to + kD) = make_float4(mm, den, 0.f, 0.f);
+        }
+    }
+}
+
+template <int PK>
+__global__ __launch_bounds__(64 * kWaves) void shared_decode_kernel(SharedArgs p)
+{
+    __shared__ __align__(16) float s_part[kWaves * 16 * kPartial];
+    const int lane = threadIdx.x & 63;
+    const int most = p.width * kPageTokens;
+    Work k{};
+    k.total_slots = p.prefix_parts + p.own_parts;
+    if (blockIdx.x < p.prefix_blocks) {
+        const uint32_t of_tile = (uint32_t)p.Hkv * p.prefix_parts, rest = blockIdx.x % of_tile;
+        int tile = blockIdx.x / of_tile;
+        k.hk = rest % p.Hkv;
+        k.part = rest / p.Hkv;
+        // the tile's group: tiles of the groups in front of each are counted 64 groups at a time
+        bool found = false;
+        for (int g0 = 0; g0 < p.G && !found; g0 += 64) {
+            const int g = g0 + lane;
+            int first = 0, columns = 0, tokens = 0;
+            if (g < p.G) {
+                first = min(max(p.cu[g], 0), p.B);
+                columns = max(min(p.cu[g + 1], p.B) - first, 0) * p.R;
+                tokens = min(max(p.prefix_lens[g], 0), most);
+            }
+            const int tiles = tokens ? (columns + kPrefixColumns - 1) / kPrefixColumns : 0;
+            int upto = tiles;
+            for (int o = 1; o < 64; o <<= 1) {
+                const int v = __shfl_up(upto, o, 64);
+                if (lane >= o) upto += v;
+            }
+            const unsigned long long who = __builtin_amdgcn_ballot_w64(upto > tile);
+            if (who) {
+                const int f = __builtin_ctzll(who);
+                const int at = tile - (__shfl(upto, f, 64) - __shfl(tiles, f, 64));
+                const int group_first = __builtin_amdgcn_readfirstlane(__shfl(first, f, 64));
+                k.hi = __builtin_amdgcn_readfirstlane(__shfl(tokens, f, 64));
+                k.columns = __builtin_amdgcn_readfirstlane(min(__shfl(columns, f, 64) - at * kPrefixColumns, kPrefixColumns));
+                k.first = group_first;
+                k.column0 = __builtin_amdgcn_readfirstlane(at * kPrefixColumns);
+                k.pages_of = p.table + (int64_t)group_first * p.width;
+                found = true;
+            } else {
+                tile -= __shfl(upto, 63, 64);
+            }
+        }
+        if (!found) return;
+        k.parts = attending((k.hi + kChunk - 1) / kChunk, p.prefix_parts);
+        if (k.part >= k.parts) return;
+        k.slot = k.part;
+        attend<kColumnTiles, 1, true>(p, k, s_part);
+    } else {
+        const uint32_t i = blockIdx.x - p.prefix_blocks, pairs = (uint32_t)p.B * p.Hkv, bh = i % pairs;
+        const int b = bh / p.Hkv;
+        k.hk = bh - b * p.Hkv;
+        k.part = i / pairs;
+        k.hi = min(max(p.seq_lens[b], 0), most);
+        k.lo = min(prefix_of(p, b, lane), k.hi);
+        if (k.lo == k.hi) return;
+        k.parts = attending((k.hi + kChunk - 1) / kChunk - k.lo / kChunk, p.own_parts);
+        if (k.part >= k.parts) return;
+        k.pages_of = p.table + (int64_t)b * p.width;
+        k.first = b;
+        k.columns = p.R;
+        k.slot = p.prefix_parts + k.part;
+        attend<1, PK, false>(p, k, s_part);
+    }
+}
+
+// The parts of a head, a wave to a head: two elements to a lane, a part's reference to a lane.
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
+{
+    const int lane = threadIdx.x & 63;
+    const int H = p.Hkv * p.R;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= (int64_t)p.B * H) return;
+    const int b = (int)(row / H);
+    const int most = p.width * kPageTokens;
+    const int P = prefix_of(p, b, lane), L = min(max(p.seq_lens[b], 0), most), lo = min(P, L);
+    const int n_prefix = P && L ? attending((P + kChunk - 1) / kChunk, p.prefix_parts) : 0;
+    const int n_own = L > lo ? attending((L + kChunk - 1) / kChunk - lo / kChunk, p.own_parts) : 0;
+    const int total = p.prefix_parts + p.own_parts, n = n_prefix + n_own;
+    const float* parts = p.parts + row * total * kPartial;
+    auto slot = [&](int i) { return i < n_prefix ? i : p.prefix_parts + i - n_prefix; };
+    float f[2], den = 0.f, top = -1e29f;
+    float2 ml[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        ml[e] = make_float2(-1e29f, 0.f);
+        if (lane + 64 * e < n) ml[e] = *reinterpret_cast<const float2*>(parts + (int64_t)slot(lane + 64 * e) * kPartial + kD);
+        top = fmaxf(top, ml[e].x);
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        f[e] = __builtin_amdgcn_exp2f(ml[e].x - top);
+        den = fmaf(ml[e].y, f[e], den);
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) den += __shfl_xor(den, o, 64);
+    float2 sum = make_float2(0.f, 0.f);
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+        const float2 a = *reinterpret_cast<const float2*>(parts + (int64_t)slot(i) * kPartial + 2 * lane);
+        const float g = __shfl(i < 64 ? f[0] : f[1], i & 63, 64);
+        sum.x = fmaf(a.x, g, sum.x); sum.y = fmaf(a.y, g, sum.y);
+    }
+    const float inv = den > 0.f ? 1.f / den : 1.f;       // nothing seen: zero, as the sums are (NaN stays)
+    reinterpret_cast<h2*>(p.out + row * kD)[lane] = (h2){(_Float16)(sum.x * inv), (_Float16)(sum.y * inv)};
+}
+
+int64_t prefix_tiles(int64_t B, int64_t G, int64_t R) { return G ? B * R / kPrefixColumns + G : 0; }
+// Workgroups that stand by for each tile of columns of a prefix and KV head, and for each sequence and KV head: two to a compute unit.
+int parts_for(int64_t items, int64_t width)
+{
+    if (items <= 0) return 0;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({kMaxParts, 512 / items, (2 * width + 2 * kWaves - 1) / (2 * kWaves)}));
+}
+
+}  // namespace
+
+size_t shared_decode_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t width, int64_t G)
+{
+    const int64_t slots = parts_for(prefix_tiles(B, G, H / Hkv) * Hkv, width) + parts_for(B * Hkv, width);
+    return (size_t)(B * H * slots) * kPartial * sizeof(float);
+}
+
+hipError_t launch_shared_decode(const void* q, int64_t q_stride, const uint8_t* pool, int64_t pages, const int32_t* table, int64_t width,
+                                const int32_t* seq_lens, const int32_t* group_cu, const int32_t* prefix_lens, int64_t B, int64_t G, int64_t H,
+                                int64_t Hkv, void* out, void* workspace, hipStream_t s)
+{
+    SharedArgs p{};
+    p.pool = pool; p.table = table; p.seq_lens = seq_lens; p.cu = group_cu; p.prefix_lens = prefix_lens;
+    p.q = static_cast<const __half*>(q); p.q_stride = q_stride;
+    p.parts = static_cast<float*>(workspace);
+    p.out = static_cast<__half*>(out);
+    p.pages = (uint32_t)pages; p.width = (int)width; p.B = (int)B; p.G = (int)G; p.Hkv = (int)Hkv; p.R = (int)(H / Hkv);
+    const int64_t tiles = prefix_tiles(B, G, p.R);
+    p.prefix_parts = parts_for(tiles * Hkv, width);
+    p.own_parts = parts_for(B * Hkv, width);
+    const int64_t prefix_blocks = tiles * Hkv * p.prefix_parts, blocks = prefix_blocks + B * Hkv * p.own_parts, joins = (B * H + 3) / 4;
+    if (blocks >= (int64_t)1 << 24 || joins >= (int64_t)1 << 24) return hipErrorInvalidValue;    // 2^32 threads
+    p.prefix_blocks = (uint32_t)prefix_blocks;
+    const int PK = p.R <= 8 ? 2 : 1;
+    auto* kernel = PK == 2 ? shared_decode_kernel<2> : shared_decode_kernel<1>;
+    kernel<<<(unsigned)blocks, 64 * kWaves, 0, s>>>(p);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    shared_join_kernel<<<(unsigned)joins, 256, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace qoq

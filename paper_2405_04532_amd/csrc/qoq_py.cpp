@@ -637,6 +637,193 @@ PyObject* attention_prefill(PyObject*, PyObject* const* a, Py_ssize_t n)    // q
     END_HANDLE_TH_ERRORS
 }
 
+// q, pool, block_table, seq_lens, group_cu, prefix_lens, Hkv, out, workspace
+PyObject* kv4_shared_attention_decode(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (!counted(n, 9)) return nullptr;
+    const at::Tensor* q = heads_tensor(a[0], "q", -1);
+    if (!q) return nullptr;
+    const int dev = q->get_device();
+    const int64_t B = q->size(0), H = q->size(1);
+    const at::Tensor* lens = dense(a[3], at::kInt, 1, "seq_lens", dev);
+    const at::Tensor* cu = lens ? dense(a[4], at::kInt, 1, "group_cu", dev) : nullptr;
+    const at::Tensor* prefix = cu ? dense(a[5], at::kInt, 1, "prefix_lens", dev) : nullptr;
+    int64_t Hkv;
+    Pool pool;
+    Scratch ws;
+    at::Tensor out, scratch;
+    if (!prefix || !have_shape(*lens, {B}, "seq_lens") || !have_shape(*cu, {prefix->numel() + 1}, "group_cu") || !integer(a[6], &Hkv) ||
+        !pool.ready(a[1], a[2], B, Hkv, dev) || !ws.ready(a[8], dev))
+        return nullptr;
+    c10::hip::HIPGuard guard(static_cast<c10::DeviceIndex>(dev));
+    const int64_t groups = prefix->numel();
+    if (!dense_or_new(a[7], *q, {B, H, 128}, "out", out)) return nullptr;
+    if (!ws.ptr) {
+        const size_t need = qoq_kv4_shared_attention_workspace_bytes(B, H, Hkv, 128, pool.width, groups);
+        if (need) {
+            scratch = new_like(*q, {(int64_t)need}, at::kByte);
+            ws.ptr = scratch.data_ptr();
+            ws.bytes = need;
+        }
+    }
+    void *s = stream_of(*q), *op = out.data_ptr();
+    const void *qp = q->data_ptr(), *pp = pool.bytes->data_ptr();
+    const int32_t *tp = static_cast<const int32_t*>(pool.table->data_ptr()), *lp = static_cast<const int32_t*>(lens->data_ptr());
+    const int32_t *cp = static_cast<const int32_t*>(cu->data_ptr()), *xp = static_cast<const int32_t*>(prefix->data_ptr());
+    const int64_t stride = token_stride(*q);
+    if (!call([&] {
+            return qoq_kv4_shared_attention_decode(qp, stride, pp, pool.pages, tp, pool.width, lp, cp, xp, groups, B, H, Hkv, 128, op, ws.ptr, ws.bytes, s);
+        }))
+        return nullptr;
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// FP16 [rows, columns] on `device`, contiguous but for the stride from row to row
+const at::Tensor* rows_tensor(PyObject* o, const char* name, int device)
+{
+    const at::Tensor* t = tensor(o, name);
+    if (!t) return nullptr;
+    if (!t->is_cuda() || t->scalar_type() != at::kHalf) {
+        PyErr_Format(PyExc_TypeError, "%s: expected a torch.float16 tensor on the GPU", name);
+        return nullptr;
+    }
+    if (!has_dims(*t, 2, name)) return nullptr;
+    if (device >= 0 && t->get_device() != device) {
+        PyErr_Format(PyExc_ValueError, "%s: expected on the GPU of the other tensors", name);
+        return nullptr;
+    }
+    if (t->stride(1) != 1 && t->size(1) > 1 && t->numel()) {
+        PyErr_Format(PyExc_ValueError, "%s: expected contiguous rows", name);
+        return nullptr;
+    }
+    return t;
+}
+int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : (t.size(1) + 7) / 8 * 8; }
+
+PyObject* lora_plan(PyObject*, PyObject* const* a, Py_ssize_t n)    // row_adapter, adapters, plan
+{
+    HANDLE_TH_ERRORS
+    if (!counted(n, 3)) return nullptr;
+    const at::Tensor* rows = dev_tensor(a[0], at::kInt, "row_adapter");
+    int64_t adapters;
+    if (!rows || !has_dims(*rows, 1, "row_adapter") || !integer(a[1], &adapters)) return nullptr;
+    const int dev = rows->get_device();
+    const int64_t M = rows->numel();
+    const size_t need = qoq_lora_plan_bytes(M, adapters);
+    if (!need) return call([] { return (int)QOQ_ERR_SHAPE; }), nullptr;
+    c10::hip::HIPGuard guard(static_cast<c10::DeviceIndex>(dev));
+    at::Tensor plan;
+    if (a[2] == Py_None) {
+        plan = new_like(*rows, {(int64_t)(need / 4)}, at::kInt);
+    } else {
+        const at::Tensor* given = dense(a[2], at::kInt, 1, "plan", dev);
+        if (!given) return nullptr;
+        plan = *given;
+    }
+    void *s = stream_of(*rows), *pp = plan.data_ptr();
+    const size_t bytes = (size_t)plan.numel() * 4;
+    const int32_t* rp = static_cast<const int32_t*>(rows->data_ptr());
+    if (!call([&] { return qoq_lora_plan(rp, M, adapters, pp, bytes, s); })) return nullptr;
+    return THPVariable_Wrap(plan);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* lora_add(PyObject*, PyObject* const* a, Py_ssize_t n)    // base, x, a, b, plan, scales, out, workspace
+{
+    HANDLE_TH_ERRORS
+    if (!counted(n, 8)) return nullptr;
+    const at::Tensor* base = rows_tensor(a[0], "base", -1);
+    if (!base) return nullptr;
+    const int dev = base->get_device();
+    const at::Tensor* x = rows_tensor(a[1], "x", dev);
+    const at::Tensor* la = x ? dense(a[2], at::kHalf, 3, "a", dev) : nullptr;
+    const at::Tensor* lb = la ? dense(a[3], at::kHalf, 3, "b", dev) : nullptr;
+    const at::Tensor* plan = lb ? dense(a[4], at::kInt, 1, "plan", dev) : nullptr;
+    const at::Tensor* scales;
+    Scratch ws;
+    if (!plan || !dense_or_none(a[5], at::kFloat, 1, "scales", dev, &scales) || !ws.ready(a[7], dev)) return nullptr;
+    const int64_t M = base->size(0), N = base->size(1), K = x->size(1), adapters = la->size(0), rank = la->size(1);
+    if (!have_shape(*x, {M, K}, "x") || !have_shape(*la, {adapters, rank, K}, "a") || !have_shape(*lb, {adapters, N, rank}, "b") ||
+        (scales && !have_shape(*scales, {adapters}, "scales")))
+        return nullptr;
+    c10::hip::HIPGuard guard(static_cast<c10::DeviceIndex>(dev));
+    at::Tensor out, scratch;
+    if (a[6] == Py_None) {
+        out = new_like(*base, {M, N}, at::kHalf);
+    } else {
+        const at::Tensor* given = rows_tensor(a[6], "out", dev);
+        if (!given || !have_shape(*given, {M, N}, "out")) return nullptr;
+        out = *given;
+    }
+    void* s = stream_of(*base);
+    if (!ws.ptr) {
+        const size_t need = qoq_lora_workspace_bytes(M, N, K, rank, adapters);
+        if (need && M) {
+            scratch = new_like(*base, {(int64_t)need}, at::kByte);
+            ws.ptr = scratch.data_ptr();
+            ws.bytes = need;
+            if (!call([&] { return qoq_gemm_workspace_prepare(ws.ptr, std::min(need, qoq::kCounterBytes), s); })) return nullptr;
+        }
+    }
+    const void *bp = base->data_ptr(), *xp = x->data_ptr(), *ap = la->data_ptr(), *lbp = lb->data_ptr(), *pp = plan->data_ptr();
+    const float* sp = scales ? static_cast<const float*>(scales->data_ptr()) : nullptr;
+    void* op = out.data_ptr();
+    const int64_t bs = row_stride(*base), xs = row_stride(*x), os = row_stride(out);
+    const size_t plan_bytes = (size_t)plan->numel() * 4;
+    if (!call([&] { return qoq_lora_add(bp, bs, xp, xs, ap, lbp, sp, pp, plan_bytes, M, N, K, rank, adapters, op, os, ws.ptr, ws.bytes, s); }))
+        return nullptr;
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n)    // logits, tokens, top, workspace
+{
+    HANDLE_TH_ERRORS
+    if (!counted(n, 4)) return nullptr;
+    const at::Tensor* x = tensor(a[0], "logits");
+    if (!x) return nullptr;
+    if (!x->is_cuda() || (x->scalar_type() != at::kHalf && x->scalar_type() != at::kFloat)) {
+        PyErr_SetString(PyExc_TypeError, "logits: expected a torch.float16 or torch.float32 tensor on the GPU");
+        return nullptr;
+    }
+    if (!has_dims(*x, 2, "logits")) return nullptr;
+    if (x->stride(1) != 1 && x->size(1) > 1 && x->numel()) {
+        PyErr_SetString(PyExc_ValueError, "logits: expected contiguous rows");
+        return nullptr;
+    }
+    const int dev = x->get_device();
+    const int64_t M = x->size(0), V = x->size(1), stride = M > 1 ? x->stride(0) : V;
+    const int dtype = x->scalar_type() == at::kFloat ? QOQ_FP32 : QOQ_FP16;
+    const at::Tensor* tokens;
+    int64_t top;
+    Scratch ws;
+    if (!dense_or_none(a[1], at::kInt, 1, "tokens", dev, &tokens) || (tokens && !have_shape(*tokens, {M}, "tokens")) || !integer(a[2], &top) ||
+        !ws.ready(a[3], dev))
+        return nullptr;
+    if (top < 0 || top > 32) return call([] { return (int)QOQ_ERR_SHAPE; }), nullptr;
+    c10::hip::HIPGuard guard(static_cast<c10::DeviceIndex>(dev));
+    at::Tensor logprob, rank, ids, tops, entropy = new_like(*x, {M}, at::kFloat);
+    if (tokens) {
+        logprob = new_like(*x, {M}, at::kFloat);
+        rank = new_like(*x, {M}, at::kInt);
+    }
+    if (top) {
+        ids = new_like(*x, {M, top}, at::kInt);
+        tops = new_like(*x, {M, top}, at::kFloat);
+    }
+    void* s = stream_of(*x);
+    auto at_or_null = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+    const void* xp = x->data_ptr();
+    const int32_t* tp = tokens ? static_cast<const int32_t*>(tokens->data_ptr()) : nullptr;
+    float *lp = static_cast<float*>(at_or_null(logprob)), *ep = static_cast<float*>(entropy.data_ptr()), *vp = static_cast<float*>(at_or_null(tops));
+    int32_t *rp = static_cast<int32_t*>(at_or_null(rank)), *ip = static_cast<int32_t*>(at_or_null(ids));
+    if (!call([&] { return qoq_token_logprobs(xp, dtype, stride, tp, M, V, top, lp, rp, ep, ip, vp, ws.ptr, ws.bytes, s); })) return nullptr;
+    return Py_BuildValue("NNNNN", Quantized::wrap(logprob), Quantized::wrap(rank), Quantized::wrap(entropy), Quantized::wrap(ids), Quantized::wrap(tops));
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject* set_raise_status(PyObject*, PyObject* f)
 {
     Py_INCREF(f);
@@ -684,6 +871,7 @@ PyObject* channel_order(PyObject*, PyObject* const* a, Py_ssize_t n)    // salie
 PyMethodDef methods[] = {FAST(quant_act), FAST(quant_act_reordered), FAST(rmsnorm_quant), FAST(silu_mul_quant), FAST(w4a8_gemm),
                          FAST(w4a8_gemm_noalloc), FAST(w4a8_gemm_token_sum), FAST(w4a8_linear), FAST(kv4_append), FAST(kv4_attention_decode), FAST(channel_order),
                          FAST(qk_rope_kv4_append), FAST(kv4_paged_gather), FAST(kv4_paged_attention_decode), FAST(attention_prefill),
+                         FAST(kv4_shared_attention_decode), FAST(lora_plan), FAST(lora_add), FAST(token_logprobs),
                          {"set_raise_status", set_raise_status, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 #undef FAST
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_qoq_py", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,700 @@
+"""Shared-prefix decode attention, adapters of many requests and log probabilities on the GPU against the float64 oracle.
+
+Attention is bounded term by term as in tests/test_gpu_paged.py, with FP32 sums of any order over the tokens:
+    |got - ref| <= 2^-11 |ref|                                     the result's rounding to FP16
+                 + (2^-11 + 2 e + 2^-20 + (L + 160) 2^-24) sum_t p_t |v_t|   weight times scale rounded, scores, exp2, FP32 sums over tokens and parts
+                 + 15 L 2^-25 + 2^-25                              the lightest tokens; FP16's smallest step
+Adapters: FP32 sums of K and of 2 r products in any order, the middle product as pairs (oracle.requests.lora), and the result's rounding.
+Log probabilities: each e^(x - r) is off by 2^-23 (the instruction) and its argument's rounding, ln 2 times 2^-24 of at most 1.45 |x - max| + 8, which
+  weighted by p gives  dT = 2^-23 + 2^-24 (1.1 E|x - max| + 6) + chain 2^-24  with a chain of additions of at most V / 64 + 100; logprob is off by dT + 2^-24
+  of itself, the entropy by dT (2 + 2 (1.45 E|x - max| + 8)) + 2^-24 of itself.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged, requests
+from paper_2405_04532_amd import api, workloads as wl
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+D, PAGE = 128, 64
+
+
+def _ints(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _heads(rows, heads, seed, values=False, gain=8.0):
+    return wl.make_kv(1, heads, rows, D, seed, DEV, gain=gain)[int(values)][0].transpose(0, 1).contiguous()
+
+
+def _same(a, b):
+    return bool(((a.view(torch.int16) == b.view(torch.int16)) | (a.isnan() & b.isnan())).all()) if a.dtype == torch.float16 else bool(
+        ((a == b) | (a.isnan() & b.isnan())).all())
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# Shared prefixes
+# ------------------------------------------------------------------------------------------------------------------
+class _Batch:
+    """Sequences with their own copies of nothing: whole pages of a prefix are shared, the page in which it ends is the first member's."""
+
+    def __init__(self, groups, lens, Hkv, seed, width=None, spare=2):
+        # groups: (first, behind the last, prefix); lens: tokens of every sequence in all
+        self.lens, self.Hkv, self.B = lens, Hkv, len(lens)
+        self.cu = [g[0] for g in groups] + [groups[-1][1]] if groups else [0]
+        self.prefix = [g[2] for g in groups]
+        first = {b: (a, p) for a, e, p in groups for b in range(a, e)}
+        reach = [max(n, first.get(b, (b, 0))[1] if first.get(b, (b, 0))[0] == b else 0) for b, n in enumerate(lens)]
+        self.width = width or max(1, max(-(-max([n] + [p for _, _, p in groups]) // PAGE) for n in reach))
+        need = []                                                              # pages of each sequence that are its own
+        for b, n in enumerate(reach):
+            a, p = first.get(b, (b, 0))
+            need.append(-(-n // PAGE) - (0 if a == b else min(p, n) // PAGE))
+        self.pages = sum(need) + spare
+        perm = torch.randperm(self.pages, generator=torch.Generator().manual_seed(seed)).to(torch.int32)
+        table, at = torch.full((self.B, self.width), -1, dtype=torch.int32), 0
+        for b, n in enumerate(reach):
+            a, p = first.get(b, (b, 0))
+            skip = 0 if a == b else min(p, n) // PAGE
+            table[b, :skip] = table[a, :skip]
+            table[b, skip:skip + need[b]] = perm[at:at + need[b]]
+            at += need[b]
+        # rows written: the first member all that it reaches, the others what lies behind the prefix
+        starts = [0 if first.get(b, (b, 0))[0] == b else min(first[b][1], n) for b, n in enumerate(lens)]
+        rows = [max(n - s, 0) for n, s in zip(reach, starts)]
+        cu = np.concatenate(([0], np.cumsum(rows)))
+        M = int(cu[-1])
+        k, v = _heads(max(M, 1), Hkv, seed), _heads(max(M, 1), Hkv, seed + 1, True)
+        self.table = table.to(DEV)
+        self.pool = torch.full((self.pages * Hkv * 8704,), 0xFF, dtype=torch.uint8, device=DEV)    # NaN parameters where nothing is written
+        api.kv4_paged_append(self.pool, k[:M].contiguous(), v[:M].contiguous(), self.table, _ints(cu.tolist()), _ints(starts))
+        kq, vq = paged.quantized(k.cpu().numpy()), paged.quantized(v.cpu().numpy())
+        held = {}                                                              # (page, token) -> row
+        for b in range(self.B):
+            for i in range(rows[b]):
+                held[paged.place(table.numpy(), self.pages, b, starts[b] + i)] = int(cu[b]) + i
+        self.rows = lambda t, b, pos: held.get(paged.place(t, self.pages, b, pos))
+        self.read = lambda b, t: (lambda row: None if row is None else (kq[row], vq[row]))(self.rows(self.table_np, b, t))
+        self.table_np = table.numpy()
+
+    def call(self, q, lens=None, groups=True, **kw):
+        cu, prefix = (self.cu, self.prefix) if groups else ([0], [])
+        return api.kv4_shared_attention_decode(q, self.pool, self.table, _ints(self.lens if lens is None else lens), _ints(cu),
+                                               _ints(prefix) if prefix else torch.empty(0, dtype=torch.int32, device=DEV), self.Hkv, **kw)
+
+    def check(self, out, q, lens=None, cu=None, prefix=None):
+        got, qd = out.cpu().numpy().astype(np.float64), q.cpu().numpy().astype(np.float64)
+        ref = requests.shared_attention(qd, self.read, self.lens if lens is None else lens, self.cu if cu is None else cu, self.prefix if prefix is None else prefix)
+        for b, (want, spread, k) in enumerate(ref):
+            L, r = len(k), q.shape[1] // self.Hkv
+            e = max([float((np.abs(k[:, h // r]) @ np.abs(qd[b, h])).max()) for h in range(q.shape[1])] if L else [0.0]) * 130 * 2.0 ** -24 / np.sqrt(128.0)
+            tol = 2.0 ** -11 * np.abs(want) + (2.0 ** -11 + 2 * e + 2.0 ** -20 + (L + 160) * 2.0 ** -24) * spread + 15 * L * 2.0 ** -25 + 2.0 ** -25
+            assert (np.abs(got[b] - want) <= tol).all(), (b, L, float((np.abs(got[b] - want) / tol).max()))
+            if L == 0:
+                assert not got[b].any()
+
+
+@pytest.mark.parametrize("H,Hkv", [(4, 4), (8, 2), (7, 1), (16, 1), (9, 1), (6, 2)])
+@pytest.mark.parametrize("prefix", [1, 31, 32, 33, 63, 64, 65, 100, 192, 250])
+def test_shared(H, Hkv, prefix):
+    lens = [prefix + n for n in (1, 5, 0, 31, 64, 200)] + [0, prefix // 2, prefix + 40]
+    s = _Batch([(0, len(lens), prefix)], lens, Hkv, 31 + H)
+    q = wl.make_queries(len(lens), H, D, 33, DEV)
+    s.check(s.call(q), q)
+
+
+@pytest.mark.parametrize("H,Hkv,groups,lens", [
+    (4, 2, [(0, 3, 70), (3, 4, 130), (4, 9, 0), (9, 12, 64)], [80, 70, 200, 131, 5, 64, 65, 1, 0, 65, 100, 64]),     # a group of one, one without a prefix
+    (8, 8, [(2, 5, 90), (5, 6, 33)], [17, 130, 100, 91, 90, 40, 300, 1]),                                             # sequences in front and behind
+    (3, 1, [(0, 70, 129)], [129 + i for i in range(70)]),                                                             # more columns than a tile, heads that do not divide it
+    (16, 1, [(0, 33, 65), (33, 40, 66)], [65 + (i * 7) % 50 for i in range(40)]),
+    (2, 2, [], [100, 0, 65]),                                                                                         # no groups at all
+    (2, 1, [(i, i + 1, i) for i in range(150)], [i + 3 for i in range(150)])])                                        # more groups than lanes
+def test_shared_groups(H, Hkv, groups, lens):
+    s = _Batch(groups, lens, Hkv, 41)
+    q = wl.make_queries(len(lens), H, D, 43, DEV)
+    s.check(s.call(q), q)
+
+
+@pytest.mark.parametrize("B,H,Hkv,prefix,own", [(3, 4, 1, 4100, 700), (40, 8, 2, 1500, 40), (2, 16, 1, 3000, 1), (12, 8, 8, 900, 300)])
+def test_shared_by_workgroups(B, H, Hkv, prefix, own):
+    """Long prefixes cut over workgroups, in a workspace of any contents; the same bits every time, in graphs too, and within the bound of
+    the call that reads every sequence by itself."""
+    lens = [prefix + own - i * own // (2 * B) for i in range(B)]
+    s = _Batch([(0, B, prefix)], lens, Hkv, 51)
+    q = wl.make_queries(B, H, D, 53, DEV)
+    need = api.kv4_shared_attention_workspace_bytes(B, H, Hkv, s.width, 1)
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV)
+    out = s.call(q, workspace=ws)
+    pick = sorted({0, 1, B // 2, B - 1})
+    got, want = out.cpu().numpy().astype(np.float64), requests.shared_attention(q.cpu().numpy().astype(np.float64)[pick],
+                                                                                lambda i, t: s.read(pick[i], t) if t >= prefix else s.read(0, t),
+                                                                                [lens[b] for b in pick], [0], [])
+    for i, b in enumerate(pick):
+        ref, spread, k = want[i]
+        e = max(float((np.abs(k[:, h // (H // Hkv)]) @ np.abs(q[b, h].cpu().numpy().astype(np.float64))).max()) for h in range(H)) * 130 * 2.0 ** -24 / np.sqrt(128.0)
+        tol = 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2 * e + 2.0 ** -20 + (len(k) + 160) * 2.0 ** -24) * spread + 15 * len(k) * 2.0 ** -25 + 2.0 ** -25
+        assert (np.abs(got[b] - ref) <= tol).all(), (b, float((np.abs(got[b] - ref) / tol).max()))
+    for _ in range(3):
+        assert _same(s.call(q, workspace=ws), out)
+    assert _same(s.call(q), out)
+    # two captured graphs that take turns in one workspace, with shorter sequences in the second
+    outs, graphs, short = [torch.zeros_like(out), torch.zeros_like(out)], [], [n // 2 for n in lens]
+    cu, pl, seqs = _ints(s.cu), _ints(s.prefix), [_ints(lens), _ints(short)]
+    want = [out, s.call(q, lens=short, workspace=ws)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for o, seq in zip(outs, seqs):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            api.kv4_shared_attention_decode(q, s.pool, s.table, seq, cu, pl, Hkv, out=o, workspace=ws)
+        graphs.append(graph)
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        for graph in graphs:
+            graph.replay()
+        assert _same(s.call(q, workspace=ws), out)
+        torch.cuda.synchronize()
+        assert _same(outs[0], want[0]) and _same(outs[1], want[1])
+    with pytest.raises(api.QoqError):
+        s.call(q, workspace=ws[:need - 16])
+
+
+def test_shared_agrees_with_the_call_without_groups():
+    """Prefixes of whole pages, which every member's table names: both calls read the same tokens."""
+    H, Hkv, lens = 8, 2, [300, 257, 256, 400, 70]
+    s = _Batch([(0, 4, 256)], lens, Hkv, 61)
+    q = wl.make_queries(5, H, D, 63, DEV)
+    whole = api.kv4_paged_attention_decode(q, s.pool, s.table, _ints(lens), Hkv)
+    s.check(whole, q)
+    s.check(s.call(q), q)
+    s.check(s.call(q, groups=False), q, cu=[0], prefix=[])
+
+
+def test_shared_garbage_lengths_pages_and_groups():
+    H, Hkv = 4, 2
+    s = _Batch([(0, 3, 128)], [256, 190, 160, 130], Hkv, 71, width=5)
+    q = wl.make_queries(4, H, D, 73, DEV)
+    lens = _ints([1 << 30, -5, 160, 130])                                   # past the table and below zero
+    s.table[0, 1], s.table[2, 2] = -7, s.pages                              # pages that are none: in the prefix, and behind it
+    s.table_np = s.table.cpu().numpy()
+    out = api.kv4_shared_attention_decode(q, s.pool, s.table, lens, _ints([0, 3]), _ints([128]), Hkv)
+    s.check(out, q, lens=[320, 0, 160, 130])
+    # lengths of prefixes past the table and below zero
+    out = api.kv4_shared_attention_decode(q, s.pool, s.table, _ints([200, 190, 160, 130]), _ints([0, 1, 4]), _ints([-3, 1 << 30]), Hkv)
+    s.check(out, q, lens=[200, 190, 160, 130], cu=[0, 1, 4], prefix=[0, 320])
+    # bounds outside the batch: the nearest ones
+    out = api.kv4_shared_attention_decode(q, s.pool, s.table, _ints([200, 190, 160, 130]), _ints([-4, 1 << 30]), _ints([64]), Hkv)
+    s.check(out, q, lens=[200, 190, 160, 130], cu=[0, 4], prefix=[64])
+
+
+def test_shared_values_that_are_not_finite_reach_the_sequences_that_see_them():
+    """An infinity among the prefix's last tokens (its scale is one, its values 0 times that): not in the results of members that end in front of it."""
+    H, Hkv, prefix = 4, 2, 100
+    lens = [130, 90, 99, 100, 7, 97]
+    s = _Batch([(0, 6, prefix)], lens, Hkv, 81)
+    q = wl.make_queries(6, H, D, 83, DEV)
+    clean = s.call(q)
+    s.check(clean, q)
+    bad = torch.full((1, Hkv, D), float("inf"), dtype=torch.float16, device=DEV)
+    api.kv4_paged_append(s.pool, bad, bad, s.table[:1].contiguous(), _ints([0, 1]), _ints([98]))
+    out = s.call(q)
+    sees = torch.tensor([n > 98 for n in lens])
+    assert _same(out[~sees.to(DEV)], clean[~sees.to(DEV)])
+    assert out[sees.to(DEV)].isnan().all()
+
+
+def test_shared_strided_queries_another_stream_and_refusals():
+    H, Hkv, B = 8, 2, 21
+    s = _Batch([(0, B, 130)], [131 + 3 * i for i in range(B)], Hkv, 91)
+    qkv = _heads(B, H + 2 * Hkv, 92)
+    q = qkv[:, :H]
+    want = s.call(q.contiguous())
+    assert _same(s.call(q), want)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = s.call(q)
+    side.synchronize()
+    assert _same(got, want)
+    out = torch.empty_like(want)
+    assert s.call(q, out=out) is out or _same(out, want)
+    assert _same(out, want)
+    cu, prefix, lens = _ints(s.cu), _ints(s.prefix), _ints(s.lens)
+    with pytest.raises(ValueError):
+        api.kv4_shared_attention_decode(q, s.pool, s.table, lens, cu, _ints([1, 2]), Hkv)
+    with pytest.raises(ValueError):
+        api.kv4_shared_attention_decode(q, s.pool, s.table, lens[:3].contiguous(), cu, prefix, Hkv)
+    with pytest.raises(TypeError):
+        api.kv4_shared_attention_decode(q, s.pool, s.table, lens, cu.long(), prefix, Hkv)
+    with pytest.raises(api.QoqError):
+        api.kv4_shared_attention_decode(q[:, :7], s.pool, s.table, lens, cu, prefix, Hkv)
+
+
+def test_shared_two_streams_at_once():
+    H, Hkv = 8, 2
+    s = _Batch([(0, 9, 700)], [705 + 5 * i for i in range(9)], Hkv, 101)
+    q = wl.make_queries(9, H, D, 103, DEV)
+    want = s.call(q)
+    streams, spaces = [torch.cuda.Stream() for _ in range(2)], [torch.empty(api.kv4_shared_attention_workspace_bytes(9, H, Hkv, s.width, 1), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    cu, prefix, lens = _ints(s.cu), _ints(s.prefix), _ints(s.lens)
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(20):
+        for stream, ws in zip(streams, spaces):
+            with torch.cuda.stream(stream):
+                got.append(api.kv4_shared_attention_decode(q, s.pool, s.table, lens, cu, prefix, Hkv, workspace=ws))
+    torch.cuda.synchronize()
+    assert all(_same(g, want) for g in got)
+
+
+def test_shared_pages_past_four_gigabytes():
+    Hkv, pages = 8, 70000                                                   # 4.87 GB
+    pool = torch.empty(pages * Hkv * 8704, dtype=torch.uint8, device=DEV)
+    table = _ints([[69999, 65000], [69999, 12]])
+    k, v = _heads(100, Hkv, 111), _heads(100, Hkv, 112, True)
+    api.kv4_paged_append(pool, k[:90].contiguous(), v[:90].contiguous(), table[:1].contiguous(), _ints([0, 90]))
+    api.kv4_paged_append(pool, k[90:].contiguous(), v[90:].contiguous(), table[1:].contiguous(), _ints([0, 10]), _ints([64]))
+    q = wl.make_queries(2, 8, D, 113, DEV)
+    out = api.kv4_shared_attention_decode(q, pool, table, _ints([90, 74]), _ints([0, 2]), _ints([64]), Hkv)
+    want = api.kv4_paged_attention_decode(q, pool, table, _ints([90, 74]), Hkv)
+    assert (out.float() - want.float()).abs().max() <= 4 * 2.0 ** -11 * want.float().abs().max() + 1e-4
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# Adapters
+# ------------------------------------------------------------------------------------------------------------------
+def _half(seed, *shape, scale=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return (torch.randn(shape, generator=g, device=DEV) * scale).half()
+
+
+def _lora_inputs(M, N, K, rank, adapters, seed):
+    x = _half(seed, M, K)
+    x[:, ::97] *= 20.0
+    return (_half(seed + 1, M, N), x, _half(seed + 2, adapters, rank, K, scale=K ** -0.5), _half(seed + 3, adapters, N, rank, scale=0.1),
+            torch.rand(adapters, generator=torch.Generator().manual_seed(seed)).add(0.5).to(DEV))
+
+
+def _check_lora(out, base, x, a, b, rows, scales, pick=None):
+    pick = list(range(len(rows))) if pick is None else pick
+    used = sorted({rows[m] for m in pick if 0 <= rows[m] < a.shape[0]}) or [0]
+    at = {n: i for i, n in enumerate(used)}
+    f = lambda t: t.cpu().numpy().astype(np.float64)      # noqa: E731
+    ref, off = requests.lora(f(base[pick]), f(x[pick]), f(a[used]), f(b[used]), [at.get(rows[m], -1) for m in pick], None if scales is None else f(scales[used]))
+    got = f(out[pick])
+    with np.errstate(invalid="ignore"):                                     # (what is not finite in the definition is the same here)
+        tol = 2.0 ** -11 * np.abs(ref) + off + 2.0 ** -25
+        assert ((np.abs(got - ref) <= tol) | (got == ref) & np.isinf(ref) | np.isnan(got) & np.isnan(ref)).all(), float(np.nanmax(np.abs(got - ref) / tol))
+
+
+@pytest.mark.parametrize("M", [1, 2, 15, 16, 17, 64, 130])
+@pytest.mark.parametrize("N,K,rank", [(8, 8, 8), (64, 128, 16), (200, 776, 24), (72, 264, 32), (136, 1000, 40), (1032, 4096, 64)])
+def test_lora(M, N, K, rank):
+    adapters = 5
+    base, x, a, b, scales = _lora_inputs(M, N, K, rank, adapters, M + N)
+    rows = [(m * 7 + 3) % 6 for m in range(M)]                              # 5: none
+    plan = api.lora_plan(_ints(rows), adapters)
+    out = api.lora_add(base, x, a, b, plan, scales=scales)
+    _check_lora(out, base, x, a, b, rows, scales)
+
+
+@pytest.mark.parametrize("M,N,K,rank,adapters", [(513, 72, 136, 8, 3), (700, 264, 520, 16, 2), (1100, 520, 264, 64, 9), (600, 200, 2056, 40, 1), (520, 136, 72, 72, 2),
+                                                 (640, 136, 200, 200, 600), (30, 264, 136, 512, 4), (5, 136, 264, 104, 4096), (1030, 72, 88, 128, 40)])
+def test_lora_tiles_of_64_rows_and_large_ranks(M, N, K, rank, adapters):
+    base, x, a, b, scales = _lora_inputs(M, N, K, rank, adapters, 7 * M)
+    rows = [(m * m // 50) % (adapters + 2) - 1 for m in range(M)]
+    plan = api.lora_plan(_ints(rows), adapters)
+    pick = list(range(0, M, 13)) + [M - 1]
+    out = api.lora_add(base, x, a, b, plan, scales=scales)
+    _check_lora(out, base, x, a, b, rows, scales, pick)
+    none = [m for m in range(M) if not 0 <= rows[m] < adapters]
+    if none:
+        assert _same(out[none], base[none])
+    again = api.lora_add(base, x, a, b, api.lora_plan(_ints(rows), adapters), scales=scales)
+    assert _same(out, again)                                               # whatever the order in a tile
+
+
+@pytest.mark.parametrize("M", [33, 600])
+def test_lora_in_place_strided_and_without_scales(M):
+    """Onto slices of a fused projection's output, from a slice of wider activations; what lies beside is left alone."""
+    N, K, rank, adapters = 192, 256, 16, 3
+    _, x, a, b, _ = _lora_inputs(M, N, K, rank, adapters, 5)
+    wide_x, fused = _half(11, M, K + 24), _half(12, M, 3 * N)
+    wide_x[:, 8:8 + K] = x
+    rows = [m % 4 for m in range(M)]
+    plan = api.lora_plan(_ints(rows), adapters)
+    keep = fused.clone()
+    out = api.lora_add(fused[:, N:2 * N], wide_x[:, 8:8 + K], a, b, plan, out=fused[:, N:2 * N])
+    assert out.data_ptr() == fused[:, N:2 * N].data_ptr()
+    _check_lora(fused[:, N:2 * N], keep[:, N:2 * N], x, a, b, rows, None, list(range(0, M, 7)))
+    assert _same(fused[:, :N], keep[:, :N]) and _same(fused[:, 2 * N:], keep[:, 2 * N:])
+    assert _same(fused[3::4, N:2 * N], keep[3::4, N:2 * N])
+    apart = torch.full((M, N + 8), 7.0, dtype=torch.float16, device=DEV)
+    api.lora_add(keep[:, N:2 * N], x, a, b, plan, out=apart[:, :N])
+    assert _same(apart[:, :N], fused[:, N:2 * N]) and (apart[:, N:] == 7.0).all()
+
+
+def test_lora_of_no_rows_and_of_rows_without_adapters():
+    base, x, a, b, scales = _lora_inputs(40, 64, 64, 8, 2, 3)
+    empty = torch.empty(0, dtype=torch.int32, device=DEV)
+    assert api.lora_add(base[:0], x[:0], a, b, api.lora_plan(empty, 2)).shape == (0, 64)
+    for value in (-1, 2, 1 << 30, -(1 << 31)):
+        assert _same(api.lora_add(base, x, a, b, api.lora_plan(_ints([value] * 40), 2), scales=scales), base)
+
+
+def test_lora_plan_of_another_batch_writes_nothing():
+    base, x, a, b, _ = _lora_inputs(40, 64, 64, 8, 2, 3)
+    for plan in (api.lora_plan(_ints([0] * 41), 2), api.lora_plan(_ints([0] * 40), 3), torch.zeros(1000, dtype=torch.int32, device=DEV),
+                 torch.full((1000,), 40, dtype=torch.int32, device=DEV)):
+        out = torch.full_like(base, 7.0)
+        api.lora_add(base, x, a, b, plan, out=out)
+        assert (out == 7.0).all()
+
+
+@pytest.mark.parametrize("M", [20, 530])
+def test_lora_infinities_and_large_numbers(M):
+    """What is not finite stays in its row; middle products past FP16's range count in full."""
+    N, K, rank = 72, 136, 16
+    base, x, a, b, scales = _lora_inputs(M, N, K, rank, 2, 9)
+    rows = [m % 2 for m in range(M)]
+    plan = api.lora_plan(_ints(rows), 2)
+    clean = api.lora_add(base, x, a, b, plan, scales=scales)
+    bad = x.clone()
+    bad[3, 5], bad[8, 0] = float("nan"), float("inf")
+    out = api.lora_add(base, bad, a, b, plan, scales=scales)
+    others = [m for m in range(M) if m not in (3, 8)]
+    assert _same(out[others], clean[others]) and out[3].isnan().all() and not torch.isfinite(out[8]).any()
+    big = (x.float() * 1000.0).half()
+    small = (b.float() / 4096.0).half()
+    _check_lora(api.lora_add(base, big, (a.float() * 200.0).half(), small, plan, scales=scales), base, big, (a.float() * 200.0).half(), small, rows, scales, others[::5])
+    tiny = (x.float() / 60000.0).half()
+    _check_lora(api.lora_add(base, tiny, a, b, plan, scales=scales), base, tiny, a, b, rows, scales, others[::5])
+
+
+def test_lora_graph_with_its_plan_and_streams():
+    """Plan and two projections in one graph, replayed with other adapters and activations in the same tensors; overlapping calls."""
+    M, K, rank, adapters = 48, 512, 16, 6
+    base, x, a, b, scales = _lora_inputs(M, 320, K, rank, adapters, 21)
+    base2, x2, a2, b2, _ = _lora_inputs(M, 128, 320, rank, adapters, 22)
+    need = max(api.lora_workspace_bytes(M, 320, K, rank, adapters), api.lora_workspace_bytes(M, 128, 320, rank, adapters))
+    ws = api.new_workspace(need, DEV)
+    ws[api.GEMM_COUNTER_BYTES:] = 0xFF
+    row = _ints([m % 7 for m in range(M)])
+    plan, outs = api.lora_plan(row, adapters), [torch.empty_like(base), torch.empty_like(base2)]
+
+    def step():
+        api.lora_plan(row, adapters, out=plan)
+        api.lora_add(base, x, a, b, plan, scales=scales, out=outs[0], workspace=ws)
+        api.lora_add(base2, outs[0], a2, b2, plan, scales=scales, out=outs[1], workspace=ws)
+
+    def fill(i):
+        row.copy_(_ints([(m * (i + 1)) % 7 for m in range(M)]))
+        x.copy_(_half(30 + i, M, K))
+
+    want = []
+    for i in range(3):
+        fill(i)
+        step()
+        want.append([o.clone() for o in outs])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for i in (0, 1, 2, 1, 0):
+        fill(i)
+        for o in outs:
+            o.fill_(7.0)
+        graph.replay()
+        assert _same(outs[0], want[i][0]) and _same(outs[1], want[i][1])
+        torch.cuda.synchronize()
+        api.lora_add(base, x, a, b, plan, workspace=ws)
+    assert not ws[:api.GEMM_COUNTER_BYTES].any()
+    fill(0)
+    api.lora_plan(row, adapters, out=plan)
+    torch.cuda.synchronize()
+    streams, spaces, got = [torch.cuda.Stream() for _ in range(2)], [api.new_workspace(need, DEV) for _ in range(2)], []
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, space in zip(streams, spaces):
+            with torch.cuda.stream(stream):
+                got.append(api.lora_add(base, x, a, b, plan, scales=scales, workspace=space))
+    torch.cuda.synchronize()
+    assert all(_same(g, want[0][0]) for g in got)
+
+
+def test_lora_binding_refuses():
+    base, x, a, b, scales = _lora_inputs(8, 64, 64, 8, 2, 3)
+    plan = api.lora_plan(_ints([0] * 8), 2)
+    for args in ((base, x[:7], a, b, plan), (base, x, a[:1], b, plan), (base, x, a, b[:, :32].contiguous(), plan), (base, x, a[:, :, :32].contiguous(), b, plan)):
+        with pytest.raises(ValueError):
+            api.lora_add(*args)
+    with pytest.raises(TypeError):
+        api.lora_add(base.float(), x, a, b, plan)
+    with pytest.raises(ValueError):
+        api.lora_add(base, x, a, b, plan, scales=scales[:1].contiguous())
+    with pytest.raises(ValueError):
+        api.lora_add(base.t().contiguous().t(), x, a, b, plan)
+    with pytest.raises(api.QoqError):
+        api.lora_add(base, x, a, b, plan[:20].contiguous())
+    with pytest.raises(api.QoqError):
+        api.lora_plan(_ints([0] * 8), 0)
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# Log probabilities
+# ------------------------------------------------------------------------------------------------------------------
+def _check_logprobs(got, x, tokens, top, rows=None):
+    lp, rank, ent, ids, tops = (None if t is None else t.cpu().numpy() for t in got)
+    xs = x.detach().cpu().float().numpy()
+    V = xs.shape[1]
+    for m in range(xs.shape[0]) if rows is None else rows:
+        wlp, wrank, went, wids, wtops, dist = requests.logprobs(xs[m], -1 if tokens is None else int(tokens[m]), top)
+        dT = 2.0 ** -23 + 2.0 ** -24 * (1.1 * dist + 6) + (V / 64 + 100) * 2.0 ** -24
+
+        def near(a, b, tol):
+            a, b = np.asarray(a, dtype=np.float64), np.asarray(b, dtype=np.float64)
+            with np.errstate(invalid="ignore"):
+                return ((a == b) | (np.isnan(a) & np.isnan(b)) | (np.abs(a - b) <= tol)).all()
+
+        if tokens is not None:
+            assert near(lp[m], wlp, dT + 2.0 ** -24 * abs(wlp)), (m, lp[m], wlp)
+            assert rank[m] == wrank, (m, rank[m], wrank)
+        assert near(ent[m], went, dT * (2 + 2 * (1.45 * dist + 8)) + 2.0 ** -24 * abs(went)), (m, ent[m], went)
+        if top:
+            assert list(ids[m]) == list(wids), (m, ids[m], wids)
+            with np.errstate(invalid="ignore"):
+                assert near(tops[m], wtops, dT + 2.0 ** -24 * np.abs(wtops)), (m, tops[m], wtops)
+
+
+def _logits(M, V, seed, dtype, spread=2.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn((M, V), generator=g, device=DEV) * spread
+    x.scatter_add_(1, torch.randint(0, V, (M, 6), generator=g, device=DEV), torch.rand((M, 6), generator=g, device=DEV) * 14.0)
+    return x.to(dtype)
+
+
+def _workspace(x, top):
+    return api.new_workspace(api.token_logprobs_workspace_bytes(x.shape[0], x.shape[1], top, x.dtype), DEV)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("V", [1, 2, 7, 8, 9, 31, 63, 100, 255, 257, 1000, 2047, 2048, 2049, 4099, 16385, 32000, 50257])
+@pytest.mark.parametrize("top", [0, 1, 5, 32])
+def test_logprobs(dtype, V, top):
+    M, top = 5, min(top, V)
+    x = _logits(M, V, V, dtype)
+    tokens = [0, V - 1, int(x[2].float().argmax()), V // 2, V // 3]
+    for ws in (None, _workspace(x, top)):
+        _check_logprobs(api.token_logprobs(x, _ints(tokens), top, workspace=ws), x, tokens, top)
+    _check_logprobs(api.token_logprobs(x, None, top), x, None, top)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("top", [0, 20])
+def test_logprobs_strides_and_unaligned_rows(dtype, top):
+    """Rows at any element, of any distance; what lies in front and behind does not count."""
+    V = 4099
+    wide = _logits(9, V + 1037, 3, dtype)
+    wide[:, :5], wide[:, 5 + V:] = float("nan"), float("inf")
+    for first in (5,):
+        x = wide[:, first:first + V]
+        tokens = [0, 1, V - 1, 17, 2000, -1, V, 3, 4000]
+        for ws in (None, _workspace(x, top)):
+            _check_logprobs(api.token_logprobs(x, _ints(tokens), top, workspace=ws), x, tokens, top)
+    flat = _logits(1, 12 * 37 + 8, 4, dtype)[0]
+    for shift in range(8):
+        x = flat[shift:shift + 12 * 37].view(12, 37)
+        tokens = list(range(0, 36, 3))
+        _check_logprobs(api.token_logprobs(x, _ints(tokens), min(top, 37)), x, tokens, min(top, 37))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("V", [300, 5003, 40000])
+def test_logprobs_of_equal_logits_masks_and_extremes(dtype, shared, V):
+    top, low = 20, torch.finfo(dtype).min
+    x = torch.zeros((14, V), dtype=dtype, device=DEV)
+    x[1] = 3.0
+    x[2] = low                                                              # a mask of the type's lowest value everywhere: a uniform row
+    x[3] = low
+    x[3, V - 2] = 1.0
+    x[4] = -float("inf")
+    x[4, V // 2] = -5.0                                                     # one token allowed
+    x[5] = -float("inf")
+    x[5, 7::9] = torch.randn(len(range(7, V, 9)), device=DEV).to(dtype)
+    x[6] = torch.arange(V, device=DEV) % 3                                  # many equal ones
+    x[7] = -(torch.arange(V, device=DEV) % 2).to(dtype) * 0.0               # zeros of both signs
+    x[8] = torch.finfo(dtype).max
+    x[9, ::2] = low
+    x[10] = torch.linspace(-30, 30, V, device=DEV).to(dtype)
+    x[11] = torch.linspace(30, -30, V, device=DEV).to(dtype)
+    x[12] = torch.randint(-3, 3, (V,), device=DEV).to(dtype)
+    x[13, V // 3] = torch.finfo(dtype).max
+    tokens = [V - 1, 5, V // 2, V - 2, 3, 16, V - 1, 1, 0, 1, V // 2, V // 2, V - 1, V // 3]
+    ws = _workspace(x, top) if shared else None
+    _check_logprobs(api.token_logprobs(x, _ints(tokens), top, workspace=ws), x, tokens, top)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_logprobs_of_rows_without_an_answer(dtype):
+    V = 9001
+    x = _logits(8, V, 5, dtype)
+    x[0, 17], x[1, V - 1], x[2], x[3, 0], x[4, 100], x[4, 200] = float("nan"), float("inf"), -float("inf"), float("nan"), float("inf"), float("nan")
+    x[5] = float("nan")
+    tokens = [17, 0, 4, V - 1, 100, 1, V - 1, 0]
+    for top in (0, 7):
+        for ws in (None, _workspace(x, top)):
+            _check_logprobs(api.token_logprobs(x, _ints(tokens), top, workspace=ws), x, tokens, top)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("shared", [False, True])
+def test_logprobs_of_large_tokens_at_one_distance(dtype, shared):
+    """The largest logits all at places that one lane reads, more than can be ranked at once."""
+    V, top = 1 << 20, 32
+    x = torch.randn((2, V), device=DEV).clamp(-4, 4).to(dtype)
+    vec = 16 * 8 // torch.finfo(dtype).bits
+    at = (torch.arange(0, V, 256 * vec, device=DEV)[:, None] + torch.arange(vec, device=DEV)).flatten()
+    x[0, at] = (torch.rand(at.numel(), device=DEV) * 4 + 8).to(dtype)
+    x[1, at] = 9.0
+    tokens = [int(at[-1]), int(at[3000])]
+    ws = _workspace(x, top) if shared else None
+    _check_logprobs(api.token_logprobs(x, _ints(tokens), top, workspace=ws), x, tokens, top)
+
+
+def test_logprobs_many_rows_and_the_longest():
+    x = _logits(3000, 515, 7, torch.float16)
+    tokens = [(m * 31) % 515 for m in range(3000)]
+    _check_logprobs(api.token_logprobs(x, _ints(tokens), 3, workspace=_workspace(x, 3)), x, tokens, 3, range(0, 3000, 37))
+    x = _logits(1, 1 << 24, 8, torch.float16)
+    for ws in (None, _workspace(x, 32)):
+        _check_logprobs(api.token_logprobs(x, _ints([12345678]), 32, workspace=ws), x, [12345678], 32)
+
+
+def test_logprobs_past_four_gigabytes():
+    V = 70001
+    x = torch.zeros((32000, V), dtype=torch.float16, device=DEV)            # 4.5 GB: 2.24e9 elements
+    rows = [0, 15338, 31999]
+    for m in rows:
+        x[m] = _logits(1, V, m, torch.float16)[0]
+    tokens = torch.full((32000,), 5, dtype=torch.int32, device=DEV)
+    got = api.token_logprobs(x, tokens, 4)
+    pick = torch.tensor(rows, device=DEV)
+    _check_logprobs([t[pick] for t in got], x[pick], [5, 5, 5], 4)
+    assert (got[1][1:100] == 6).all() and (got[3][1:100] == torch.arange(4, device=DEV)).all()
+
+
+def test_logprobs_same_bits_in_graphs_and_on_streams():
+    x, y = _logits(7, 32000, 11, torch.float16), _logits(7, 32000, 12, torch.float16)
+    tokens, top = _ints([5, 100, 31999, 0, 7, 8, 9]), 20
+    ws = _workspace(x, top)
+    ws[api.GEMM_COUNTER_BYTES:] = 0xFF
+    want = [[t.clone() for t in api.token_logprobs(z, tokens, top, workspace=ws)] for z in (x, y)]
+    for _ in range(5):
+        assert all(_same(a, b) for a, b in zip(api.token_logprobs(x, tokens, top, workspace=ws), want[0]))
+    here = x.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        outs = api.token_logprobs(here, tokens, top, workspace=ws)
+    for i in (1, 0, 1, 0):
+        here.copy_((x, y)[i])
+        for o in outs:
+            o.fill_(3)
+        graph.replay()
+        assert all(_same(a, b) for a, b in zip(outs, want[i]))
+        torch.cuda.synchronize()
+        api.token_logprobs(y[:3], tokens[:3].contiguous(), 2, workspace=ws)
+    assert not ws[:api.GEMM_COUNTER_BYTES].any()
+    streams, spaces, got = [torch.cuda.Stream() for _ in range(2)], [_workspace(x, top) for _ in range(2)], []
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, space in zip(streams, spaces):
+            with torch.cuda.stream(stream):
+                got.append(api.token_logprobs(x, tokens, top, workspace=space))
+    torch.cuda.synchronize()
+    assert all(_same(a, b) for g in got for a, b in zip(g, want[0]))
+    with pytest.raises(api.QoqError):
+        api.token_logprobs(x, tokens, top, workspace=ws[:1024])
+    with pytest.raises(api.QoqError):
+        api.token_logprobs(x, tokens, 33)
+    with pytest.raises(ValueError):
+        api.token_logprobs(x, tokens[:2].contiguous())
+    with pytest.raises(ValueError):
+        api.token_logprobs(x.t(), tokens)
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# Together
+# ------------------------------------------------------------------------------------------------------------------
+def test_a_decode_step_of_many_requests():
+    """Two layers' worth of a step, as a server runs them: adapters on the fused QKV projection, append, attention over a shared prefix, adapters on the
+    output projection, the last projection's log probabilities; eager and as one graph, replayed as the sequences grow."""
+    B, H, Hkv, hidden, V, rank, adapters, prefix = 12, 8, 2, 512, 1024, 16, 5, 192
+    N = (H + 2 * Hkv) * D
+    s = _Batch([(0, 10, prefix)], [prefix + 3 + i for i in range(10)] + [20, 64], Hkv, 131, width=6)
+    weights = [api.pack_weights(wl.make_weights(n, k, seed, DEV)) for n, k, seed in ((N, hidden, 1), (hidden, H * D, 2), (V, hidden, 3))]
+    la = [(_half(41, adapters, rank, hidden, scale=0.05), _half(42, adapters, N, rank, scale=0.1)), (_half(43, adapters, rank, H * D, scale=0.05), _half(44, adapters, hidden, rank, scale=0.1))]
+    scales = torch.tensor([0.5, 1.0, 2.0, 1.5, 0.25], device=DEV)
+    row = _ints([b % 6 for b in range(B)])
+    angles = api.rope_angles(s.width * PAGE, device=DEV)
+    cu, group_cu, pl = _ints(list(range(B + 1))), _ints(s.cu), _ints(s.prefix)
+    # every sequence writes its next token into a page of its own: the tables get them now
+    pool = torch.cat((s.pool, torch.zeros(B * 2 * Hkv * 8704, dtype=torch.uint8, device=DEV)))
+    table = s.table.clone()
+    for b in range(B):
+        n = -(-s.lens[b] // PAGE)
+        table[b, n:n + 2] = _ints([s.pages + 2 * b, s.pages + 2 * b + 1])[:s.width - n]
+    lens = _ints(s.lens)
+    starts, tokens = lens.clone(), _ints([3 * b for b in range(B)])
+    ws = api.new_workspace(max(api.gemm_workspace_bytes(B, N, hidden), api.gemm_workspace_bytes(B, hidden, H * D), api.gemm_workspace_bytes(B, V, hidden),
+                               api.lora_workspace_bytes(B, N, hidden, rank, adapters), api.lora_workspace_bytes(B, hidden, H * D, rank, adapters),
+                               api.token_logprobs_workspace_bytes(B, V, 5)), DEV)
+    scratch = torch.empty(api.kv4_shared_attention_workspace_bytes(B, H, Hkv, s.width, 1), dtype=torch.uint8, device=DEV)
+    x = wl.make_activations(B, hidden, 7, DEV)
+    plan = api.lora_plan(row, adapters)
+
+    def step():
+        api.lora_plan(row, adapters, out=plan)
+        starts.copy_(lens)
+        lens.add_(1)
+        qkv = api.w4a8_linear(x, weights[0], N, workspace=ws)[0]
+        api.lora_add(qkv, x, *la[0], plan, scales=scales, out=qkv, workspace=ws)
+        heads = qkv.view(B, H + 2 * Hkv, D)
+        q, _ = api.qk_rope_kv4_append(heads[:, :H], heads[:, H:H + Hkv], heads[:, H + Hkv:], pool, table, cu, starts, angles)
+        att = api.kv4_shared_attention_decode(q, pool, table, lens, group_cu, pl, Hkv, workspace=scratch)
+        out = api.w4a8_linear(att.view(B, H * D), weights[1], hidden, workspace=ws)[0]
+        api.lora_add(out, att.view(B, H * D), *la[1], plan, scales=scales, out=out, workspace=ws)
+        logits = api.w4a8_linear(out, weights[2], V, workspace=ws)[0]
+        return (q, att, out, logits, *api.token_logprobs(logits, tokens, 5, workspace=ws))
+
+    first = [t.clone() for t in step()]
+    q, att, out, logits = first[:4]
+    _check_logprobs(first[4:], logits, tokens.tolist(), 5)
+    base = api.w4a8_linear(att.view(B, H * D), weights[1], hidden)[0]
+    _check_lora(out, base, att.view(B, H * D), *la[1], row.tolist(), scales)
+    # the prefix is of whole pages, which every member's table names: each sequence by itself reads the same tokens, and both results are within
+    # 2^-11 of themselves and 2^-10 of the values' average of the exact one
+    alone = api.kv4_paged_attention_decode(q, pool, table, lens, Hkv)
+    rows = [int(n) for n in lens.tolist()]
+    _, v = api.kv4_paged_gather(pool, table, _ints(np.concatenate(([0], np.cumsum(rows))).tolist()), None, sum(rows), Hkv)
+    most = float(v.float().abs().max())
+    assert (alone.float() - att.float()).abs().max() <= 2 * (2.0 ** -11 + 2.0 ** -10) * most
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    lens.copy_(_ints(s.lens))
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        kept = step()
+    for _ in range(3):
+        lens.copy_(_ints(s.lens))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(_same(a, b) for a, b in zip(kept, first))
+    graph.replay()                                                          # a step further on: another token in every sequence
+    torch.cuda.synchronize()
+    assert not _same(kept[1], first[1]) and torch.isfinite(kept[1].float()).all()
