@@ -360,7 +360,7 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
  *   Sums are FP32, held relative to the row's largest.  Logits of minus infinity (a masked vocabulary) have probability 0 and logprob minus
  *   infinity.  A token outside [0, V): logprob NaN, rank 0.  A row that holds a NaN or plus infinity, or minus infinity only: all of its
  *   results NaN, rank 0, top_ids -1.  tokens may be NULL with logprob and rank; logprob, rank and entropy may be NULL.
- *   workspace  NULL, or qoq_token_logprobs_workspace_bytes(...) bytes (0: none is needed), zero-filled once as above, shared in turns as above;
+ *   workspace  NULL, or qoq_token_logprobs_workspace_bytes(...) bytes (0: none is needed), 16-byte aligned, contents irrelevant on entry and exit;
  *              without one a row is not shared by several workgroups.
  * Limits: groups <= 1048576; rank % 8 == 0, rank <= 512, N % 8 == 0, K % 8 == 0, N and K <= 4194304, adapters <= 4096, M <= 1048576 (adapters);
  * V <= 16777216, M <= 16777216 (logits; 2^24 workgroups or more: QOQ_ERR_HIP); the rest as for the paged decode.  Errors as above. */

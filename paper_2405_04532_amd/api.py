@@ -457,8 +457,9 @@ def token_logprobs_workspace_bytes(M, V, top=0, dtype=torch.float16):
 def token_logprobs(logits, tokens=None, top=0, workspace=None):
     """Of each row of logits [M, V], FP16 or FP32: log probability and rank (1: the most likely) of the token that `tokens` [M] INT32 names,
     the entropy, and the `top` (at most 32) most likely tokens with their log probabilities, equal logits by index; returns
-    (logprob [M] FP32 | None, rank [M] INT32 | None, entropy [M] FP32, top_ids [M, top] INT32 | None, top_logprobs [M, top] FP32 | None).
-    With a `workspace` (new_workspace of token_logprobs_workspace_bytes) several workgroups may share a row."""
+    (logprob [M] FP32 | None, rank [M] INT32 | None, entropy [M] FP32, top_ids [M, top] INT32 | None, top_logprobs [M, top] FP32 | None),
+    parts of one allocation.
+    With a `workspace` (uint8 tensor of token_logprobs_workspace_bytes, any contents) several workgroups may share a row."""
     return (_native or _load_native()).token_logprobs(logits, tokens, top, workspace)
 
 
