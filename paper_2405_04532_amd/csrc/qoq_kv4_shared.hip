@@ -23,8 +23,12 @@ constexpr int kPartial = kD + 4;                         // floats of a part: 12
 constexpr int kChunk = 32;                               // tokens: two tiles of 16 (divides the page)
 constexpr int kWaves = 4;                                // of a workgroup
 constexpr int kMaxParts = 64;                            // of a prefix, and of a sequence's own tokens
+constexpr int kInFlight = 8;                             // parts that the join requests together
 constexpr int kColumnTiles = 2;                          // of 16 columns for each wave, over a prefix
 constexpr int kPrefixColumns = 16 * kColumnTiles;
+constexpr int kWide = 2;                                 // the same where a prefix's columns are many and a workgroup's waves have columns of their own
+constexpr int kWideWorkgroups = 512;                     // that share the prefixes then: two on a compute unit
+constexpr int kLeastRun = 4;                             // pages of a run
 
 struct SharedArgs {
     const uint8_t* pool;
@@ -34,13 +38,18 @@ struct SharedArgs {
     __half* out;
     int64_t q_stride;
     uint32_t pages;
-    int width, B, G, Hkv, R, prefix_parts, own_parts;
-    uint32_t prefix_blocks;
+    int width, B, G, Hkv, R, prefix_parts, own_parts, prefix_workgroups;
+    uint32_t prefix_blocks, ratio_magic;                 // ceil(2^32 / R)
 };
+// n / R for n < 2^28
+__device__ __forceinline__ int by_ratio(const SharedArgs& p, int n) { return p.R == 1 ? n : (int)__umulhi((uint32_t)n, p.ratio_magic); }
 
 typedef const __attribute__((address_space(1))) uint8_t* global_bytes;
 typedef const __attribute__((address_space(1))) u32x4* global_u32x4;
 typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+// the block table, which no kernel here writes: entries at addresses that a wave shares come through the scalar cache, and only their use waits
+typedef const __attribute__((address_space(4))) int32_t* constant_ints;
+__device__ __forceinline__ constant_ints constant(const int32_t* at) { return (constant_ints)(uintptr_t)at; }
 
 // Workgroups that attend to `chunks` chunks, of the `parts` that stand by: as few as leave each wave two, if there are that many.
 __device__ __forceinline__ int attending(int chunks, int parts) { return min(parts, (chunks + 2 * kWaves - 1) / (2 * kWaves)); }
@@ -62,6 +71,28 @@ __device__ __forceinline__ int prefix_of(const SharedArgs& p, int b, int lane)
     return 0;
 }
 
+// sums over the lanes up to each, in registers
+__device__ __forceinline__ int upto_lane(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);       // from 1, 2, 4, 8 lanes back in a row of 16
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);       // the last of rows 0 and 2 into 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);       // the last of row 1 into 2 and 3
+    return v;
+}
+__device__ __forceinline__ int largest_of_lanes(int v)                    // (of numbers that are not negative)
+{
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
 struct Work {
     const int32_t* pages_of;                             // the block table's row
     int hk, lo, hi;                                      // KV head; tokens lo .. hi - 1
@@ -69,6 +100,7 @@ struct Work {
     int first, column0, columns;                         // column c is head (column0 + c) % R of sequence first + (column0 + c) / R
     int slot;                                            // of the parts
     int total_slots;
+    int page, page_end;                                  // of the wide form, in place of part and parts
 };
 
 // One workgroup's range of tokens for up to 16 CT columns.  PK = 2: two tiles of tokens share the columns of a matrix instruction (at most
@@ -119,7 +151,7 @@ __device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float
     auto chunk_of = [&](int it) __attribute__((always_inline)) {           // of the wave's it-th turn, or its last
         return __builtin_amdgcn_readfirstlane(c0 + min(i0 + max(min(it, n_iter - 1), 0) * stride, n - 1));
     };
-    auto page_of = [&](int it) __attribute__((always_inline)) { return (uint32_t)k.pages_of[chunk_of(it) >> 1]; };
+    auto page_of = [&](int it) __attribute__((always_inline)) { return (uint32_t)constant(k.pages_of)[chunk_of(it) >> 1]; };
     Chunk A, Bf;
     uint32_t id_a = page_of(0), id_b = page_of(1);
     load_chunk(A, chunk_of(0), id_a);
@@ -130,8 +162,8 @@ __device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float
     int least = k.hi, most = LIMITS ? 0 : k.hi;          // of the columns' limits: what lies behind all of them need not have been written
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        const int column = c * 16 + (PK == 2 ? r16 & 7 : r16), held = k.column0 + min(column, k.columns - 1), b = k.first + held / R;
-        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_stride + (int64_t)(k.hk * R + held % R) * kD + kb * 32);
+        const int column = c * 16 + (PK == 2 ? r16 & 7 : r16), held = k.column0 + min(column, k.columns - 1), s = by_ratio(p, held), b = k.first + s;
+        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_stride + (int64_t)(k.hk * R + held - s * R) * kD + kb * 32);
         const uint32_t some = column < k.columns ? ~0u : 0u;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -146,13 +178,8 @@ __device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float
         }
     }
     if (LIMITS) {
-#pragma unroll
-        for (int o = 8; o; o >>= 1) {
-            least = min(least, __shfl_xor(least, o, 64));
-            most = max(most, __shfl_xor(most, o, 64));
-        }
-        least = __builtin_amdgcn_readfirstlane(least);
-        most = __builtin_amdgcn_readfirstlane(most);
+        least = k.hi - largest_of_lanes(k.hi - least);
+        most = largest_of_lanes(most);
     }
 
     // of a lane's columns, over the tokens they have seen: the reference that scores are taken from before they become weights, and the weights' sum
@@ -297,23 +324,16 @@ __device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float
         }
     };
 
-    int it = 0;
-    for (; it + 2 < n_iter; it += 2) {
-        load_chunk(Bf, chunk_of(it + 1), id_b);
-        const uint32_t now = id_a;
-        id_a = page_of(it + 2);
-        process(A, it, now);
-        load_chunk(A, chunk_of(it + 2), id_a);
-        const uint32_t then = id_b;
-        id_b = page_of(it + 3);
-        process(Bf, it + 1, then);
-    }
-    if (it + 2 == n_iter) {
+    // One copy of the arithmetic: a call on short sequences runs through its code once, and pays for fetching it.  The last turn requests its own
+    // chunk again (which is in the caches).
+#pragma unroll 1
+    for (int it = 0; it < n_iter; ++it) {
+        const uint32_t id_after = page_of(it + 2);
         load_chunk(Bf, chunk_of(it + 1), id_b);
         process(A, it, id_a);
-        process(Bf, it + 1, id_b);
-    } else if (n_iter > 0) {
-        process(A, it, id_a);
+        A = Bf;
+        id_a = id_b;
+        id_b = id_after;
     }
 
     // ---- the partial results of the waves (and of the column halves) meet in LDS, a column tile at a time: [wave, half][16 / PK][kPartial] ----
@@ -350,8 +370,8 @@ __device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float
                 num.x = fmaf(a.x, f, num.x); num.y = fmaf(a.y, f, num.y); num.z = fmaf(a.z, f, num.z); num.w = fmaf(a.w, f, num.w);
                 den = fmaf(ml.y, f, den);
             }
-            const int held = k.column0 + i * 16 + at;
-            const int64_t row = ((int64_t)(k.first + held / R) * p.Hkv + k.hk) * R + held % R;
+            const int held = k.column0 + i * 16 + at, s = by_ratio(p, held);
+            const int64_t row = ((int64_t)(k.first + s) * p.Hkv + k.hk) * R + held - s * R;
             float* to = p.parts + (row * k.total_slots + k.slot) * kPartial;
             *reinterpret_cast<float4*>(to + d) = num;
             if (d == 0) *reinterpret_cast<float4*>(to + kD) = make_float4(mm, den, 0.f, 0.f);
@@ -359,55 +379,411 @@ __device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float
     }
 }
 
-template <int PK>
-__global__ __launch_bounds__(64 * kWaves) void shared_decode_kernel(SharedArgs p)
+// ---- A prefix that many columns share: four waves of 16 CT columns each, the pages unpacked once for all of them ----
+// A page goes through LDS in the order of the matrix instructions' operands, [fragment][lane] of 16 bytes, a quarter of it unpacked by each
+// wave, the next page while this one is used.
+constexpr int kPageFragments = 32;                       // of 1 KB: keys [tile][word], values [chunk][u][j]
+// Binades that the reference is set above what the largest weight needs, so that it seldom has to follow: each time costs half a chunk's arithmetic
+constexpr float kSpare = 6.f;
+struct WidePage {
+    uint4 fragment[kPageFragments][64];
+    float ks[kPageTokens], vs[kPageTokens];              // scale of a token's scores, log2(e) / sqrt(128) with it; of its values
+    float below;                                         // exponent of the largest of those, as the reference takes it
+};
+
+template <int CT>
+__device__ __forceinline__ void attend_wide(const SharedArgs& p, const Work& k, WidePage* s_page)
 {
-    __shared__ __align__(16) float s_part[kWaves * 16 * kPartial];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r16 = lane & 15, kb = lane >> 4, R = p.R;
+    const int first = k.page, end = k.page_end;
+
+    uint4 qv[CT][4];
+    int limit[CT];
+    int least = k.hi, most = 0;                          // of this wave's columns' limits; of all, behind which nothing need have been written
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        const int column = (wave * CT + c) * 16 + r16, held = k.column0 + min(column, k.columns - 1), s = by_ratio(p, held), b = k.first + s;
+        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_stride + (int64_t)(k.hk * R + held - s * R) * kD + kb * 32);
+        const uint32_t some = column < k.columns ? ~0u : 0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint4 t = src[e];
+            qv[c][e] = make_uint4(t.x & some, t.y & some, t.z & some, t.w & some);
+        }
+        limit[c] = min(max(p.seq_lens[b], 0), k.hi);
+        least = min(least, limit[c]);
+    }
+    for (int s = by_ratio(p, k.column0) + lane, last = by_ratio(p, k.column0 + k.columns - 1); s <= last; s += 64) most = max(most, min(max(p.seq_lens[k.first + s], 0), k.hi));
+    least = k.hi - largest_of_lanes(k.hi - least);
+    most = largest_of_lanes(most);
+
+    // this wave's quarter of a page: the keys of tile `wave`, half u of the values' elements of chunk `wave` / 2
+    struct Staged {
+        uint4 kc, vp[2];
+        uint2 vc[2];
+        uint32_t kz, param;                              // of token `lane`: of its key (wave 0), its value (wave 1)
+    };
+    const int chunk = wave >> 1, u = wave & 1;
+    auto page_id = [&](int i) __attribute__((always_inline)) { return (uint32_t)constant(k.pages_of)[min(i, end - 1)]; };
+    auto load = [&](Staged& s, uint32_t id) __attribute__((always_inline)) {
+        const uint32_t held = id < p.pages ? id : 0;
+        const uint8_t* page = p.pool + ((int64_t)held * p.Hkv + k.hk) * kPageBytes;
+        s.kc = *reinterpret_cast<const uint4*>(page + wave * 1024 + r16 * (kD / 2) + kb * 16);
+        s.kz = *reinterpret_cast<const uint32_t*>(page + kCodeBytes + (wave * 16 + r16) * 4);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            s.vc[tt] = *reinterpret_cast<const uint2*>(page + kHalfPage + (2 * chunk + tt) * 1024 + lane * 16 + 8 * u);
+            s.vp[tt] = *reinterpret_cast<const uint4*>(page + kHalfPage + kCodeBytes + ((2 * chunk + tt) * 16 + 4 * kb) * 4);
+        }
+        s.param = *reinterpret_cast<const uint32_t*>(page + (wave == 1 ? kHalfPage : 0) + kCodeBytes + lane * 4);
+    };
+    const float kScale = 1.4426950408889634f * 0.08838834764831845f;      // log2(e) / sqrt(128)
+    const h2 k960 = {(_Float16)960.0f, (_Float16)960.0f};
+    auto unpack = [&](Staged s, int i, uint32_t id, WidePage& to) __attribute__((always_inline)) {
+        const int held = (id < p.pages ? most : 0) - i * kPageTokens;     // tokens of the page that some column sees
+        if (held < kPageTokens) {
+            s.kz = wave * 16 + r16 < held ? s.kz : 0xE4000000u;           // -(1024 + 0): the others' parameters may be anything
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                const int t = (2 * chunk + tt) * 16 + 4 * kb;
+                s.vp[tt] = make_uint4(t < held ? s.vp[tt].x : 0xE4000000u, t + 1 < held ? s.vp[tt].y : 0xE4000000u, t + 2 < held ? s.vp[tt].z : 0xE4000000u,
+                                      t + 3 < held ? s.vp[tt].w : 0xE4000000u);
+            }
+            s.param = lane < held ? s.param : 0;
+        }
+        {
+            const h2 c = __builtin_bit_cast(h2, __builtin_amdgcn_perm(s.kz, s.kz, 0x07060706u));
+            const h2 c16 = c + k960;
+            const uint32_t kw[4] = {s.kc.x, s.kc.y, s.kc.z, s.kc.w};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                h2 kh[4];
+                unpack4(kw[w], c, c16, kh);
+                to.fragment[wave * 4 + w][lane] = __builtin_bit_cast(uint4, join(kh[0], kh[1], kh[2], kh[3]));
+            }
+        }
+        h2 vh[2][2][4];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            const uint32_t zw[4] = {s.vp[tt].x, s.vp[tt].y, s.vp[tt].z, s.vp[tt].w}, vw[2] = {s.vc[tt].x, s.vc[tt].y};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const h2 cz = __builtin_bit_cast(h2, __builtin_amdgcn_perm(zw[2 * h + 1], zw[2 * h], 0x07060302u));
+                unpack4(vw[h], cz, cz + k960, vh[tt][h]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to.fragment[16 + wave * 4 + j][lane] = __builtin_bit_cast(uint4, join(vh[0][0][j], vh[0][1][j], vh[1][0][j], vh[1][1][j]));
+        const float scale = (float)half_of(s.param);
+        if (wave == 0) to.ks[lane] = scale * kScale;
+        if (wave == 1) {
+            to.vs[lane] = scale;
+            int exponent = (int)((s.param >> 10) & 31u);
+#pragma unroll
+            for (int o = 32; o; o >>= 1) exponent = max(exponent, __shfl_xor(exponent, o, 64));
+            if (lane == 0) to.below = (float)exponent - 29.f;
+        }
+    };
+
+    float m[CT], l[CT];
+    f4 acc[CT][8];                                       // acc[.][4u + j][x]: element d = 16 kb + 4x + 64u + j of the column
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        m[c] = -1e29f; l[c] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[c][i] = (f4){0.f, 0.f, 0.f, 0.f};
+    }
+    auto process = [&](const WidePage& page, int i, uint32_t id) __attribute__((always_inline)) {
+        const bool partly = !(id < p.pages && (i + 1) * kPageTokens <= least);
+        const float below = page.below;
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            // (the operands of a half are requested together, those of the second product in front of the softmax: requested one at a time, as
+            // the compiler orders them, each trip to LDS is waited for, twice what the arithmetic takes)
+            uint4 kf[8], vf[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) kf[e] = page.fragment[half * 8 + e][lane];
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_sched_barrier(0);
+            f4 d[CT][2];
+            float t[CT][8], over[CT];
+            bool follow = partly;
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    d[c][e >> 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, kf[e]), __builtin_bit_cast(h8, qv[c][e & 3]), e & 3 ? d[c][e >> 2] : (f4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            float ks[8], vs[8];                          // [4 tt + x]: of token 4 kb + x of tile tt
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                const float4 a = *reinterpret_cast<const float4*>(page.ks + (2 * half + tt) * 16 + 4 * kb), b = *reinterpret_cast<const float4*>(page.vs + (2 * half + tt) * 16 + 4 * kb);
+                ks[4 * tt] = a.x; ks[4 * tt + 1] = a.y; ks[4 * tt + 2] = a.z; ks[4 * tt + 3] = a.w;
+                vs[4 * tt] = b.x; vs[4 * tt + 1] = b.y; vs[4 * tt + 2] = b.z; vs[4 * tt + 3] = b.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) vf[e] = page.fragment[16 + half * 8 + e][lane];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                over[c] = -1e30f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    t[c][e] = fmaf(d[c][e >> 2][e & 3], ks[e], -m[c]);
+                    over[c] = fmaxf(over[c], t[c][e]);
+                }
+                // The reference has to follow: a weight times the largest scale would pass 2^15.  (Where FP32 no longer holds a score's units, the sum
+                // of score and exponent would be rounded by more than there is room: the score itself is the reference.)
+                follow |= over[c] + (fabsf(m[c]) < 0x1p23f - 64.f ? below : 0.f) > 0.f;
+            }
+            // softmax weight times value scale of column tile c, the operand of the second product, and the weights' sum
+            auto weights = [&](int c, const float (&by)[8]) __attribute__((always_inline)) {
+                uint32_t b[4];
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(t[c][e]), p1 = __builtin_amdgcn_exp2f(t[c][e + 1]);
+                    l[c] += p0;
+                    l[c] += p1;
+                    b[e / 2] = __builtin_bit_cast(uint32_t, (h2){(_Float16)(p0 * by[e]), (_Float16)(p1 * by[e + 1])});
+                }
+                return __builtin_bit_cast(h8, make_uint4(b[0], b[1], b[2], b[3]));
+            };
+            float scale[CT][8];                          // of what a column sees
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) scale[c][e] = vs[e];
+            if (__builtin_amdgcn_ballot_w64(follow) != 0) {
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    const int end_c = (id < p.pages ? limit[c] : 0) - i * kPageTokens - half * 32 - 4 * kb;
+                    float top = -1e30f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool seen = (e >> 2) * 16 + (e & 3) < end_c;
+                        t[c][e] = seen ? d[c][e >> 2][e & 3] * ks[e] : -1e30f;
+                        scale[c][e] = seen ? vs[e] : 0.f;
+                        top = fmaxf(top, t[c][e]);
+                    }
+                    const float m_new = max_other_half(max_other_row(fmaxf(m[c], top + (fabsf(top) < 0x1p23f ? below + kSpare : 0.f))));
+                    const float alpha = __builtin_amdgcn_exp2f(m[c] - m_new);
+                    m[c] = m_new;
+                    l[c] *= alpha;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        acc[c][e] *= alpha;
+                        t[c][e] -= m_new;
+                    }
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                const h8 b8 = weights(c, scale[c]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, vf[e]), b8, acc[c][e], 0, 0, 0);
+            }
+        }
+    };
+
+    // (a wave may be a page ahead of the others, which then use the other buffer)
+    Staged staged;
+    uint32_t id = page_id(first), id_next = page_id(first + 1);
+    load(staged, id);
+#pragma unroll 1
+    for (int i = first; i < end; ++i) {
+        const uint32_t id_after = page_id(i + 2);
+        WidePage& page = s_page[(i - first) & 1];
+        unpack(staged, i, id, page);
+        load(staged, id_next);                           // (the last turn its own page again)
+        __syncthreads();
+        process(page, i, id);
+        id = id_next;
+        id_next = id_after;
+    }
+    // The parts leave through LDS, a column tile at a time, in whole rows: stored from the registers, 16 bytes here and there, they took as long as
+    // three pages (64 sequences behind 4096 tokens of 32 / 8 heads 41 us, 28 without the stores).
+    __syncthreads();                                     // (the pages are done with)
+    float* s_rows = reinterpret_cast<float*>(s_page) + wave * 16 * kPartial;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        l[c] += __shfl_xor(l[c], 16, 64);
+        l[c] += __shfl_xor(l[c], 32, 64);
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                *reinterpret_cast<float4*>(s_rows + r16 * kPartial + 16 * kb + 4 * x + 64 * v) = make_float4(acc[c][4 * v][x], acc[c][4 * v + 1][x], acc[c][4 * v + 2][x], acc[c][4 * v + 3][x]);
+        if (kb == 0) *reinterpret_cast<float4*>(s_rows + r16 * kPartial + kD) = make_float4(m[c], l[c], 0.f, 0.f);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");           // the wave's own writes, then its reads
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        const int column0 = (wave * CT + c) * 16, columns = min(k.columns - column0, 16);
+#pragma unroll 1
+        for (int i = lane; i < columns * (kPartial / 4); i += 64) {
+            const int column = i / (kPartial / 4), held = k.column0 + column0 + column, s = by_ratio(p, held);
+            const int64_t row = ((int64_t)(k.first + s) * p.Hkv + k.hk) * R + held - s * R;
+            *reinterpret_cast<float4*>(p.parts + (row * k.total_slots + k.slot) * kPartial + (i - column * (kPartial / 4)) * 4) = *reinterpret_cast<const float4*>(s_rows + i * 4);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();                                     // (the next run begins with the first buffer)
+}
+
+// The work over all prefixes where they are wide: units of a page for a tile of columns, by group, KV head, tile and page, dealt to the workgroups in
+// equal runs of `run` units, of which none covers a tile in more parts than there are slots.
+struct Units {
+    int all, run;
+    int before;                                          // units of the groups in front of the one looked for
+    int first, columns, tokens, pages, tiles;            // that group
+};
+
+// Groups g0 .. g0 + 63, one to a lane.
+template <int TILE>
+struct GroupLanes {
+    int first, last, tokens, columns, pages, tiles, units, upto;
+    __device__ __forceinline__ void load(const SharedArgs& p, int g0)
+    {
+        const int g = g0 + (int)(threadIdx.x & 63);
+        first = last = tokens = 0;
+        if (g < p.G) {
+            const int a = p.cu[g], e = p.cu[g + 1], n = p.prefix_lens[g];
+            first = min(max(a, 0), p.B);
+            last = max(min(e, p.B), first);
+            tokens = min(max(n, 0), p.width * kPageTokens);
+        }
+        columns = (last - first) * p.R;
+        tiles = (columns + TILE - 1) / TILE;
+        pages = tiles ? (tokens + kPageTokens - 1) / kPageTokens : 0;
+        units = tiles * p.Hkv * pages;
+        upto = upto_lane(units);
+    }
+    __device__ __forceinline__ void pick(Units& f, unsigned long long who, int before) const
+    {
+        const int w = __builtin_ctzll(who);
+        f.before = before + __builtin_amdgcn_readlane(upto, w) - __builtin_amdgcn_readlane(units, w);
+        f.first = __builtin_amdgcn_readlane(first, w);
+        f.columns = __builtin_amdgcn_readlane(columns, w);
+        f.tokens = __builtin_amdgcn_readlane(tokens, w);
+        f.pages = __builtin_amdgcn_readlane(pages, w);
+        f.tiles = __builtin_amdgcn_readlane(tiles, w);
+    }
+};
+// All units and the runs they are dealt in; where `b` >= 0, the group of sequence b as well (tokens 0: none).  `g` is left at the last 64 groups.
+template <int TILE>
+__device__ __forceinline__ void count_units(const SharedArgs& p, GroupLanes<TILE>& g, Units& f, int b)
+{
+    f.all = 0;
+    f.tokens = 0;
+    int longest = 0;
+    for (int g0 = 0; g0 < p.G; g0 += 64) {
+        g.load(p, g0);
+        if (b >= 0 && !f.tokens) {
+            const unsigned long long who = __builtin_amdgcn_ballot_w64(g.first <= b && b < g.last && g.tokens > 0);
+            if (who) g.pick(f, who, f.all);
+        }
+        f.all += __builtin_amdgcn_readlane(g.upto, 63);
+        longest = max(longest, largest_of_lanes(g.pages));
+    }
+    f.run = max(max((f.all + p.prefix_workgroups - 1) / p.prefix_workgroups, min(kLeastRun, max(longest, 1))), (longest + p.prefix_parts - 3) / (p.prefix_parts - 2));
+}
+template <int TILE>
+__device__ __forceinline__ void find_unit(const SharedArgs& p, GroupLanes<TILE>& g, Units& f, int unit)
+{
+    int before = 0;
+    for (int g0 = 0; g0 < p.G; g0 += 64) {
+        if (p.G > 64) g.load(p, g0);
+        const unsigned long long who = __builtin_amdgcn_ballot_w64(before + g.upto > unit && g.units > 0);
+        if (who) {
+            g.pick(f, who, before);
+            return;
+        }
+        before += __builtin_amdgcn_readlane(g.upto, 63);
+    }
+}
+
+// WIDE: column tiles of a wave where the prefix's columns are many, 0 where a workgroup's waves share the tokens of kPrefixColumns
+template <int PK, int WIDE>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void shared_decode_kernel(SharedArgs p)
+{
+    constexpr size_t kNarrowBytes = kWaves * 16 * kPartial * sizeof(float), kWideBytes = 2 * sizeof(WidePage);
+    __shared__ __align__(16) unsigned char s_bytes[WIDE && kWideBytes > kNarrowBytes ? kWideBytes : kNarrowBytes];
+    float* s_part = reinterpret_cast<float*>(s_bytes);
     const int lane = threadIdx.x & 63;
     const int most = p.width * kPageTokens;
     Work k{};
     k.total_slots = p.prefix_parts + p.own_parts;
     if (blockIdx.x < p.prefix_blocks) {
-        const uint32_t of_tile = (uint32_t)p.Hkv * p.prefix_parts, rest = blockIdx.x % of_tile;
-        int tile = blockIdx.x / of_tile;
-        k.hk = rest % p.Hkv;
-        k.part = rest / p.Hkv;
-        // the tile's group: tiles of the groups in front of each are counted 64 groups at a time
-        bool found = false;
-        for (int g0 = 0; g0 < p.G && !found; g0 += 64) {
-            const int g = g0 + lane;
-            int first = 0, columns = 0, tokens = 0;
-            if (g < p.G) {
-                first = min(max(p.cu[g], 0), p.B);
-                columns = max(min(p.cu[g + 1], p.B) - first, 0) * p.R;
-                tokens = min(max(p.prefix_lens[g], 0), most);
+        if constexpr (WIDE != 0) {
+            constexpr int kTile = 64 * WIDE;
+            // runs of neighbouring units on one chiplet: its L2 then holds the pages of a KV head or two
+            const int w = (int)(blockIdx.x % 8) * (p.prefix_workgroups / 8) + (int)(blockIdx.x / 8);
+            Units f;
+            GroupLanes<kTile> g;
+            count_units<kTile>(p, g, f, -1);
+            int unit = w * f.run;
+            const int end = min(unit + f.run, f.all);
+#pragma unroll 1
+            while (unit < end) {
+                find_unit<kTile>(p, g, f, unit);
+                const int of_group = unit - f.before, column_tile = of_group / f.pages, hk = column_tile / f.tiles, tile = column_tile - hk * f.tiles;
+                k.page = of_group - column_tile * f.pages;
+                k.page_end = min(k.page + end - unit, f.pages);
+                k.hk = hk;
+                k.hi = f.tokens;
+                k.first = f.first;
+                k.column0 = tile * kTile;
+                k.columns = min(f.columns - tile * kTile, kTile);
+                k.pages_of = p.table + (int64_t)k.first * p.width;
+                k.slot = w - (unit - k.page) / f.run;
+                unit += k.page_end - k.page;
+                attend_wide<WIDE>(p, k, reinterpret_cast<WidePage*>(s_bytes));
             }
-            const int tiles = tokens ? (columns + kPrefixColumns - 1) / kPrefixColumns : 0;
-            int upto = tiles;
-            for (int o = 1; o < 64; o <<= 1) {
-                const int v = __shfl_up(upto, o, 64);
-                if (lane >= o) upto += v;
+            return;
+        } else {
+            const uint32_t of_tile = (uint32_t)p.Hkv * p.prefix_parts, rest = blockIdx.x % of_tile;
+            int tile = blockIdx.x / of_tile;
+            k.hk = rest % p.Hkv;
+            k.part = rest / p.Hkv;
+            // the tile's group: tiles of the groups in front of each are counted 64 groups at a time
+            bool found = false;
+            for (int g0 = 0; g0 < p.G && !found; g0 += 64) {
+                const int g = g0 + lane;
+                int first = 0, columns = 0, tokens = 0;
+                if (g < p.G) {
+                    first = min(max(p.cu[g], 0), p.B);
+                    columns = max(min(p.cu[g + 1], p.B) - first, 0) * p.R;
+                    tokens = min(max(p.prefix_lens[g], 0), most);
+                }
+                const int tiles = tokens ? (columns + kPrefixColumns - 1) / kPrefixColumns : 0;
+                int upto = tiles;
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int v = __shfl_up(upto, o, 64);
+                    if (lane >= o) upto += v;
+                }
+                const unsigned long long who = __builtin_amdgcn_ballot_w64(upto > tile);
+                if (who) {
+                    const int f = __builtin_ctzll(who);
+                    const int at = tile - (__shfl(upto, f, 64) - __shfl(tiles, f, 64));
+                    const int group_first = __builtin_amdgcn_readfirstlane(__shfl(first, f, 64));
+                    k.hi = __builtin_amdgcn_readfirstlane(__shfl(tokens, f, 64));
+                    k.columns = __builtin_amdgcn_readfirstlane(min(__shfl(columns, f, 64) - at * kPrefixColumns, kPrefixColumns));
+                    k.first = group_first;
+                    k.column0 = __builtin_amdgcn_readfirstlane(at * kPrefixColumns);
+                    k.pages_of = p.table + (int64_t)group_first * p.width;
+                    found = true;
+                } else {
+                    tile -= __shfl(upto, 63, 64);
+                }
             }
-            const unsigned long long who = __builtin_amdgcn_ballot_w64(upto > tile);
-            if (who) {
-                const int f = __builtin_ctzll(who);
-                const int at = tile - (__shfl(upto, f, 64) - __shfl(tiles, f, 64));
-                const int group_first = __builtin_amdgcn_readfirstlane(__shfl(first, f, 64));
-                k.hi = __builtin_amdgcn_readfirstlane(__shfl(tokens, f, 64));
-                k.columns = __builtin_amdgcn_readfirstlane(min(__shfl(columns, f, 64) - at * kPrefixColumns, kPrefixColumns));
-                k.first = group_first;
-                k.column0 = __builtin_amdgcn_readfirstlane(at * kPrefixColumns);
-                k.pages_of = p.table + (int64_t)group_first * p.width;
-                found = true;
-            } else {
-                tile -= __shfl(upto, 63, 64);
-            }
+            if (!found) return;
+            k.parts = attending((k.hi + kChunk - 1) / kChunk, p.prefix_parts);
+            if (k.part >= k.parts) return;
+            k.slot = k.part;
+            attend<kColumnTiles, 1, true>(p, k, s_part);
         }
-        if (!found) return;
-        k.parts = attending((k.hi + kChunk - 1) / kChunk, p.prefix_parts);
-        if (k.part >= k.parts) return;
-        k.slot = k.part;
-        attend<kColumnTiles, 1, true>(p, k, s_part);
     } else {
         const uint32_t i = blockIdx.x - p.prefix_blocks, pairs = (uint32_t)p.B * p.Hkv, bh = i % pairs;
         const int b = bh / p.Hkv;
@@ -427,6 +803,7 @@ __global__ __launch_bounds__(64 * kWaves) void shared_decode_kernel(SharedArgs p
 }
 
 // The parts of a head, a wave to a head: two elements to a lane, a part's reference to a lane.
+template <int WIDE>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
 {
     const int lane = threadIdx.x & 63;
@@ -435,8 +812,23 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
     if (row >= (int64_t)p.B * H) return;
     const int b = (int)(row / H);
     const int most = p.width * kPageTokens;
-    const int P = prefix_of(p, b, lane), L = min(max(p.seq_lens[b], 0), most), lo = min(P, L);
-    const int n_prefix = P && L ? attending((P + kChunk - 1) / kChunk, p.prefix_parts) : 0;
+    const int L = min(max(p.seq_lens[b], 0), most);
+    int P, n_prefix = 0;
+    if constexpr (WIDE != 0) {
+        Units f;
+        GroupLanes<64 * WIDE> g;
+        count_units<64 * WIDE>(p, g, f, b);
+        P = f.tokens;
+        if (P && L) {
+            const int h = (int)(row % H), hk = h / p.R, tile = ((b - f.first) * p.R + h % p.R) / (64 * WIDE);
+            const int unit = f.before + (hk * f.tiles + tile) * f.pages;
+            n_prefix = (unit + f.pages - 1) / f.run - unit / f.run + 1;
+        }
+    } else {
+        P = prefix_of(p, b, lane);
+        if (P && L) n_prefix = attending((P + kChunk - 1) / kChunk, p.prefix_parts);
+    }
+    const int lo = min(P, L);
     const int n_own = L > lo ? attending((L + kChunk - 1) / kChunk - lo / kChunk, p.own_parts) : 0;
     const int total = p.prefix_parts + p.own_parts, n = n_prefix + n_own;
     const float* parts = p.parts + row * total * kPartial;
@@ -459,17 +851,24 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
 #pragma unroll
     for (int o = 32; o; o >>= 1) den += __shfl_xor(den, o, 64);
     float2 sum = make_float2(0.f, 0.f);
-#pragma unroll 8
-    for (int i = 0; i < n; ++i) {
-        const float2 a = *reinterpret_cast<const float2*>(parts + (int64_t)slot(i) * kPartial + 2 * lane);
-        const float g = __shfl(i < 64 ? f[0] : f[1], i & 63, 64);
-        sum.x = fmaf(a.x, g, sum.x); sum.y = fmaf(a.y, g, sum.y);
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += kInFlight) {
+        float2 a[kInFlight];
+#pragma unroll
+        for (int e = 0; e < kInFlight; ++e) a[e] = *reinterpret_cast<const float2*>(parts + (int64_t)slot(min(i0 + e, n - 1)) * kPartial + 2 * lane);
+#pragma unroll
+        for (int e = 0; e < kInFlight; ++e) {
+            const int i = i0 + e;
+            const float g = i < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(i < 64 ? f[0] : f[1]), i & 63)) : 0.f;
+            sum.x = fmaf(a[e].x, g, sum.x); sum.y = fmaf(a[e].y, g, sum.y);
+        }
     }
     const float inv = den > 0.f ? 1.f / den : 1.f;       // nothing seen: zero, as the sums are (NaN stays)
     reinterpret_cast<h2*>(p.out + row * kD)[lane] = (h2){(_Float16)(sum.x * inv), (_Float16)(sum.y * inv)};
 }
 
-int64_t prefix_tiles(int64_t B, int64_t G, int64_t R) { return G ? B * R / kPrefixColumns + G : 0; }
+bool wide_prefix(int64_t B, int64_t G, int64_t R) { return G && B * R / G >= 64; }
+int64_t prefix_tiles(int64_t B, int64_t G, int64_t R) { return G ? B * R / (wide_prefix(B, G, R) ? 64 * kWide : kPrefixColumns) + G : 0; }
 // Workgroups that stand by for each tile of columns of a prefix and KV head, and for each sequence and KV head: two to a compute unit.
 int parts_for(int64_t items, int64_t width)
 {
@@ -477,11 +876,19 @@ int parts_for(int64_t items, int64_t width)
     return (int)std::max<int64_t>(1, std::min<int64_t>({kMaxParts, 512 / items, (2 * width + 2 * kWaves - 1) / (2 * kWaves)}));
 }
 
+// Parts of a tile of columns of a prefix: twice what an even share of the workgroups comes to, and the pieces at its ends.
+int prefix_parts(int64_t B, int64_t G, int64_t R, int64_t Hkv, int64_t width)
+{
+    const int64_t items = prefix_tiles(B, G, R) * Hkv;
+    if (!wide_prefix(B, G, R)) return parts_for(items, width);
+    return (int)std::min<int64_t>(kMaxParts, 2 * kWideWorkgroups / items + 3);
+}
+
 }  // namespace
 
 size_t shared_decode_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t width, int64_t G)
 {
-    const int64_t slots = parts_for(prefix_tiles(B, G, H / Hkv) * Hkv, width) + parts_for(B * Hkv, width);
+    const int64_t slots = prefix_parts(B, G, H / Hkv, Hkv, width) + parts_for(B * Hkv, width);
     return (size_t)(B * H * slots) * kPartial * sizeof(float);
 }
 
@@ -495,17 +902,22 @@ hipError_t launch_shared_decode(const void* q, int64_t q_stride, const uint8_t* 
     p.parts = static_cast<float*>(workspace);
     p.out = static_cast<__half*>(out);
     p.pages = (uint32_t)pages; p.width = (int)width; p.B = (int)B; p.G = (int)G; p.Hkv = (int)Hkv; p.R = (int)(H / Hkv);
-    const int64_t tiles = prefix_tiles(B, G, p.R);
-    p.prefix_parts = parts_for(tiles * Hkv, width);
+    const bool wide = wide_prefix(B, G, p.R);
+    p.prefix_parts = prefix_parts(B, G, p.R, Hkv, width);
     p.own_parts = parts_for(B * Hkv, width);
-    const int64_t prefix_blocks = tiles * Hkv * p.prefix_parts, blocks = prefix_blocks + B * Hkv * p.own_parts, joins = (B * H + 3) / 4;
+    p.prefix_workgroups = kWideWorkgroups;
+    p.ratio_magic = (uint32_t)((((uint64_t)1 << 32) + p.R - 1) / p.R);
+    const int64_t prefix_blocks = wide ? kWideWorkgroups : prefix_tiles(B, G, p.R) * Hkv * p.prefix_parts;
+    const int64_t blocks = prefix_blocks + B * Hkv * p.own_parts, joins = (B * H + 3) / 4;
     if (blocks >= (int64_t)1 << 24 || joins >= (int64_t)1 << 24) return hipErrorInvalidValue;    // 2^32 threads
+    if (wide && prefix_tiles(B, G, p.R) * Hkv * width >= (int64_t)1 << 31) return hipErrorInvalidValue;  // units of work, counted in 32 bits
     p.prefix_blocks = (uint32_t)prefix_blocks;
     const int PK = p.R <= 8 ? 2 : 1;
-    auto* kernel = PK == 2 ? shared_decode_kernel<2> : shared_decode_kernel<1>;
+    auto* kernel = PK == 2 ? (wide ? shared_decode_kernel<2, kWide> : shared_decode_kernel<2, 0>) : (wide ? shared_decode_kernel<1, kWide> : shared_decode_kernel<1, 0>);
     kernel<<<(unsigned)blocks, 64 * kWaves, 0, s>>>(p);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    shared_join_kernel<<<(unsigned)joins, 256, 0, s>>>(p);
+    auto* join = wide ? shared_join_kernel<kWide> : shared_join_kernel<0>;
+    join<<<(unsigned)joins, 256, 0, s>>>(p);
     return hipGetLastError();
 }
 
