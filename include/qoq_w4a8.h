@@ -329,7 +329,8 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
 
 /* ---- A decode step of many requests ---------------------------------------------------------------------------
  * Requests that share a long prompt, each with an adapter of its own, whose answers are scored: what such a step runs beside
- * the calls above.
+ * the calls above.  These calls may take turns in one workspace, whatever it holds, on one stream (not in a GEMM's, whose counters they would
+ * overwrite: its bytes behind the first QOQ_GEMM_COUNTER_BYTES will do); calls that overlap in time need workspaces of their own.
  *
  * qoq_kv4_shared_attention_decode: qoq_kv4_paged_attention_decode (without a window) of B sequences, of which those of a group g,
  *   group_cu[g] .. group_cu[g + 1] - 1, share their first prefix_lens[g] tokens.  Those are read from the pages that the block table names
@@ -340,8 +341,7 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
  *     group_cu     [groups + 1] INT32, device, ascending; sequences in front of the first and behind the last share nothing
  *     prefix_lens  [groups] INT32, device, clamped to [0, 64 width]; a sequence that is shorter sees its seq_lens[b] tokens of it
  *     groups = 0: the pointers may be NULL.  Descending or overlapping groups give unspecified results and touch nothing else.
- *   workspace  required, qoq_kv4_shared_attention_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant on entry and exit (it may
- *              be a GEMM workspace's part behind the counters, or any scratch); calls that overlap in time need workspaces of their own.
+ *   workspace  required, qoq_kv4_shared_attention_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant on entry and exit.
  * qoq_lora_add: out[m] = base[m] + scales[a] (x[m] A_a^T) B_a^T for the rows m of adapter a, out[m] = base[m] for those of none.
  *   base [M, N], x [M, K], out [M, N] FP16 with row strides in elements (multiples of 8), so that they may be slices of a fused projection's;
  *   out may be base (with its stride), but not overlap base, x, a or b otherwise.  a [adapters, rank, K], b [adapters, N, rank] FP16 contiguous;
@@ -349,8 +349,7 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
  *   second product to 2^-22 of itself, or 2^-39 of the largest of its 64 ranks where that is more; one rounding at the end.
  *   plan  of qoq_lora_plan for the same M and adapters: which rows are whose, worked out once and used by every projection of a step (and
  *         by calls on other streams that are ordered behind it).  A plan of another M or number of adapters, or none: nothing is written.
- *   workspace  required, qoq_lora_workspace_bytes(...) bytes, 16-byte aligned, zero-filled once with qoq_gemm_workspace_prepare, as for
- *              qoq_w4a8_gemm, whose workspace may be the same one.
+ *   workspace  required, qoq_lora_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant on entry and exit.
  * qoq_lora_plan: row_adapter [M] INT32, device: the adapter of each row; any value outside [0, adapters) is none.  Opaque, qoq_lora_plan_bytes
  *   bytes, 16-byte aligned.
  * qoq_token_logprobs: per row of logits [M, V], FP16 or FP32 (dtype), with a row stride in elements (any, at least V):

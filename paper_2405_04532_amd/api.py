@@ -446,7 +446,8 @@ def lora_workspace_bytes(M, N, K, rank, adapters):
 def lora_add(base, x, a, b, plan, scales=None, out=None, workspace=None):
     """base + scales[i] (x a[i]^T) b[i]^T per row with its adapter i, base where it has none: base [M, N] (the shared projection's
     output), x [M, K], a [adapters, rank, K], b [adapters, N, rank] FP16, scales [adapters] FP32 or None.  Rows may be strided; out may be
-    base.  `plan` is lora_plan's for these rows.  The `workspace` (new_workspace of lora_workspace_bytes) is made if None."""
+    base.  `plan` is lora_plan's for these rows.  The `workspace` (uint8 tensor of lora_workspace_bytes, any contents) is
+    allocated if None."""
     return (_native or _load_native()).lora_add(base, x, a, b, plan, scales, out, workspace)
 
 

@@ -5,18 +5,16 @@
 // Plan.  Which rows belong to which adapter is the same for every projection of a step, so it is worked out once: the rows ordered by
 // adapter, and tiles of up to tile_rows(M) of them that share one, so that an adapter's matrices are read once for a tile.
 //
-// Two launches.  The first forms h = x A^T, tile by tile, K cut over workgroups where there are few tiles; the last workgroup of a tile adds the
-// partial sums up, in their order whichever arrives when, and leaves h as pairs of FP16 numbers hi + lo of h scaled by a power of two for each
-// row (and 64 ranks): within 2^-22 of h, or 2^-39 of the row's largest.  The second forms hi B^T + lo B^T: one product whose k runs over the
-// pairs, B's columns taken twice.
+// The first launch forms h = x A^T, tile by tile, K cut over workgroups.  h enters the second product as pairs of FP16 numbers hi + lo of h
+// scaled by a power of two for each row (and 64 ranks): within 2^-22 of h, or 2^-39 of the row's largest; hi B^T + lo B^T is one product whose k
+// runs over the pairs, B's columns taken twice.  For few rows the launch of the second product adds the slices of K up and forms the pairs itself;
+// for many that is a launch between.  (Joined by the last workgroup of a tile, past the caches, a slice of 4096 x 64 sums took 3 us.)
 #include <hip/hip_fp16.h>
 
 #include <algorithm>
 
-#include "qoq_gemm_common.h"
 #include "qoq_internal.h"
 #include "qoq_kv4_common.h"
-#include "qoq_workspace.h"
 
 namespace qoq {
 namespace {
@@ -93,22 +91,28 @@ struct ShrinkArgs {
     const int4* tiles;
     const int* rows;
     float* parts;                                        // [slices][M][rank]
-    __half* h;                                           // [M][2 rank]: 64 ranks at a time, hi then lo
-    float* scales;                                       // [M][chunks]
-    int* counters;
     int64_t x_stride;
-    int M, adapters, K, rank, chunks, slice;             // slice: elements of K, a multiple of 32
+    int M, adapters, K, rank, slice;                     // slice: elements of K, a multiple of 128
 };
 
+// 2^shift that brings a row's largest number to 2^13 .. 2^14, with room for the others in FP16's range
+__device__ __forceinline__ int shift_of(float most) { return most > 0.f ? min(140 - (int)(__float_as_uint(most) >> 23), 100) : 0; }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+__device__ __forceinline__ float finite_size(float v) { return fabsf(v) < __builtin_inff() ? fabsf(v) : 0.f; }
+__device__ __forceinline__ _Float16 low_part(float y, _Float16 hi)
+{
+    const float back = (float)hi;
+    return fabsf(back) < __builtin_inff() ? (_Float16)(y - back) : (_Float16)0.f;
+}
+
+// The sums of a tile over a slice of K.  Bound by x and A where rows are many, else by the trips to memory one after the other: a wave has all of its steps in flight.
 template <int CT, int RT>
 __global__ __launch_bounds__(256) void lora_shrink_kernel(ShrinkArgs p)
 {
-    __shared__ __align__(16) float s_part[4][RT * 16][17];
-    __shared__ int s_last;
-    const int tile = blockIdx.x, part = blockIdx.y, parts = gridDim.y, z = blockIdx.z;
-    if (tile >= tiles_of(p.head, p.M, p.adapters)) return;
-    const int4 t = p.tiles[tile];
-    if (t.x < 0) return;
+    __shared__ float s_part[4][RT * 16][17];
+    const int tile = blockIdx.x, part = blockIdx.y, z = blockIdx.z;
+    const int4 t = p.tiles[tile];                        // (whatever it holds, beside the head)
+    if (tile >= tiles_of(p.head, p.M, p.adapters) || t.x < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, kb = lane >> 4;
     const int first_rank = z * kRankChunk, ranks = min(p.rank - first_rank, kRankChunk);
@@ -125,206 +129,276 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(ShrinkArgs p)
 #pragma unroll
         for (int i = 0; i < RT; ++i) acc[c][i] = (f4){0.f, 0.f, 0.f, 0.f};
 
-    const int k0 = part * p.slice, k1 = min(k0 + p.slice, p.K);
-    constexpr int kTurn = CT * RT >= 8 ? 1 : CT * RT >= 4 ? 2 : 4;       // steps in flight
-    auto load = [&](const __half* row, int k) __attribute__((always_inline)) {
-        return k < k1 ? *reinterpret_cast<const uint4*>(row + k) : make_uint4(0, 0, 0, 0);
+    // (a quarter of the slice for each wave: side by side, the waves' and slices' places in a row are spread over the memory channels, which rows of
+    // a power of two apart are not)
+    const int k0 = part * p.slice + wave * (p.slice / 4), k1 = min(k0 + p.slice / 4, p.K);
+    constexpr int kTurn = CT * RT >= 8 ? 1 : CT * RT >= 4 ? 2 : 4;       // steps requested together; twice that are in flight where rows are many
+    struct Turn { uint4 x[kTurn][CT], a[kTurn][RT]; };
+    auto load = [&](Turn& v, int k) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < kTurn; ++s) {                // (elements behind the slice are read inside the row, and left out below)
+            const int at = min(k + 32 * s + kb * 8, p.K - 8);
+#pragma unroll
+            for (int i = 0; i < RT; ++i) v.a[s][i] = *reinterpret_cast<const uint4*>(a_row[i] + at);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) v.x[s][c] = *reinterpret_cast<const uint4*>(x_row[c] + at);
+        }
     };
-    for (int k = k0 + wave * 32 + kb * 8; k - kb * 8 < k1; k += 128 * kTurn) {
-        uint4 xv[kTurn][CT], av[kTurn][RT];
+    auto multiply = [&](Turn& v, int k) __attribute__((always_inline)) {
 #pragma unroll
         for (int s = 0; s < kTurn; ++s) {
+            if (k + 32 * s >= k1) break;
+            if (k + 32 * s + 32 > k1) {
+                const uint32_t some = k + 32 * s + kb * 8 < k1 ? ~0u : 0u;
+                auto kept = [&](uint4 v) { return make_uint4(v.x & some, v.y & some, v.z & some, v.w & some); };
 #pragma unroll
-            for (int c = 0; c < CT; ++c) xv[s][c] = load(x_row[c], k + 128 * s);
+                for (int c = 0; c < CT; ++c) v.x[s][c] = kept(v.x[s][c]);
 #pragma unroll
-            for (int i = 0; i < RT; ++i) av[s][i] = load(a_row[i], k + 128 * s);
-        }
-#pragma unroll
-        for (int s = 0; s < kTurn; ++s)
+                for (int i = 0; i < RT; ++i) v.a[s][i] = kept(v.a[s][i]);
+            }
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
                 for (int i = 0; i < RT; ++i)
-                    acc[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, av[s][i]), __builtin_bit_cast(h8, xv[s][c]), acc[c][i], 0, 0, 0);
+                    acc[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, v.a[s][i]), __builtin_bit_cast(h8, v.x[s][c]), acc[c][i], 0, 0, 0);
+        }
+    };
+    Turn now;
+    if (k0 < k1) {
+        load(now, k0);
+        if constexpr (CT > 1) {
+            Turn next;
+#pragma unroll 1
+            for (int k = k0; k < k1; k += 64 * kTurn) {
+                load(next, k + 32 * kTurn);
+                multiply(now, k);
+                load(now, k + 64 * kTurn);
+                multiply(next, k + 32 * kTurn);
+            }
+        } else {
+#pragma unroll 1
+            for (int k = k0;;) {
+                multiply(now, k);
+                k += 32 * kTurn;
+                if (k >= k1) break;
+                load(now, k);
+            }
+        }
     }
 
-    // ---- the waves' sums meet in LDS, sixteen rows at a time; sixteen lanes to a row, lane w its ranks w, w + 16, ... ----
-    const int w = tid & 15, g = tid >> 4;
-    auto finish = [&](int row, const float (&v)[RT]) __attribute__((always_inline)) {       // row of the tile, whole sums
-        float most = 0.f;
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const float m = fabsf(v[i]);
-            most = fmaxf(most, i * 16 + w < ranks && m < __builtin_inff() ? m : 0.f);
-        }
-        most = row_max16(most);
-        // 2^shift brings the largest to 2^13 .. 2^14, with room for the others' sums in FP16's range
-        const int shift = most > 0.f ? min(140 - (int)(__float_as_uint(most) >> 23), 100) : 0;
-        const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
-        if (row >= t.z) return;
-        __half* to = p.h + (int64_t)(t.y + row) * 2 * p.rank + 2 * first_rank;
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const int rank = i * 16 + w;
-            if (rank >= ranks) continue;
-            const float y = v[i] * up;
-            const __half hi = __float2half_rn(y);
-            const float back = __half2float(hi);
-            to[rank] = hi;
-            to[ranks + rank] = fabsf(back) < __builtin_inff() ? __float2half_rn(y - back) : __float2half_rn(0.f);
-        }
-        if (w == 0) p.scales[(int64_t)(t.y + row) * p.chunks + z] = __uint_as_float((uint32_t)(127 - shift) << 23);
-    };
-    auto place = [&](int s, int row) { return p.parts + ((int64_t)s * p.M + t.y + row) * p.rank + first_rank; };
-#pragma unroll
+    // ---- the waves' sums meet in LDS, sixteen rows at a time; sixteen lanes to a row, RT neighbouring ranks to a lane ----
+    const int w = tid & 15, g = tid >> 4, rank0 = w * RT;
+#pragma unroll 1
     for (int c = 0; c < CT; ++c) {
         if (c * 16 >= t.z) break;
         if (c) __syncthreads();
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) s_part[wave][i * 16 + 4 * kb + x][r16] = acc[c][i][x];
-        __syncthreads();
-        float v[RT];
-#pragma unroll
-        for (int i = 0; i < RT; ++i) v[i] = (s_part[0][i * 16 + w][g] + s_part[1][i * 16 + w][g]) + (s_part[2][i * 16 + w][g] + s_part[3][i * 16 + w][g]);
-        if (parts == 1) {
-            finish(c * 16 + g, v);
-        } else if (c * 16 + g < t.z) {
-            float* to = place(part, c * 16 + g);
-#pragma unroll
-            for (int i = 0; i < RT; ++i)
-                if (i * 16 + w < ranks) __hip_atomic_store(to + i * 16 + w, v[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-    }
-    if (parts == 1) return;
-    // The stores above went past the caches that other workgroups do not share; they have arrived when the counter is raised.
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) {
-        int* counter = p.counters + tile * p.chunks + z;
-        const int old = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = old == parts - 1;
-        if (old == parts - 1) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __syncthreads();
-    if (!s_last) return;
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        if (c * 16 >= t.z) break;
-        const int row = min(c * 16 + g, t.z - 1);
-        float v[RT];
-#pragma unroll
-        for (int i = 0; i < RT; ++i) v[i] = 0.f;
-        constexpr int kInFlight = 32 / RT;
-        for (int s0 = 0; s0 < parts; s0 += kInFlight) {
-            float got[kInFlight][RT];
-#pragma unroll
-            for (int s = 0; s < kInFlight; ++s)
+        for (int q = 0; q < CT; ++q)                     // (registers have no index)
+            if (q == c)
 #pragma unroll
                 for (int i = 0; i < RT; ++i)
-                    got[s][i] = __hip_atomic_load(place(min(s0 + s, parts - 1), row) + min(i * 16 + w, ranks - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
-            for (int s = 0; s < kInFlight; ++s)
+                    for (int x = 0; x < 4; ++x) s_part[wave][i * 16 + 4 * kb + x][r16] = acc[q][i][x];
+        __syncthreads();
+        const int row = c * 16 + g;
+        if (row >= t.z || rank0 >= ranks) continue;      // (ranks come in eights)
+        float v[RT];
 #pragma unroll
-                for (int i = 0; i < RT; ++i) v[i] += s0 + s < parts ? got[s][i] : 0.f;
-        }
-        finish(c * 16 + g, v);
+        for (int i = 0; i < RT; ++i) v[i] = (s_part[0][rank0 + i][g] + s_part[1][rank0 + i][g]) + (s_part[2][rank0 + i][g] + s_part[3][rank0 + i][g]);
+        float* to = p.parts + ((int64_t)part * p.M + t.y + row) * p.rank + first_rank + rank0;
+        if constexpr (RT == 4) *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+        else if constexpr (RT == 2) *reinterpret_cast<float2*>(to) = make_float2(v[0], v[1]);
+        else *to = v[0];
     }
 }
 
+// The slices' sums of a place and 64 ranks added up, in their order, and left as pairs: sixteen lanes to a place, four ranks to a lane.
+struct PairArgs {
+    const float* parts;
+    __half* h;                                           // [M][2 rank]: 64 ranks at a time, hi then lo
+    float* scales;                                       // [M][chunks]
+    int M, rank, chunks, slices;
+};
+__global__ __launch_bounds__(256) void lora_pair_kernel(PairArgs p)
+{
+    const int w = threadIdx.x & 15, place = min((int)(blockIdx.x * 16 + (threadIdx.x >> 4)), p.M - 1), z = blockIdx.y;
+    const int first = z * kRankChunk, ranks = min(p.rank - first, kRankChunk), rank = min(4 * w, ranks - 4);
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    constexpr int kInFlight = 8;
+#pragma unroll 1
+    for (int s0 = 0; s0 < p.slices; s0 += kInFlight) {
+        float4 got[kInFlight];
+#pragma unroll
+        for (int s = 0; s < kInFlight; ++s) got[s] = *reinterpret_cast<const float4*>(p.parts + ((int64_t)min(s0 + s, p.slices - 1) * p.M + place) * p.rank + first + rank);
+#pragma unroll
+        for (int s = 0; s < kInFlight; ++s) {
+            const bool some = s0 + s < p.slices;
+            v[0] += some ? got[s].x : 0.f; v[1] += some ? got[s].y : 0.f; v[2] += some ? got[s].z : 0.f; v[3] += some ? got[s].w : 0.f;
+        }
+    }
+    const int shift = shift_of(row_max16(fmaxf(fmaxf(finite_size(v[0]), finite_size(v[1])), fmaxf(finite_size(v[2]), finite_size(v[3])))));
+    if (4 * w >= ranks || blockIdx.x * 16 + (threadIdx.x >> 4) >= (unsigned)p.M) return;
+    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+    h4 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float y = v[e] * power_of_two(shift);
+        hi[e] = (_Float16)y;
+        lo[e] = low_part(y, hi[e]);
+    }
+    _Float16* to = reinterpret_cast<_Float16*>(p.h) + (int64_t)place * 2 * p.rank + 2 * first + rank;
+    *reinterpret_cast<h4*>(to) = hi;
+    *reinterpret_cast<h4*>(to + ranks) = lo;
+    if (w == 0) p.scales[(int64_t)place * p.chunks + z] = power_of_two(-shift);
+}
+
+constexpr int kExpandTiles = 4, kExpandWaves = 2;
 struct ExpandArgs {
     const __half *base, *b;                              // b [adapters, N, rank]
     __half* out;
     const __half* h;
     const float *scales, *adapter_scales;                // adapter_scales may be null
+    const float* parts;
     const int* head;
     const int4* tiles;
     const int* rows;
     int64_t base_stride, out_stride;
-    int M, adapters, N, rank, chunks, blocks;            // blocks of 64 channels for each wave
+    int M, adapters, N, rank, chunks, slices, blocks;    // blocks of 64 channels for each wave
 };
 
-// STEPS matrix instructions for the pairs of a chunk of ranks; WIDE: several chunks.
-template <int CT, int STEPS, bool WIDE>
-__global__ __launch_bounds__(64) void lora_expand_kernel(ExpandArgs p)
+// STEPS matrix instructions for the pairs of a chunk of ranks, which `FULL` fill; WIDE: several chunks.  SUM: the pairs are formed here from the
+// slices' sums, which for few rows takes less than to join them first.
+// Bound by base and out; B of an adapter comes from the L2 for all but its first tile.
+template <int CT, int STEPS, bool FULL, bool WIDE, bool SUM>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(WIDE ? 1 : kExpandWaves))) void lora_expand_kernel(ExpandArgs p)
 {
-    const int tile = blockIdx.x;
+    constexpr int kParts = SUM ? 1 : 64 / (16 * CT);     // workgroups to a tile: fewer rows to a wave, more waves that wait for memory
+    const int tile = blockIdx.y / kParts;
+    int4 t = p.tiles[tile];                              // (whatever it holds, beside the head)
     if (tile >= tiles_of(p.head, p.M, p.adapters)) return;
-    const int4 t = p.tiles[tile];
+    t.y += blockIdx.y % kParts * 16 * CT;
+    t.z -= blockIdx.y % kParts * 16 * CT;
+    if (t.z <= 0) return;
     const int lane = threadIdx.x, r16 = lane & 15, kb = lane >> 4;
     const bool in_place = p.base == p.out;
     if (t.x < 0 && in_place) return;
     const __half* from[CT];
     __half* to[CT];
-    bool there[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        there[c] = c * 16 + r16 < t.z;
         const int64_t row = p.rows[t.y + min(c * 16 + r16, t.z - 1)];
         from[c] = p.base + row * p.base_stride;
         to[c] = p.out + row * p.out_stride;
     }
-    uint4 hv[STEPS][CT];
+    uint4 hv[CT][STEPS];
     float scale[CT];
+    const float of_adapter = p.adapter_scales && t.x >= 0 ? p.adapter_scales[t.x] : 1.f;
     auto load_h = [&](int z) __attribute__((always_inline)) {
         const int ranks = min(p.rank - z * kRankChunk, kRankChunk);
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
             const int64_t place = t.y + min(c * 16 + r16, t.z - 1);
-            const __half* at = p.h + place * 2 * p.rank + 2 * z * kRankChunk;
-            scale[c] = p.scales[place * p.chunks + z] * (p.adapter_scales ? p.adapter_scales[t.x] : 1.f);
+            if constexpr (SUM) {
+                float v[STEPS][8], most = 0.f;
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) hv[s][c] = s * 32 + kb * 8 < 2 * ranks ? *reinterpret_cast<const uint4*>(at + s * 32 + kb * 8) : make_uint4(0, 0, 0, 0);
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[s][e] = 0.f;
+#pragma unroll 4
+                for (int q = 0; q < p.slices; ++q) {
+                    const float* at = p.parts + ((int64_t)q * p.M + place) * p.rank + z * kRankChunk;
+#pragma unroll
+                    for (int s = 0; s < STEPS; ++s) {
+                        const int pair = s * 32 + kb * 8, rank = pair < ranks ? pair : min(pair, 2 * ranks - 8) - ranks;
+                        const float4 a = *reinterpret_cast<const float4*>(at + rank), b = *reinterpret_cast<const float4*>(at + rank + 4);
+                        v[s][0] += a.x; v[s][1] += a.y; v[s][2] += a.z; v[s][3] += a.w;
+                        v[s][4] += b.x; v[s][5] += b.y; v[s][6] += b.z; v[s][7] += b.w;
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_size(v[s][e]));
+                const int shift = shift_of(max_other_half(max_other_row(most)));
+                scale[c] = power_of_two(-shift) * of_adapter;
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) {
+                    const int pair = s * 32 + kb * 8;
+                    _Float16 o[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float y = v[s][e] * power_of_two(shift);
+                        const _Float16 hi = (_Float16)y;
+                        o[e] = pair < ranks ? hi : low_part(y, hi);
+                        if (!FULL && pair >= 2 * ranks) o[e] = (_Float16)0.f;
+                    }
+                    hv[c][s] = __builtin_bit_cast(uint4, (h8){o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]});
+                }
+            } else {
+                const __half* at = p.h + place * 2 * p.rank + 2 * z * kRankChunk;
+                scale[c] = p.scales[place * p.chunks + z] * of_adapter;
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) {
+                    const int pair = s * 32 + kb * 8;
+                    hv[c][s] = *reinterpret_cast<const uint4*>(at + (FULL ? pair : min(pair, 2 * ranks - 8)));
+                    if (!FULL && pair >= 2 * ranks) hv[c][s] = make_uint4(0, 0, 0, 0);
+                }
+            }
         }
     };
     if (t.x >= 0 && !WIDE) load_h(0);
     const __half* b = p.b + (int64_t)max(t.x, 0) * p.N * p.rank;
+#pragma unroll 1
     for (int i = 0; i < p.blocks; ++i) {
-        const int n0 = (blockIdx.y * p.blocks + i) * 64;
+        const int n0 = (i * gridDim.x + blockIdx.x) * 64;            // neighbouring workgroups go through neighbouring channels together
         if (n0 >= p.N) return;
-        // a lane's results: 16 channels n0 + 16 kb .. of its row, 4 of each matrix product j
-        const int n = n0 + kb * 16;
+        // a lane's results: channels n .. n + 7 and n + 32 .. n + 39 of its row, 4 of each matrix product j, so that four lanes take 64 bytes of a row
+        // together (what lies behind the last channel is computed from the last ones' operands, and not stored)
+        const int n = n0 + kb * 8;
         uint4 bv[CT][2];
 #pragma unroll
         for (int c = 0; c < CT; ++c)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) bv[c][e] = there[c] && n + 8 * e < p.N ? *reinterpret_cast<const uint4*>(from[c] + n + 8 * e) : make_uint4(0, 0, 0, 0);
-        if (t.x < 0) {
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (there[c] && n + 8 * e < p.N) *reinterpret_cast<uint4*>(to[c] + n + 8 * e) = bv[c][e];
-            continue;
-        }
+            for (int e = 0; e < 2; ++e) bv[c][e] = *reinterpret_cast<const uint4*>(from[c] + min(n + 32 * e, p.N - 8));
         f4 sum[CT][4];
-        for (int z = 0; z < (WIDE ? p.chunks : 1); ++z) {
-            if (WIDE) load_h(z);
-            const int ranks = min(p.rank - z * kRankChunk, kRankChunk);
-            f4 acc[CT][4];
+        if (t.x >= 0) {
+#pragma unroll 1
+            for (int z = 0; z < (WIDE ? p.chunks : 1); ++z) {
+                if (WIDE) load_h(z);
+                const int ranks = min(p.rank - z * kRankChunk, kRankChunk);
+                uint4 w[STEPS][4];
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
+                for (int s = 0; s < STEPS; ++s) {
+                    if constexpr (FULL && STEPS % 2 == 0) {               // (16 STEPS ranks: the second half of the steps takes B as the first)
+                        if (s >= STEPS / 2) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[c][j] = (f4){0.f, 0.f, 0.f, 0.f};
+                            for (int j = 0; j < 4; ++j) w[s][j] = w[s - STEPS / 2][j];
+                            continue;
+                        }
+                    }
+                    const int pair = s * 32 + kb * 8, rank = pair < ranks ? pair : (FULL ? pair : min(pair, 2 * ranks - 8)) - ranks;
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                const int pair = s * 32 + kb * 8, rank = pair < ranks ? pair : pair - ranks;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int row = n0 + (r16 >> 2) * 16 + j * 4 + (r16 & 3);
-                    const uint4 w = pair < 2 * ranks ? *reinterpret_cast<const uint4*>(b + (int64_t)min(row, p.N - 1) * p.rank + z * kRankChunk + rank) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                    for (int c = 0; c < CT; ++c)
-                        acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, w), __builtin_bit_cast(h8, hv[s][c]), acc[c][j], 0, 0, 0);
+                    for (int j = 0; j < 4; ++j) {
+                        const int row = min(n0 + (j >> 1) * 32 + (r16 >> 2) * 8 + (j & 1) * 4 + (r16 & 3), p.N - 1);
+                        w[s][j] = *reinterpret_cast<const uint4*>(b + (int64_t)row * p.rank + z * kRankChunk + rank);
+                        if (!FULL && pair >= 2 * ranks) w[s][j] = make_uint4(0, 0, 0, 0);
+                    }
                 }
+                f4 acc[CT][4];
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int c = 0; c < CT; ++c)
+                            acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, w[s][j]), __builtin_bit_cast(h8, hv[c][s]), s ? acc[c][j] : (f4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int c = 0; c < CT; ++c)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) sum[c][j][x] = !WIDE || z == 0 ? acc[c][j][x] * scale[c] : fmaf(acc[c][j][x], scale[c], sum[c][j][x]);
             }
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) sum[c][j][x] = z == 0 ? acc[c][j][x] * scale[c] : fmaf(acc[c][j][x], scale[c], sum[c][j][x]);
         }
 #pragma unroll
         for (int c = 0; c < CT; ++c)
@@ -336,31 +410,51 @@ __global__ __launch_bounds__(64) void lora_expand_kernel(ExpandArgs p)
                 for (int k = 0; k < 4; ++k) {
                     const h2 o = __builtin_bit_cast(h2, old[k]);
                     const float y0 = (float)o.x + sum[c][2 * e + k / 2][2 * (k & 1)], y1 = (float)o.y + sum[c][2 * e + k / 2][2 * (k & 1) + 1];
-                    now[k] = __builtin_bit_cast(uint32_t, (h2){(_Float16)y0, (_Float16)y1});
+                    now[k] = t.x >= 0 ? __builtin_bit_cast(uint32_t, (h2){(_Float16)y0, (_Float16)y1}) : old[k];
                 }
-                if (there[c] && n + 8 * e < p.N) *reinterpret_cast<uint4*>(to[c] + n + 8 * e) = make_uint4(now[0], now[1], now[2], now[3]);
+                if (c * 16 + r16 < t.z && n + 32 * e < p.N) *reinterpret_cast<uint4*>(to[c] + n + 32 * e) = make_uint4(now[0], now[1], now[2], now[3]);
             }
     }
 }
 
-// Slices of K: workgroups enough to fill the chip, of 128 elements at least (a step of each wave).
+bool pair_first(int64_t M) { return tile_rows(M) == 64; }
+// Slices of K.  Few rows: workgroups enough to fill the chip twice, of 512 elements at least (four steps of each wave, which are in flight together).
+// Many rows: one workgroup to a compute unit; the tiles' sums are 16 KB a slice (4096 rows of 8192 elements and 64 ranks 33.8 us with 3 slices, 33.6 with 7,
+// 41 with 10, 77 with one; 1733 of 4096 and 8 ranks 9.1 with 7, 10.1 with 14, 10.5 with 3).
 int shrink_slices(int64_t M, int64_t K, int64_t rank, int64_t adapters)
 {
     const int64_t chunks = (rank + kRankChunk - 1) / kRankChunk, tiles = most_tiles(M, adapters);
-    if (tiles <= 0 || tiles * chunks > kMaxCounters) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(512 / (tiles * chunks), (K + 127) / 128));
+    if (tiles <= 0) return 1;
+    if (pair_first(M)) return (int)std::max<int64_t>(1, std::min<int64_t>(256 / (tiles * chunks), (K + 255) / 256));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / (tiles * chunks), (K + 511) / 512, 16}));
 }
 
-struct Layout { size_t scales, h, parts, all; };          // of the workspace, behind the counters
+typedef void (*ExpandKernel)(ExpandArgs);
+template <int STEPS, bool FULL, bool WIDE>
+ExpandKernel pick_expand(bool big) { return big ? lora_expand_kernel<kExpandTiles, STEPS, FULL, WIDE, false> : lora_expand_kernel<1, STEPS, FULL, WIDE, true>; }
+ExpandKernel pick_expand_of(int64_t rank, bool big)
+{
+    switch (rank / 8) {
+        case 1: return pick_expand<1, false, false>(big);
+        case 2: return pick_expand<1, true, false>(big);
+        case 3: return pick_expand<2, false, false>(big);
+        case 4: return pick_expand<2, true, false>(big);
+        case 5: return pick_expand<3, false, false>(big);
+        case 6: return pick_expand<3, true, false>(big);
+        case 7: return pick_expand<4, false, false>(big);
+        default: return pick_expand<4, true, false>(big);
+    }
+}
+
+struct Layout { size_t h, parts, all; };                  // of the workspace: scales, pairs, the slices' sums
 Layout workspace_layout(int64_t M, int64_t K, int64_t rank, int64_t adapters)
 {
     auto up = [](int64_t n) { return (size_t)((n + 255) / 256 * 256); };
-    const int64_t chunks = (rank + kRankChunk - 1) / kRankChunk, slices = shrink_slices(M, K, rank, adapters);
+    const int64_t chunks = (rank + kRankChunk - 1) / kRankChunk;
     Layout l;
-    l.scales = kCounterBytes;
-    l.h = l.scales + up(M * chunks * 4);
-    l.parts = l.h + up(M * rank * 4);
-    l.all = l.parts + (slices > 1 ? up(slices * M * rank * 4) : 0);
+    l.h = pair_first(M) ? up(M * chunks * 4) : 0;
+    l.parts = l.h + (pair_first(M) ? up(M * rank * 4) : 0);
+    l.all = l.parts + up(shrink_slices(M, K, rank, adapters) * M * rank * 4);
     return l;
 }
 
@@ -392,37 +486,39 @@ hipError_t launch_lora_add(const LoraAdd& l, hipStream_t s)
     a.head = static_cast<const int*>(l.plan);
     a.tiles = reinterpret_cast<const int4*>(a.head + kPlanHead);
     a.rows = a.head + kPlanHead + 4 * tiles;
-    a.counters = reinterpret_cast<int*>(ws);
-    a.scales = reinterpret_cast<float*>(ws + at.scales);
-    a.h = reinterpret_cast<__half*>(ws + at.h);
     a.parts = reinterpret_cast<float*>(ws + at.parts);
     a.x_stride = l.x_stride;
-    a.M = (int)l.M; a.adapters = (int)l.adapters; a.K = (int)l.K; a.rank = (int)l.rank; a.chunks = (int)chunks;
-    a.slice = (int)(((l.K + slices - 1) / slices + 31) / 32 * 32);
-    const bool big = tile_rows(l.M) == 64;
+    a.M = (int)l.M; a.adapters = (int)l.adapters; a.K = (int)l.K; a.rank = (int)l.rank;
+    a.slice = (int)(((l.K + slices - 1) / slices + 127) / 128 * 128);
+    const bool big = pair_first(l.M);
     const int rt = l.rank <= 16 ? 1 : l.rank <= 32 ? 2 : 4;
     const int64_t blocks64 = (l.N + 63) / 64;
     // blocks of 64 channels for each wave, which keeps h meanwhile
-    const int64_t each = std::max<int64_t>(1, std::min<int64_t>(8, tiles * blocks64 / 4096)), groups = (blocks64 + each - 1) / each;
-    if (tiles >= (int64_t)1 << 22 || tiles * slices * chunks >= (int64_t)1 << 24 || tiles * groups >= (int64_t)1 << 24 || groups > 65535) return hipErrorInvalidValue;
+    const int64_t of_tile = big ? 4 / kExpandTiles : 1;
+    const int64_t each = std::max<int64_t>(1, std::min<int64_t>(8, tiles * of_tile * blocks64 / 8192)), groups = (blocks64 + each - 1) / each;
+    if (tiles >= (int64_t)1 << 22 || tiles * slices * chunks >= (int64_t)1 << 24 || tiles * of_tile * groups >= (int64_t)1 << 24) return hipErrorInvalidValue;
     const dim3 grid((unsigned)tiles, (unsigned)slices, (unsigned)chunks);
     auto* shrink = big ? (rt == 1 ? lora_shrink_kernel<4, 1> : rt == 2 ? lora_shrink_kernel<4, 2> : lora_shrink_kernel<4, 4>)
                        : (rt == 1 ? lora_shrink_kernel<1, 1> : rt == 2 ? lora_shrink_kernel<1, 2> : lora_shrink_kernel<1, 4>);
     shrink<<<grid, 256, 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    __half* h = reinterpret_cast<__half*>(ws + at.h);
+    float* scales = reinterpret_cast<float*>(ws);
+    if (big) {
+        PairArgs q{};
+        q.parts = a.parts; q.h = h; q.scales = scales;
+        q.M = (int)l.M; q.rank = (int)l.rank; q.chunks = (int)chunks; q.slices = (int)slices;
+        lora_pair_kernel<<<dim3((unsigned)((l.M + 15) / 16), (unsigned)chunks), 256, 0, s>>>(q);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
     ExpandArgs e{};
     e.base = static_cast<const __half*>(l.base); e.b = static_cast<const __half*>(l.b); e.out = static_cast<__half*>(l.out);
-    e.h = a.h; e.scales = a.scales; e.adapter_scales = l.scales;
+    e.h = h; e.scales = scales; e.parts = a.parts; e.adapter_scales = l.scales;
     e.head = a.head; e.tiles = a.tiles; e.rows = a.rows;
     e.base_stride = l.base_stride; e.out_stride = l.out_stride;
-    e.M = (int)l.M; e.adapters = (int)l.adapters; e.N = (int)l.N; e.rank = (int)l.rank; e.chunks = (int)chunks; e.blocks = (int)each;
-    const int steps = chunks > 1 ? 4 : (int)((2 * l.rank + 31) / 32);
-    auto* expand = chunks > 1   ? (big ? lora_expand_kernel<4, 4, true> : lora_expand_kernel<1, 4, true>)
-                   : steps == 1 ? (big ? lora_expand_kernel<4, 1, false> : lora_expand_kernel<1, 1, false>)
-                   : steps == 2 ? (big ? lora_expand_kernel<4, 2, false> : lora_expand_kernel<1, 2, false>)
-                   : steps == 3 ? (big ? lora_expand_kernel<4, 3, false> : lora_expand_kernel<1, 3, false>)
-                                : (big ? lora_expand_kernel<4, 4, false> : lora_expand_kernel<1, 4, false>);
-    expand<<<dim3((unsigned)tiles, (unsigned)groups), 64, 0, s>>>(e);
+    e.M = (int)l.M; e.adapters = (int)l.adapters; e.N = (int)l.N; e.rank = (int)l.rank; e.chunks = (int)chunks; e.slices = (int)slices; e.blocks = (int)each;
+    auto* expand = chunks > 1 ? pick_expand<4, false, true>(big) : pick_expand_of(l.rank, big);
+    expand<<<dim3((unsigned)groups, (unsigned)(tiles * of_tile)), 64, 0, s>>>(e);
     return hipGetLastError();
 }
 

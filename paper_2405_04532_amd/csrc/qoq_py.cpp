@@ -764,7 +764,6 @@ PyObject* lora_add(PyObject*, PyObject* const* a, Py_ssize_t n)    // base, x, a
             scratch = new_like(*base, {(int64_t)need}, at::kByte);
             ws.ptr = scratch.data_ptr();
             ws.bytes = need;
-            if (!call([&] { return qoq_gemm_workspace_prepare(ws.ptr, std::min(need, qoq::kCounterBytes), s); })) return nullptr;
         }
     }
     const void *bp = base->data_ptr(), *xp = x->data_ptr(), *ap = la->data_ptr(), *lbp = lb->data_ptr(), *pp = plan->data_ptr();
