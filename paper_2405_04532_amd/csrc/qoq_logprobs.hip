@@ -126,11 +126,11 @@ __device__ __forceinline__ Sums all_lanes(Sums s)                    // of the w
     return s;
 }
 
-// A (value, index) at or in front of which there are n of the 64 J (key, index) that a wave's lanes hold, and few more: at most n / 2 + 4,
-// unless there are fewer than n at all (key 0: none).  The key's bits are settled from the highest one down, by ballots, then where more than that
+// A (value, index) at or in front of which there are n of the 64 J (key, index) that a wave's lanes hold, and at most `most`, unless there are
+// no more at all (key 0: none).  The key's bits are settled from the highest one down, by ballots, then where more than that
 // are equal the index's, until few enough are left.
 template <class T, int J>
-__device__ __forceinline__ void threshold(const uint32_t (&key)[J], const int (&index)[J], int n, float& tau_v, int& tau_i)
+__device__ __forceinline__ void threshold(const uint32_t (&key)[J], const int (&index)[J], int n, int most, float& tau_v, int& tau_i)
 {
     unsigned long long alive[J], part[J];
     int left = 0, in_front = 0, need = n;                            // lanes that are not settled, those in front of them
@@ -142,7 +142,6 @@ __device__ __forceinline__ void threshold(const uint32_t (&key)[J], const int (&
     tau_v = -__builtin_inff();
     tau_i = 0x7FFFFFFF;
     if (left < n) return;
-    const int most = n + n / 2 + 4;
     // goes on with those of a part if they are enough, else with the others behind them
     auto settle = [&]() __attribute__((always_inline)) {
         int c = 0;
@@ -366,7 +365,7 @@ __global__ __launch_bounds__(kRowThreads) void logprobs_kernel(LogprobArgs p)
             key[w] = sh.best_key[w * 64 + lane];
             at_latest[w] = sh.latest[w * 64 + lane];
         }
-        threshold<T, kRowWaves>(key, at_latest, n, tau_v, tau_i);
+        threshold<T, kRowWaves>(key, at_latest, n, n + n / 2 + 4, tau_v, tau_i);
         if (best_vector >= 0 && (best > tau_v || (best == tau_v && best_vector * N - before <= tau_i))) sh.lane[atomicAdd(&sh.lanes, 1)] = tid;
         __syncthreads();
         const int lanes = sh.lanes;
@@ -456,7 +455,7 @@ __global__ __launch_bounds__(kRowThreads) void logprobs_join_kernel(LogprobArgs 
         int tau_i;
         const uint32_t key[1] = {k < each && __float_as_int(head.y) >= 0 ? Logit<T>::key(head.x) : 0};
         const int index[1] = {__float_as_int(head.y)};
-        threshold<T, 1>(key, index, n, tau_v, tau_i);
+        threshold<T, 1>(key, index, n, n, tau_v, tau_i);      // (exactly: behind each of these stands the rest of its list)
         if (tid == 0) sh.found = 0;
         __syncthreads();
 #pragma unroll 1
