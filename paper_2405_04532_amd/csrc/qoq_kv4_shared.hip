@@ -29,6 +29,10 @@ constexpr int kPrefixColumns = 16 * kColumnTiles;
 constexpr int kWide = 2;                                 // the same where a prefix's columns are many and a workgroup's waves have columns of their own
 constexpr int kWideWorkgroups = 512;                     // that share the prefixes then: two on a compute unit
 constexpr int kLeastRun = 4;                             // pages of a run
+// Units of the wide form (a page for 128 columns) from which it is taken.  Its pages go through LDS one after the other and a run's first costs three:
+// 64 sequences of 32 / 8 heads behind 2000 tokens 33.4 us, 19.5 with tokens shared by the waves, behind 8000 (2000 units) 36.8 and 35.1, behind 16000 49.6
+// and 57.6; 151 of 40 / 8 behind 2000 (1536 units) 41.0 and 35.7, behind 4000 47.7 and 54.8.  Only the device knows the prefixes' lengths.
+constexpr int kWideUnits = 2200;
 
 struct SharedArgs {
     const uint8_t* pool;
@@ -38,7 +42,10 @@ struct SharedArgs {
     __half* out;
     int64_t q_stride;
     uint32_t pages;
-    int width, B, G, Hkv, R, prefix_parts, own_parts, prefix_workgroups;
+    int width, B, G, Hkv, R;
+    int prefix_slots, own_parts;                         // slots of a head for its prefix, and for its own tokens
+    int prefix_parts, wide_parts;                        // of a tile of columns of a prefix, by the waves' way of sharing it
+    int prefix_workgroups;                               // of the wide form
     uint32_t prefix_blocks, ratio_magic;                 // ceil(2^32 / R)
 };
 // n / R for n < 2^28
@@ -560,15 +567,18 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& p, const Work& k, 
 #pragma unroll
                 for (int c = 0; c < CT; ++c) {
                     const int end_c = (id < p.pages ? limit[c] : 0) - i * kPageTokens - half * 32 - 4 * kb;
-                    float top = -1e30f;
+                    float top = -1e30f, largest = 0.f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const bool seen = (e >> 2) * 16 + (e & 3) < end_c;
                         t[c][e] = seen ? d[c][e >> 2][e & 3] * ks[e] : -1e30f;
                         scale[c][e] = seen ? vs[e] : 0.f;
                         top = fmaxf(top, t[c][e]);
+                        largest = fmaxf(largest, scale[c][e]);
                     }
-                    const float m_new = max_other_half(max_other_row(fmaxf(m[c], top + (fabsf(top) < 0x1p23f ? below + kSpare : 0.f))));
+                    // (where a column does not see all, its reference rests on what it sees: the page's largest scale may be another token's)
+                    const float room = (partly ? (float)(min(max((int)(__float_as_uint(largest) >> 23) - 112, 0), 31) - 29) : below) + kSpare;
+                    const float m_new = max_other_half(max_other_row(fmaxf(m[c], top + (fabsf(top) < 0x1p23f ? room : 0.f))));
                     const float alpha = __builtin_amdgcn_exp2f(m[c] - m_new);
                     m[c] = m_new;
                     l[c] *= alpha;
@@ -687,7 +697,7 @@ __device__ __forceinline__ void count_units(const SharedArgs& p, GroupLanes<TILE
         f.all += __builtin_amdgcn_readlane(g.upto, 63);
         longest = max(longest, largest_of_lanes(g.pages));
     }
-    f.run = max(max((f.all + p.prefix_workgroups - 1) / p.prefix_workgroups, min(kLeastRun, max(longest, 1))), (longest + p.prefix_parts - 3) / (p.prefix_parts - 2));
+    f.run = max(max((f.all + p.prefix_workgroups - 1) / p.prefix_workgroups, min(kLeastRun, max(longest, 1))), (longest + p.wide_parts - 3) / (p.wide_parts - 2));
 }
 template <int TILE>
 __device__ __forceinline__ void find_unit(const SharedArgs& p, GroupLanes<TILE>& g, Units& f, int unit)
@@ -704,6 +714,51 @@ __device__ __forceinline__ void find_unit(const SharedArgs& p, GroupLanes<TILE>&
     }
 }
 
+// The work of this workgroup where the waves share the tokens of kPrefixColumns: false if there is none.
+__device__ __forceinline__ bool narrow_work(const SharedArgs& p, Work& k)
+{
+    const int lane = threadIdx.x & 63, most = p.width * kPageTokens;
+    const uint32_t of_tile = (uint32_t)p.Hkv * p.prefix_parts, rest = blockIdx.x % of_tile;
+    int tile = blockIdx.x / of_tile;
+    k.hk = rest % p.Hkv;
+    k.part = rest / p.Hkv;
+    // the tile's group: tiles of the groups in front of each are counted 64 groups at a time
+    bool found = false;
+    for (int g0 = 0; g0 < p.G && !found; g0 += 64) {
+        const int g = g0 + lane;
+        int first = 0, columns = 0, tokens = 0;
+        if (g < p.G) {
+            first = min(max(p.cu[g], 0), p.B);
+            columns = max(min(p.cu[g + 1], p.B) - first, 0) * p.R;
+            tokens = min(max(p.prefix_lens[g], 0), most);
+        }
+        const int tiles = tokens ? (columns + kPrefixColumns - 1) / kPrefixColumns : 0;
+        int upto = tiles;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += v;
+        }
+        const unsigned long long who = __builtin_amdgcn_ballot_w64(upto > tile);
+        if (who) {
+            const int f = __builtin_ctzll(who);
+            const int at = tile - (__shfl(upto, f, 64) - __shfl(tiles, f, 64));
+            const int group_first = __builtin_amdgcn_readfirstlane(__shfl(first, f, 64));
+            k.hi = __builtin_amdgcn_readfirstlane(__shfl(tokens, f, 64));
+            k.columns = __builtin_amdgcn_readfirstlane(min(__shfl(columns, f, 64) - at * kPrefixColumns, kPrefixColumns));
+            k.first = group_first;
+            k.column0 = __builtin_amdgcn_readfirstlane(at * kPrefixColumns);
+            k.pages_of = p.table + (int64_t)group_first * p.width;
+            found = true;
+        } else {
+            tile -= __shfl(upto, 63, 64);
+        }
+    }
+    if (!found) return false;
+    k.parts = attending((k.hi + kChunk - 1) / kChunk, p.prefix_parts);
+    k.slot = k.part;
+    return k.part < k.parts;
+}
+
 // WIDE: column tiles of a wave where the prefix's columns are many, 0 where a workgroup's waves share the tokens of kPrefixColumns
 template <int PK, int WIDE>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void shared_decode_kernel(SharedArgs p)
@@ -714,7 +769,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     const int lane = threadIdx.x & 63;
     const int most = p.width * kPageTokens;
     Work k{};
-    k.total_slots = p.prefix_parts + p.own_parts;
+    k.total_slots = p.prefix_slots + p.own_parts;
     if (blockIdx.x < p.prefix_blocks) {
         if constexpr (WIDE != 0) {
             constexpr int kTile = 64 * WIDE;
@@ -723,6 +778,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
             Units f;
             GroupLanes<kTile> g;
             count_units<kTile>(p, g, f, -1);
+            if (f.all < kWideUnits) {
+                if (!narrow_work(p, k)) return;
+                attend<kColumnTiles, 1, true>(p, k, s_part);
+                return;
+            }
+            if ((int)blockIdx.x >= p.prefix_workgroups) return;
             int unit = w * f.run;
             const int end = min(unit + f.run, f.all);
 #pragma unroll 1
@@ -743,45 +804,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
             }
             return;
         } else {
-            const uint32_t of_tile = (uint32_t)p.Hkv * p.prefix_parts, rest = blockIdx.x % of_tile;
-            int tile = blockIdx.x / of_tile;
-            k.hk = rest % p.Hkv;
-            k.part = rest / p.Hkv;
-            // the tile's group: tiles of the groups in front of each are counted 64 groups at a time
-            bool found = false;
-            for (int g0 = 0; g0 < p.G && !found; g0 += 64) {
-                const int g = g0 + lane;
-                int first = 0, columns = 0, tokens = 0;
-                if (g < p.G) {
-                    first = min(max(p.cu[g], 0), p.B);
-                    columns = max(min(p.cu[g + 1], p.B) - first, 0) * p.R;
-                    tokens = min(max(p.prefix_lens[g], 0), most);
-                }
-                const int tiles = tokens ? (columns + kPrefixColumns - 1) / kPrefixColumns : 0;
-                int upto = tiles;
-                for (int o = 1; o < 64; o <<= 1) {
-                    const int v = __shfl_up(upto, o, 64);
-                    if (lane >= o) upto += v;
-                }
-                const unsigned long long who = __builtin_amdgcn_ballot_w64(upto > tile);
-                if (who) {
-                    const int f = __builtin_ctzll(who);
-                    const int at = tile - (__shfl(upto, f, 64) - __shfl(tiles, f, 64));
-                    const int group_first = __builtin_amdgcn_readfirstlane(__shfl(first, f, 64));
-                    k.hi = __builtin_amdgcn_readfirstlane(__shfl(tokens, f, 64));
-                    k.columns = __builtin_amdgcn_readfirstlane(min(__shfl(columns, f, 64) - at * kPrefixColumns, kPrefixColumns));
-                    k.first = group_first;
-                    k.column0 = __builtin_amdgcn_readfirstlane(at * kPrefixColumns);
-                    k.pages_of = p.table + (int64_t)group_first * p.width;
-                    found = true;
-                } else {
-                    tile -= __shfl(upto, 63, 64);
-                }
-            }
-            if (!found) return;
-            k.parts = attending((k.hi + kChunk - 1) / kChunk, p.prefix_parts);
-            if (k.part >= k.parts) return;
-            k.slot = k.part;
+            if (!narrow_work(p, k)) return;
             attend<kColumnTiles, 1, true>(p, k, s_part);
         }
     } else {
@@ -797,7 +820,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
         k.pages_of = p.table + (int64_t)b * p.width;
         k.first = b;
         k.columns = p.R;
-        k.slot = p.prefix_parts + k.part;
+        k.slot = p.prefix_slots + k.part;
         attend<1, PK, false>(p, k, s_part);
     }
 }
@@ -819,7 +842,9 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
         GroupLanes<64 * WIDE> g;
         count_units<64 * WIDE>(p, g, f, b);
         P = f.tokens;
-        if (P && L) {
+        if (P && L && f.all < kWideUnits) {
+            n_prefix = attending((P + kChunk - 1) / kChunk, p.prefix_parts);
+        } else if (P && L) {
             const int h = (int)(row % H), hk = h / p.R, tile = ((b - f.first) * p.R + h % p.R) / (64 * WIDE);
             const int unit = f.before + (hk * f.tiles + tile) * f.pages;
             n_prefix = (unit + f.pages - 1) / f.run - unit / f.run + 1;
@@ -830,9 +855,9 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
     }
     const int lo = min(P, L);
     const int n_own = L > lo ? attending((L + kChunk - 1) / kChunk - lo / kChunk, p.own_parts) : 0;
-    const int total = p.prefix_parts + p.own_parts, n = n_prefix + n_own;
+    const int total = p.prefix_slots + p.own_parts, n = n_prefix + n_own;
     const float* parts = p.parts + row * total * kPartial;
-    auto slot = [&](int i) { return i < n_prefix ? i : p.prefix_parts + i - n_prefix; };
+    auto slot = [&](int i) { return i < n_prefix ? i : p.prefix_slots + i - n_prefix; };
     float f[2], den = 0.f, top = -1e29f;
     float2 ml[2];
 #pragma unroll
@@ -868,7 +893,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
 }
 
 bool wide_prefix(int64_t B, int64_t G, int64_t R) { return G && B * R / G >= 64; }
-int64_t prefix_tiles(int64_t B, int64_t G, int64_t R) { return G ? B * R / (wide_prefix(B, G, R) ? 64 * kWide : kPrefixColumns) + G : 0; }
+int64_t prefix_tiles(int64_t B, int64_t G, int64_t R, int64_t columns) { return G ? B * R / columns + G : 0; }
 // Workgroups that stand by for each tile of columns of a prefix and KV head, and for each sequence and KV head: two to a compute unit.
 int parts_for(int64_t items, int64_t width)
 {
@@ -876,19 +901,19 @@ int parts_for(int64_t items, int64_t width)
     return (int)std::max<int64_t>(1, std::min<int64_t>({kMaxParts, 512 / items, (2 * width + 2 * kWaves - 1) / (2 * kWaves)}));
 }
 
-// Parts of a tile of columns of a prefix: twice what an even share of the workgroups comes to, and the pieces at its ends.
-int prefix_parts(int64_t B, int64_t G, int64_t R, int64_t Hkv, int64_t width)
+// Parts of a tile of columns of a prefix where the waves share its tokens, and where they have columns of their own: twice what an even share of
+// the workgroups comes to, and the pieces at its ends.
+int prefix_parts(int64_t B, int64_t G, int64_t R, int64_t Hkv, int64_t width) { return parts_for(prefix_tiles(B, G, R, kPrefixColumns) * Hkv, width); }
+int wide_parts(int64_t B, int64_t G, int64_t R, int64_t Hkv)
 {
-    const int64_t items = prefix_tiles(B, G, R) * Hkv;
-    if (!wide_prefix(B, G, R)) return parts_for(items, width);
-    return (int)std::min<int64_t>(kMaxParts, 2 * kWideWorkgroups / items + 3);
+    return wide_prefix(B, G, R) ? (int)std::min<int64_t>(kMaxParts, 2 * kWideWorkgroups / (prefix_tiles(B, G, R, 64 * kWide) * Hkv) + 3) : 0;
 }
 
 }  // namespace
 
 size_t shared_decode_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t width, int64_t G)
 {
-    const int64_t slots = prefix_parts(B, G, H / Hkv, Hkv, width) + parts_for(B * Hkv, width);
+    const int64_t slots = std::max(prefix_parts(B, G, H / Hkv, Hkv, width), wide_parts(B, G, H / Hkv, Hkv)) + parts_for(B * Hkv, width);
     return (size_t)(B * H * slots) * kPartial * sizeof(float);
 }
 
@@ -904,13 +929,15 @@ hipError_t launch_shared_decode(const void* q, int64_t q_stride, const uint8_t* 
     p.pages = (uint32_t)pages; p.width = (int)width; p.B = (int)B; p.G = (int)G; p.Hkv = (int)Hkv; p.R = (int)(H / Hkv);
     const bool wide = wide_prefix(B, G, p.R);
     p.prefix_parts = prefix_parts(B, G, p.R, Hkv, width);
+    p.wide_parts = wide_parts(B, G, p.R, Hkv);
+    p.prefix_slots = std::max(p.prefix_parts, p.wide_parts);
     p.own_parts = parts_for(B * Hkv, width);
     p.prefix_workgroups = kWideWorkgroups;
     p.ratio_magic = (uint32_t)((((uint64_t)1 << 32) + p.R - 1) / p.R);
-    const int64_t prefix_blocks = wide ? kWideWorkgroups : prefix_tiles(B, G, p.R) * Hkv * p.prefix_parts;
+    const int64_t prefix_blocks = std::max<int64_t>(wide ? kWideWorkgroups : 0, prefix_tiles(B, G, p.R, kPrefixColumns) * Hkv * p.prefix_parts);
     const int64_t blocks = prefix_blocks + B * Hkv * p.own_parts, joins = (B * H + 3) / 4;
     if (blocks >= (int64_t)1 << 24 || joins >= (int64_t)1 << 24) return hipErrorInvalidValue;    // 2^32 threads
-    if (wide && prefix_tiles(B, G, p.R) * Hkv * width >= (int64_t)1 << 31) return hipErrorInvalidValue;  // units of work, counted in 32 bits
+    if (wide && prefix_tiles(B, G, p.R, 64 * kWide) * Hkv * width >= (int64_t)1 << 31) return hipErrorInvalidValue;  // units of work, counted in 32 bits
     p.prefix_blocks = (uint32_t)prefix_blocks;
     const int PK = p.R <= 8 ? 2 : 1;
     auto* kernel = PK == 2 ? (wide ? shared_decode_kernel<2, kWide> : shared_decode_kernel<2, 0>) : (wide ? shared_decode_kernel<1, kWide> : shared_decode_kernel<1, 0>);

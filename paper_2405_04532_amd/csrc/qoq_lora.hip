@@ -252,7 +252,6 @@ __global__ __launch_bounds__(256) void lora_pair_kernel(PairArgs p)
     if (w == 0) p.scales[(int64_t)place * p.chunks + z] = power_of_two(-shift);
 }
 
-constexpr int kExpandTiles = 4, kExpandWaves = 2;
 struct ExpandArgs {
     const __half *base, *b;                              // b [adapters, N, rank]
     __half* out;
@@ -270,15 +269,11 @@ struct ExpandArgs {
 // slices' sums, which for few rows takes less than to join them first.
 // Bound by base and out; B of an adapter comes from the L2 for all but its first tile.
 template <int CT, int STEPS, bool FULL, bool WIDE, bool SUM>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(WIDE ? 1 : kExpandWaves))) void lora_expand_kernel(ExpandArgs p)
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(WIDE ? 1 : 2))) void lora_expand_kernel(ExpandArgs p)
 {
-    constexpr int kParts = SUM ? 1 : 64 / (16 * CT);     // workgroups to a tile: fewer rows to a wave, more waves that wait for memory
-    const int tile = blockIdx.y / kParts;
-    int4 t = p.tiles[tile];                              // (whatever it holds, beside the head)
+    const int tile = blockIdx.y;
+    const int4 t = p.tiles[tile];                        // (whatever it holds, beside the head)
     if (tile >= tiles_of(p.head, p.M, p.adapters)) return;
-    t.y += blockIdx.y % kParts * 16 * CT;
-    t.z -= blockIdx.y % kParts * 16 * CT;
-    if (t.z <= 0) return;
     const int lane = threadIdx.x, r16 = lane & 15, kb = lane >> 4;
     const bool in_place = p.base == p.out;
     if (t.x < 0 && in_place) return;
@@ -417,7 +412,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(WIDE ? 1 : k
     }
 }
 
-bool pair_first(int64_t M) { return tile_rows(M) == 64; }
+bool large_tiles(int64_t M) { return tile_rows(M) == 64; }
 // Slices of K.  Few rows: workgroups enough to fill the chip twice, of 512 elements at least (four steps of each wave, which are in flight together).
 // Many rows: one workgroup to a compute unit; the tiles' sums are 16 KB a slice (4096 rows of 8192 elements and 64 ranks 33.8 us with 3 slices, 33.6 with 7,
 // 41 with 10, 77 with one; 1733 of 4096 and 8 ranks 9.1 with 7, 10.1 with 14, 10.5 with 3).
@@ -425,14 +420,26 @@ int shrink_slices(int64_t M, int64_t K, int64_t rank, int64_t adapters)
 {
     const int64_t chunks = (rank + kRankChunk - 1) / kRankChunk, tiles = most_tiles(M, adapters);
     if (tiles <= 0) return 1;
-    if (pair_first(M)) return (int)std::max<int64_t>(1, std::min<int64_t>(256 / (tiles * chunks), (K + 255) / 256));
+    if (large_tiles(M)) return (int)std::max<int64_t>(1, std::min<int64_t>(256 / (tiles * chunks), (K + 255) / 256));
     return (int)std::max<int64_t>(1, std::min<int64_t>({512 / (tiles * chunks), (K + 511) / 512, 16}));
 }
 
+// Whether a launch of its own forms the pairs: where a wave of the second product would read more than 16 KB of sums for them (473 rows of 32 ranks beside
+// 8192 x 8192 in 30 tiles of 15 slices 41.0 us, 18.0 with the launch; 64 rows of 16 ranks beside 6144 x 4096 8.4 and 10.0).
+bool pair_first(int64_t M, int64_t K, int64_t rank, int64_t adapters)
+{
+    return large_tiles(M) || shrink_slices(M, K, rank, adapters) * rank > 256;
+}
+
 typedef void (*ExpandKernel)(ExpandArgs);
+struct Shape { bool big, pairs; };
 template <int STEPS, bool FULL, bool WIDE>
-ExpandKernel pick_expand(bool big) { return big ? lora_expand_kernel<kExpandTiles, STEPS, FULL, WIDE, false> : lora_expand_kernel<1, STEPS, FULL, WIDE, true>; }
-ExpandKernel pick_expand_of(int64_t rank, bool big)
+ExpandKernel pick_expand(Shape s)
+{
+    if (s.big) return lora_expand_kernel<4, STEPS, FULL, WIDE, false>;
+    return s.pairs ? lora_expand_kernel<1, STEPS, FULL, WIDE, false> : lora_expand_kernel<1, STEPS, FULL, WIDE, true>;
+}
+ExpandKernel pick_expand_of(int64_t rank, Shape big)
 {
     switch (rank / 8) {
         case 1: return pick_expand<1, false, false>(big);
@@ -452,8 +459,9 @@ Layout workspace_layout(int64_t M, int64_t K, int64_t rank, int64_t adapters)
     auto up = [](int64_t n) { return (size_t)((n + 255) / 256 * 256); };
     const int64_t chunks = (rank + kRankChunk - 1) / kRankChunk;
     Layout l;
-    l.h = pair_first(M) ? up(M * chunks * 4) : 0;
-    l.parts = l.h + (pair_first(M) ? up(M * rank * 4) : 0);
+    const bool pairs = pair_first(M, K, rank, adapters);
+    l.h = pairs ? up(M * chunks * 4) : 0;
+    l.parts = l.h + (pairs ? up(M * rank * 4) : 0);
     l.all = l.parts + up(shrink_slices(M, K, rank, adapters) * M * rank * 4);
     return l;
 }
@@ -490,13 +498,12 @@ hipError_t launch_lora_add(const LoraAdd& l, hipStream_t s)
     a.x_stride = l.x_stride;
     a.M = (int)l.M; a.adapters = (int)l.adapters; a.K = (int)l.K; a.rank = (int)l.rank;
     a.slice = (int)(((l.K + slices - 1) / slices + 127) / 128 * 128);
-    const bool big = pair_first(l.M);
+    const bool big = large_tiles(l.M), pairs = pair_first(l.M, l.K, l.rank, l.adapters);
     const int rt = l.rank <= 16 ? 1 : l.rank <= 32 ? 2 : 4;
     const int64_t blocks64 = (l.N + 63) / 64;
     // blocks of 64 channels for each wave, which keeps h meanwhile
-    const int64_t of_tile = big ? 4 / kExpandTiles : 1;
-    const int64_t each = std::max<int64_t>(1, std::min<int64_t>(8, tiles * of_tile * blocks64 / 8192)), groups = (blocks64 + each - 1) / each;
-    if (tiles >= (int64_t)1 << 22 || tiles * slices * chunks >= (int64_t)1 << 24 || tiles * of_tile * groups >= (int64_t)1 << 24) return hipErrorInvalidValue;
+    const int64_t each = std::max<int64_t>(1, std::min<int64_t>(8, tiles * blocks64 / 8192)), groups = (blocks64 + each - 1) / each;
+    if (tiles >= (int64_t)1 << 22 || tiles * slices * chunks >= (int64_t)1 << 24 || tiles * groups >= (int64_t)1 << 24) return hipErrorInvalidValue;
     const dim3 grid((unsigned)tiles, (unsigned)slices, (unsigned)chunks);
     auto* shrink = big ? (rt == 1 ? lora_shrink_kernel<4, 1> : rt == 2 ? lora_shrink_kernel<4, 2> : lora_shrink_kernel<4, 4>)
                        : (rt == 1 ? lora_shrink_kernel<1, 1> : rt == 2 ? lora_shrink_kernel<1, 2> : lora_shrink_kernel<1, 4>);
@@ -504,7 +511,7 @@ hipError_t launch_lora_add(const LoraAdd& l, hipStream_t s)
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     __half* h = reinterpret_cast<__half*>(ws + at.h);
     float* scales = reinterpret_cast<float*>(ws);
-    if (big) {
+    if (pairs) {
         PairArgs q{};
         q.parts = a.parts; q.h = h; q.scales = scales;
         q.M = (int)l.M; q.rank = (int)l.rank; q.chunks = (int)chunks; q.slices = (int)slices;
@@ -517,8 +524,8 @@ hipError_t launch_lora_add(const LoraAdd& l, hipStream_t s)
     e.head = a.head; e.tiles = a.tiles; e.rows = a.rows;
     e.base_stride = l.base_stride; e.out_stride = l.out_stride;
     e.M = (int)l.M; e.adapters = (int)l.adapters; e.N = (int)l.N; e.rank = (int)l.rank; e.chunks = (int)chunks; e.slices = (int)slices; e.blocks = (int)each;
-    auto* expand = chunks > 1 ? pick_expand<4, false, true>(big) : pick_expand_of(l.rank, big);
-    expand<<<dim3((unsigned)groups, (unsigned)(tiles * of_tile)), 64, 0, s>>>(e);
+    auto* expand = chunks > 1 ? pick_expand<4, false, true>({big, pairs}) : pick_expand_of(l.rank, {big, pairs});
+    expand<<<dim3((unsigned)groups, (unsigned)tiles), 64, 0, s>>>(e);
     return hipGetLastError();
 }
 

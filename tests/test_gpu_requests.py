@@ -163,6 +163,76 @@ def test_shared_by_workgroups(B, H, Hkv, prefix, own):
         s.call(q, workspace=ws[:need - 16])
 
 
+def _check_some(s, out, q, lens, pick, bounds):
+    """The bound of _Batch.check for some of the sequences; bounds: (first, behind the last, prefix) of the groups."""
+    H, R = q.shape[1], q.shape[1] // s.Hkv
+    of = {b: (a, p) for a, e, p in bounds for b in range(a, e)}
+    qd, got = q.cpu().numpy().astype(np.float64), out.cpu().numpy().astype(np.float64)
+    read = lambda i, t: s.read(of.get(pick[i], (pick[i], 0))[0] if t < of.get(pick[i], (0, 0))[1] else pick[i], t)
+    for i, (ref, spread, k) in enumerate(requests.shared_attention(qd[pick], read, [lens[b] for b in pick], [0], [])):
+        b = pick[i]
+        e = max([float((np.abs(k[:, h // R]) @ np.abs(qd[b, h])).max()) for h in range(H)] if len(k) else [0.0]) * 130 * 2.0 ** -24 / np.sqrt(128.0)
+        tol = 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2 * e + 2.0 ** -20 + (len(k) + 160) * 2.0 ** -24) * spread + 15 * len(k) * 2.0 ** -25 + 2.0 ** -25
+        assert (np.abs(got[b] - ref) <= tol).all(), (b, float((np.abs(got[b] - ref) / tol).max()))
+
+
+@pytest.mark.parametrize("H,Hkv,groups,B", [
+    (32, 2, [(0, 256, 2176)], 256), (32, 2, [(0, 256, 2177)], 256), (32, 2, [(0, 255, 2300)], 256),     # 34, 35 and 36 pages for 64 tiles of 128 columns
+    (9, 1, [(1, 600, 3361)], 601),                                                                      # heads that do not divide a tile
+    (32, 8, [(2, 120, 2500), (120, 121, 100), (121, 290, 2943), (290, 299, 0)], 300)])
+def test_shared_of_many_sequences_behind_long_prefixes(H, Hkv, groups, B):
+    of = {b: p for a, e, p in groups for b in range(a, e)}
+    lens = [of.get(b, 0) + (b * 7) % 90 for b in range(B)]
+    for a, e, p in groups:                                                   # members without tokens, with one, and that end inside the prefix or with it
+        for b, n in zip(range(a + 1, e), (0, 1, p // 2, p // 2 + 1, p - 1, p)):
+            lens[b] = max(n, 0)
+    s = _Batch(groups, lens, Hkv, 141)
+    q = wl.make_queries(B, H, D, 143, DEV)
+    pick = sorted({0, B - 1} | {b for a, e, _ in groups for b in (a, a + 1, a + 2, a + 3, a + 5, a + 6, (a + e) // 2, e - 1) if b < e})
+    out = s.call(q)
+    _check_some(s, out, q, lens, pick, groups)
+    for _ in range(3):
+        assert _same(s.call(q), out)
+
+
+def test_shared_many_sequences_limits_and_a_graph_of_other_lengths():
+    """One captured call whose prefix grows and shrinks on the device past what changes how the waves share it; what lies behind a sequence's
+    length, an infinity or pages that hold none of its tokens, is not in its result."""
+    H, Hkv, B, prefix = 32, 2, 256, 2300
+    groups = [(0, B, prefix)]
+    lens = [prefix + b % 30 if b % 3 else prefix - 3 - b for b in range(B)]
+    s = _Batch(groups, lens, Hkv, 151)
+    q = wl.make_queries(B, H, D, 153, DEV)
+    pick = [0, 1, 2, 3, 90, 129, 255]
+    clean = s.call(q)
+    _check_some(s, clean, q, lens, pick, groups)
+    cu, pl, seq, out = _ints(s.cu), _ints([prefix]), _ints(lens), torch.zeros_like(clean)
+    ws = torch.full((api.kv4_shared_attention_workspace_bytes(B, H, Hkv, s.width, 1),), 0xFF, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        api.kv4_shared_attention_decode(q, s.pool, s.table, seq, cu, pl, Hkv, out=out, workspace=ws)
+    for tokens in (prefix, 640, 2177, 1, 2176, 0, prefix):
+        # behind a shorter prefix the sequences' own pages hold the rest of it, but in the page in which it ends: lengths end with it
+        now = [min(n, tokens) if n >= tokens else n for n in lens] if tokens != prefix else lens
+        pl.copy_(_ints([tokens])), seq.copy_(_ints(now)), out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        _check_some(s, out, q, now, pick, [(0, B, tokens)])
+        assert _same(api.kv4_shared_attention_decode(q, s.pool, s.table, seq, cu, pl, Hkv), out)
+    # all sequences end in front of the prefix's last pages, which are none
+    short = [min(n, 2200 - b) for b, n in enumerate(lens)]
+    table = s.table.clone()
+    table[:, 35:] = -1
+    got = api.kv4_shared_attention_decode(q, s.pool, table, _ints(short), cu, pl, Hkv)
+    _check_some(s, got, q, short, pick, groups)
+    # an infinity among the prefix's last tokens
+    bad = torch.full((1, Hkv, D), float("inf"), dtype=torch.float16, device=DEV)
+    api.kv4_paged_append(s.pool, bad, bad, s.table[:1].contiguous(), _ints([0, 1]), _ints([prefix - 2]))
+    got, sees = s.call(q), torch.tensor([n > prefix - 2 for n in lens], device=DEV)
+    assert _same(got[~sees], clean[~sees]) and got[sees].isnan().all()
+
+
 def test_shared_agrees_with_the_call_without_groups():
     """Prefixes of whole pages, which every member's table names: both calls read the same tokens."""
     H, Hkv, lens = 8, 2, [300, 257, 256, 400, 70]
