@@ -8,7 +8,8 @@
 // chiplet (workgroups of one KV head are 8 apart where the heads are a multiple of 8).
 //
 // One launch attends, with workgroups for both kinds of work side by side, each writing unnormalised sums, references and weight sums of
-// its range of tokens; a second one joins those of each head.  The arithmetic of a chunk and the weights' reference are those of the
+// its range of tokens; a second one joins those of each head.  Where the sequences alone fill the chip, the first launch is the prefixes' and the
+// second that of the own tokens, which joins.  The arithmetic of a chunk and the weights' reference are those of the
 // paged decode kernel (qoq_kv4_paged.hip).
 #include <algorithm>
 
@@ -24,6 +25,7 @@ constexpr int kChunk = 32;                               // tokens: two tiles of
 constexpr int kWaves = 4;                                // of a workgroup
 constexpr int kMaxParts = 64;                            // of a prefix, and of a sequence's own tokens
 constexpr int kInFlight = 8;                             // parts that the join requests together
+constexpr int kOwnInFlight = 4;                          // the same where it is part of the work on a sequence's own tokens
 constexpr int kColumnTiles = 2;                          // of 16 columns for each wave, over a prefix
 constexpr int kPrefixColumns = 16 * kColumnTiles;
 constexpr int kWide = 2;                                 // the same where a prefix's columns are many and a workgroup's waves have columns of their own
@@ -53,6 +55,7 @@ __device__ __forceinline__ int by_ratio(const SharedArgs& p, int n) { return p.R
 
 typedef const __attribute__((address_space(1))) uint8_t* global_bytes;
 typedef const __attribute__((address_space(1))) u32x4* global_u32x4;
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef unsigned short us2 __attribute__((ext_vector_type(2)));
 // the block table, which no kernel here writes: entries at addresses that a wave shares come through the scalar cache, and only their use waits
 typedef const __attribute__((address_space(4))) int32_t* constant_ints;
@@ -111,9 +114,10 @@ struct Work {
 };
 
 // One workgroup's range of tokens for up to 16 CT columns.  PK = 2: two tiles of tokens share the columns of a matrix instruction (at most
-// eight columns).  LIMITS: columns may end in front of `hi`, each at its sequence's length.
-template <int CT, int PK, bool LIMITS>
-__device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float* s_part)
+// eight columns).  LIMITS: columns may end in front of `hi`, each at its sequence's length.  finish(row, d, sums, reference, weight sum) takes four
+// elements of a column's result each.
+template <int CT, int PK, bool LIMITS, class Finish>
+__device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float* s_part, Finish finish)
 {
     constexpr int NS = 2 / PK;
     const int lane = threadIdx.x & 63;
@@ -379,11 +383,19 @@ __device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float
             }
             const int held = k.column0 + i * 16 + at, s = by_ratio(p, held);
             const int64_t row = ((int64_t)(k.first + s) * p.Hkv + k.hk) * R + held - s * R;
-            float* to = p.parts + (row * k.total_slots + k.slot) * kPartial;
-            *reinterpret_cast<float4*>(to + d) = num;
-            if (d == 0) *reinterpret_cast<float4*>(to + kD) = make_float4(mm, den, 0.f, 0.f);
+            finish(row, d, num, mm, den);
         }
     }
+}
+// ... which becomes a part
+template <int CT, int PK, bool LIMITS>
+__device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float* s_part)
+{
+    attend<CT, PK, LIMITS>(p, k, s_part, [&](int64_t row, int d, float4 num, float mm, float den) __attribute__((always_inline)) {
+        float* to = p.parts + (row * k.total_slots + k.slot) * kPartial;
+        *reinterpret_cast<float4*>(to + d) = num;
+        if (d == 0) *reinterpret_cast<float4*>(to + kD) = make_float4(mm, den, 0.f, 0.f);
+    });
 }
 
 // ---- A prefix that many columns share: four waves of 16 CT columns each, the pages unpacked once for all of them ----
@@ -825,6 +837,87 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     }
 }
 
+// The prefix of sequence b, which has L tokens in all, and the parts that there are of it for its heads.
+template <int WIDE>
+struct Seen {
+    int tokens;
+    int narrow;                                          // parts where the waves shared the tokens: one number for all heads; else the units
+    Units f;
+    __device__ __forceinline__ Seen(const SharedArgs& p, int b, int L, int lane)
+    {
+        if constexpr (WIDE != 0) {
+            GroupLanes<64 * WIDE> g;
+            count_units<64 * WIDE>(p, g, f, b);
+            tokens = f.tokens;
+        } else {
+            f = Units{};
+            tokens = prefix_of(p, b, lane);
+        }
+        const bool any = tokens && L;
+        narrow = !any ? 0 : f.all < kWideUnits ? attending((tokens + kChunk - 1) / kChunk, p.prefix_parts) : -1;
+    }
+    __device__ __forceinline__ int parts(const SharedArgs& p, int b, int hk, int of_kv) const
+    {
+        if (WIDE == 0 || narrow >= 0) return narrow;
+        const int tile = ((b - f.first) * p.R + of_kv) / (64 * (WIDE ? WIDE : 1)), unit = f.before + (hk * f.tiles + tile) * f.pages;
+        return (unit + f.pages - 1) / f.run - unit / f.run + 1;
+    }
+};
+
+// A workgroup for each sequence and KV head, where those fill the chip: its own tokens, and the join with the prefix's parts.
+template <int PK, int WIDE>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))) void shared_own_kernel(SharedArgs p)
+{
+    __shared__ __align__(16) float s_part[kWaves * 16 * kPartial];
+    const int lane = threadIdx.x & 63, b = blockIdx.x / p.Hkv;
+    Work k{};
+    k.hk = blockIdx.x - b * p.Hkv;
+    k.hi = min(max(p.seq_lens[b], 0), p.width * kPageTokens);
+    const Seen<WIDE> seen(p, b, k.hi, lane);
+    k.lo = min(seen.tokens, k.hi);
+    k.parts = 1;
+    k.pages_of = p.table + (int64_t)b * p.width;
+    k.first = b;
+    k.columns = p.R;
+    const int64_t row0 = ((int64_t)b * p.Hkv + k.hk) * p.R;
+    // (the prefix's parts come a few together, each few against the largest reference so far)
+    auto finish = [&](int64_t row, int d, float4 num, float top, float den) __attribute__((always_inline)) {
+        const int n = seen.parts(p, b, k.hk, (int)(row - row0));
+        const float* parts = p.parts + row * (p.prefix_slots + p.own_parts) * kPartial;
+#pragma unroll 1
+        for (int i0 = 0; i0 < n; i0 += kOwnInFlight) {
+            float4 a[kOwnInFlight];
+            float2 ml[kOwnInFlight];
+            float most = top;
+#pragma unroll
+            for (int e = 0; e < kOwnInFlight; ++e) {
+                const float* part = parts + (int64_t)min(i0 + e, n - 1) * kPartial;
+                ml[e] = *reinterpret_cast<const float2*>(part + kD);
+                a[e] = *reinterpret_cast<const float4*>(part + d);
+            }
+#pragma unroll
+            for (int e = 0; e < kOwnInFlight; ++e) most = fmaxf(most, ml[e].x);
+            const float alpha = __builtin_amdgcn_exp2f(top - most);
+            num.x *= alpha; num.y *= alpha; num.z *= alpha; num.w *= alpha;
+            den *= alpha;
+            top = most;
+#pragma unroll
+            for (int e = 0; e < kOwnInFlight; ++e) {
+                const float f = i0 + e < n ? __builtin_amdgcn_exp2f(ml[e].x - most) : 0.f;
+                num.x = fmaf(a[e].x, f, num.x); num.y = fmaf(a[e].y, f, num.y); num.z = fmaf(a[e].z, f, num.z); num.w = fmaf(a[e].w, f, num.w);
+                den = fmaf(ml[e].y, f, den);
+            }
+        }
+        const float inv = den > 0.f ? 1.f / den : 1.f;   // nothing seen: zero, as the sums are (NaN stays)
+        *reinterpret_cast<h4*>(p.out + row * kD + d) = (h4){(_Float16)(num.x * inv), (_Float16)(num.y * inv), (_Float16)(num.z * inv), (_Float16)(num.w * inv)};
+    };
+    if (k.lo < k.hi) {
+        attend<1, PK, false>(p, k, s_part, finish);
+    } else {
+        for (int x = threadIdx.x; x < p.R * (kD / 4); x += 64 * kWaves) finish(row0 + x / (kD / 4), x % (kD / 4) * 4, make_float4(0.f, 0.f, 0.f, 0.f), -1e29f, 0.f);
+    }
+}
+
 // The parts of a head, a wave to a head: two elements to a lane, a part's reference to a lane.
 template <int WIDE>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
@@ -836,24 +929,9 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
     const int b = (int)(row / H);
     const int most = p.width * kPageTokens;
     const int L = min(max(p.seq_lens[b], 0), most);
-    int P, n_prefix = 0;
-    if constexpr (WIDE != 0) {
-        Units f;
-        GroupLanes<64 * WIDE> g;
-        count_units<64 * WIDE>(p, g, f, b);
-        P = f.tokens;
-        if (P && L && f.all < kWideUnits) {
-            n_prefix = attending((P + kChunk - 1) / kChunk, p.prefix_parts);
-        } else if (P && L) {
-            const int h = (int)(row % H), hk = h / p.R, tile = ((b - f.first) * p.R + h % p.R) / (64 * WIDE);
-            const int unit = f.before + (hk * f.tiles + tile) * f.pages;
-            n_prefix = (unit + f.pages - 1) / f.run - unit / f.run + 1;
-        }
-    } else {
-        P = prefix_of(p, b, lane);
-        if (P && L) n_prefix = attending((P + kChunk - 1) / kChunk, p.prefix_parts);
-    }
-    const int lo = min(P, L);
+    const int h = (int)(row - (int64_t)b * H), hk = by_ratio(p, h);
+    const Seen<WIDE> seen(p, b, L, lane);
+    const int n_prefix = seen.parts(p, b, hk, h - hk * p.R), lo = min(seen.tokens, L);
     const int n_own = L > lo ? attending((L + kChunk - 1) / kChunk - lo / kChunk, p.own_parts) : 0;
     const int total = p.prefix_slots + p.own_parts, n = n_prefix + n_own;
     const float* parts = p.parts + row * total * kPartial;
@@ -909,6 +987,13 @@ int wide_parts(int64_t B, int64_t G, int64_t R, int64_t Hkv)
     return wide_prefix(B, G, R) ? (int)std::min<int64_t>(kMaxParts, 2 * kWideWorkgroups / (prefix_tiles(B, G, R, 64 * kWide) * Hkv) + 3) : 0;
 }
 
+// Whether the own tokens have a launch of their own, behind the prefixes' and in place of the join, with registers and LDS for three workgroups on a
+// compute unit, not two.  Side by side with a prefix they fill what it leaves, so few gain nothing: 64 sequences of 32 / 8 heads with 300 tokens behind
+// 4096 27.6 us in two launches side by side and joined, 29.7 one behind the other; 200 of 40 / 8 with 100 behind 1000 36.1 and 32.7; 512 of 32 / 8 with
+// 300 behind 100 64.4 and 52.2; 300 of 32 / 8 with 100 behind 8000 in three groups 96 and 103, 200 of 64 / 8 with 100 behind 16000 190 and 195.  Without prefixes there is the one launch: 64 of 32 / 8 with 300 tokens
+// 11.5 us joined, 7.6 so.
+bool own_launch(int64_t B, int64_t G, int64_t Hkv, int own_parts) { return own_parts == 1 && (!G || B * Hkv > 1000); }
+
 }  // namespace
 
 size_t shared_decode_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t width, int64_t G)
@@ -935,14 +1020,22 @@ hipError_t launch_shared_decode(const void* q, int64_t q_stride, const uint8_t* 
     p.prefix_workgroups = kWideWorkgroups;
     p.ratio_magic = (uint32_t)((((uint64_t)1 << 32) + p.R - 1) / p.R);
     const int64_t prefix_blocks = std::max<int64_t>(wide ? kWideWorkgroups : 0, prefix_tiles(B, G, p.R, kPrefixColumns) * Hkv * p.prefix_parts);
-    const int64_t blocks = prefix_blocks + B * Hkv * p.own_parts, joins = (B * H + 3) / 4;
-    if (blocks >= (int64_t)1 << 24 || joins >= (int64_t)1 << 24) return hipErrorInvalidValue;    // 2^32 threads
+    const bool own = own_launch(B, G, Hkv, p.own_parts);
+    const int64_t blocks = prefix_blocks + (own ? 0 : B * Hkv * p.own_parts), joins = (B * H + 3) / 4;
+    if (blocks >= (int64_t)1 << 24 || B * Hkv >= (int64_t)1 << 24 || joins >= (int64_t)1 << 24) return hipErrorInvalidValue;    // 2^32 threads
     if (wide && prefix_tiles(B, G, p.R, 64 * kWide) * Hkv * width >= (int64_t)1 << 31) return hipErrorInvalidValue;  // units of work, counted in 32 bits
     p.prefix_blocks = (uint32_t)prefix_blocks;
     const int PK = p.R <= 8 ? 2 : 1;
     auto* kernel = PK == 2 ? (wide ? shared_decode_kernel<2, kWide> : shared_decode_kernel<2, 0>) : (wide ? shared_decode_kernel<1, kWide> : shared_decode_kernel<1, 0>);
-    kernel<<<(unsigned)blocks, 64 * kWaves, 0, s>>>(p);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (blocks) {
+        kernel<<<(unsigned)blocks, 64 * kWaves, 0, s>>>(p);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    if (own) {
+        auto* rest = PK == 2 ? (wide ? shared_own_kernel<2, kWide> : shared_own_kernel<2, 0>) : (wide ? shared_own_kernel<1, kWide> : shared_own_kernel<1, 0>);
+        rest<<<(unsigned)(B * Hkv), 64 * kWaves, 0, s>>>(p);
+        return hipGetLastError();
+    }
     auto* join = wide ? shared_join_kernel<kWide> : shared_join_kernel<0>;
     join<<<(unsigned)joins, 256, 0, s>>>(p);
     return hipGetLastError();

@@ -195,6 +195,27 @@ def test_shared_of_many_sequences_behind_long_prefixes(H, Hkv, groups, B):
         assert _same(s.call(q), out)
 
 
+@pytest.mark.parametrize("B,H,Hkv,groups", [
+    (300, 16, 4, []), (7, 9, 1, []), (40, 32, 32, []),                       # no groups: one launch
+    (400, 12, 4, [(0, 400, 300)]), (130, 8, 8, [(3, 60, 129), (60, 61, 70), (61, 125, 500)]),
+    (1100, 16, 1, [(i * 10, i * 10 + 9, 40 + i) for i in range(110)]),       # more groups than lanes
+    (520, 32, 2, [(0, 510, 2300)])])                                         # heads of a KV head in parts that differ
+def test_shared_of_sequences_that_fill_the_chip(B, H, Hkv, groups):
+    of = {b: p for a, e, p in groups for b in range(a, e)}
+    lens = [of.get(b, 0) + (b * 5) % 70 for b in range(B)]
+    for a, e, p in groups:
+        for b, n in zip(range(a + 1, min(e, a + 6)), (0, 1, p // 2, p - 1, p)):
+            lens[b] = max(n, 0)
+    s = _Batch(groups, lens, Hkv, 161)
+    q = wl.make_queries(B, H, D, 163, DEV)
+    pick = sorted({0, 1, B - 1} | {b for a, e, _ in groups[::9] for b in (a, a + 1, a + 2, a + 3, a + 5, (a + e) // 2, e - 1) if b < e})
+    ws = torch.full((api.kv4_shared_attention_workspace_bytes(B, H, Hkv, s.width, len(groups)),), 0xFF, dtype=torch.uint8, device=DEV)
+    out = s.call(q, workspace=ws)
+    _check_some(s, out, q, lens, pick, groups)
+    for _ in range(3):
+        assert _same(s.call(q), out)
+
+
 def test_shared_many_sequences_limits_and_a_graph_of_other_lengths():
     """One captured call whose prefix grows and shrinks on the device past what changes how the waves share it; what lies behind a sequence's
     length, an infinity or pages that hold none of its tokens, is not in its result."""
