@@ -92,7 +92,7 @@ __device__ __forceinline__ int upto_lane(int v)
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);       // the last of row 1 into 2 and 3
     return v;
 }
-__device__ __forceinline__ int largest_of_lanes(int v)                    // (of numbers that are not negative)
+__device__ __forceinline__ int largest_upto_lane(int v)                   // (of numbers that are not negative)
 {
     v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));
     v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
@@ -100,8 +100,9 @@ __device__ __forceinline__ int largest_of_lanes(int v)                    // (of
     v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
     v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));
     v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));
-    return __builtin_amdgcn_readlane(v, 63);
+    return v;
 }
+__device__ __forceinline__ int largest_of_lanes(int v) { return __builtin_amdgcn_readlane(largest_upto_lane(v), 63); }
 
 struct Work {
     const int32_t* pages_of;                             // the block table's row
@@ -662,20 +663,27 @@ struct Units {
     int first, columns, tokens, pages, tiles;            // that group
 };
 
-// Groups g0 .. g0 + 63, one to a lane.
+// Groups g0 .. g0 + 63, one to a lane.  Bounds that descend are taken as ascending ones: no sequence is in two groups, and the units stay within what
+// the host counted.
 template <int TILE>
 struct GroupLanes {
     int first, last, tokens, columns, pages, tiles, units, upto;
+    int reached;                                         // the largest bound in front of these groups
     __device__ __forceinline__ void load(const SharedArgs& p, int g0)
     {
         const int g = g0 + (int)(threadIdx.x & 63);
-        first = last = tokens = 0;
+        int bound = 0, end = 0;
+        tokens = 0;
         if (g < p.G) {
             const int a = p.cu[g], e = p.cu[g + 1], n = p.prefix_lens[g];
-            first = min(max(a, 0), p.B);
-            last = max(min(e, p.B), first);
+            bound = min(max(a, 0), p.B);
+            end = min(e, p.B);
             tokens = min(max(n, 0), p.width * kPageTokens);
         }
+        if (g0 == 0) reached = 0;
+        first = largest_upto_lane(max(bound, reached));
+        last = max(end, first);
+        reached = __builtin_amdgcn_readlane(first, 63);
         columns = (last - first) * p.R;
         tiles = (columns + TILE - 1) / TILE;
         pages = tiles ? (tokens + kPageTokens - 1) / kPageTokens : 0;
@@ -837,35 +845,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     }
 }
 
-// The prefix of sequence b, which has L tokens in all, and the parts that there are of it for its heads.
-template <int WIDE>
-struct Seen {
-    int tokens;
-    int narrow;                                          // parts where the waves shared the tokens: one number for all heads; else the units
-    Units f;
-    __device__ __forceinline__ Seen(const SharedArgs& p, int b, int L, int lane)
-    {
-        if constexpr (WIDE != 0) {
-            GroupLanes<64 * WIDE> g;
-            count_units<64 * WIDE>(p, g, f, b);
-            tokens = f.tokens;
-        } else {
-            f = Units{};
-            tokens = prefix_of(p, b, lane);
-        }
-        const bool any = tokens && L;
-        narrow = !any ? 0 : f.all < kWideUnits ? attending((tokens + kChunk - 1) / kChunk, p.prefix_parts) : -1;
-    }
-    __device__ __forceinline__ int parts(const SharedArgs& p, int b, int hk, int of_kv) const
-    {
-        if (WIDE == 0 || narrow >= 0) return narrow;
-        const int tile = ((b - f.first) * p.R + of_kv) / (64 * (WIDE ? WIDE : 1)), unit = f.before + (hk * f.tiles + tile) * f.pages;
-        return (unit + f.pages - 1) / f.run - unit / f.run + 1;
-    }
-};
-
 // A workgroup for each sequence and KV head, where those fill the chip: its own tokens, and the join with the prefix's parts.
-template <int PK, int WIDE>
+template <int PK>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))) void shared_own_kernel(SharedArgs p)
 {
     __shared__ __align__(16) float s_part[kWaves * 16 * kPartial];
@@ -873,8 +854,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
     Work k{};
     k.hk = blockIdx.x - b * p.Hkv;
     k.hi = min(max(p.seq_lens[b], 0), p.width * kPageTokens);
-    const Seen<WIDE> seen(p, b, k.hi, lane);
-    k.lo = min(seen.tokens, k.hi);
+    const int P = prefix_of(p, b, lane), n = P && k.hi ? attending((P + kChunk - 1) / kChunk, p.prefix_parts) : 0;
+    k.lo = min(P, k.hi);
     k.parts = 1;
     k.pages_of = p.table + (int64_t)b * p.width;
     k.first = b;
@@ -882,7 +863,6 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
     const int64_t row0 = ((int64_t)b * p.Hkv + k.hk) * p.R;
     // (the prefix's parts come a few together, each few against the largest reference so far)
     auto finish = [&](int64_t row, int d, float4 num, float top, float den) __attribute__((always_inline)) {
-        const int n = seen.parts(p, b, k.hk, (int)(row - row0));
         const float* parts = p.parts + row * (p.prefix_slots + p.own_parts) * kPartial;
 #pragma unroll 1
         for (int i0 = 0; i0 < n; i0 += kOwnInFlight) {
@@ -929,9 +909,24 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
     const int b = (int)(row / H);
     const int most = p.width * kPageTokens;
     const int L = min(max(p.seq_lens[b], 0), most);
-    const int h = (int)(row - (int64_t)b * H), hk = by_ratio(p, h);
-    const Seen<WIDE> seen(p, b, L, lane);
-    const int n_prefix = seen.parts(p, b, hk, h - hk * p.R), lo = min(seen.tokens, L);
+    int P, n_prefix = 0;
+    if constexpr (WIDE != 0) {
+        Units f;
+        GroupLanes<64 * WIDE> g;
+        count_units<64 * WIDE>(p, g, f, b);
+        P = f.tokens;
+        if (P && L && f.all < kWideUnits) {
+            n_prefix = attending((P + kChunk - 1) / kChunk, p.prefix_parts);
+        } else if (P && L) {
+            const int h = (int)(row - (int64_t)b * H), hk = by_ratio(p, h), tile = ((b - f.first) * p.R + h - hk * p.R) / (64 * WIDE);
+            const int unit = f.before + (hk * f.tiles + tile) * f.pages;
+            n_prefix = (unit + f.pages - 1) / f.run - unit / f.run + 1;
+        }
+    } else {
+        P = prefix_of(p, b, lane);
+        if (P && L) n_prefix = attending((P + kChunk - 1) / kChunk, p.prefix_parts);
+    }
+    const int lo = min(P, L);
     const int n_own = L > lo ? attending((L + kChunk - 1) / kChunk - lo / kChunk, p.own_parts) : 0;
     const int total = p.prefix_slots + p.own_parts, n = n_prefix + n_own;
     const float* parts = p.parts + row * total * kPartial;
@@ -970,8 +965,12 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
     reinterpret_cast<h2*>(p.out + row * kD)[lane] = (h2){(_Float16)(sum.x * inv), (_Float16)(sum.y * inv)};
 }
 
-bool wide_prefix(int64_t B, int64_t G, int64_t R) { return G && B * R / G >= 64; }
 int64_t prefix_tiles(int64_t B, int64_t G, int64_t R, int64_t columns) { return G ? B * R / columns + G : 0; }
+// Whether prefixes may take the wide form: half a tile of columns to a group, and room in the block table for that many units.
+bool wide_prefix(int64_t B, int64_t G, int64_t R, int64_t Hkv, int64_t width)
+{
+    return G && B * R / G >= 64 && prefix_tiles(B, G, R, 64 * kWide) * Hkv * width >= kWideUnits;
+}
 // Workgroups that stand by for each tile of columns of a prefix and KV head, and for each sequence and KV head: two to a compute unit.
 int parts_for(int64_t items, int64_t width)
 {
@@ -982,23 +981,22 @@ int parts_for(int64_t items, int64_t width)
 // Parts of a tile of columns of a prefix where the waves share its tokens, and where they have columns of their own: twice what an even share of
 // the workgroups comes to, and the pieces at its ends.
 int prefix_parts(int64_t B, int64_t G, int64_t R, int64_t Hkv, int64_t width) { return parts_for(prefix_tiles(B, G, R, kPrefixColumns) * Hkv, width); }
-int wide_parts(int64_t B, int64_t G, int64_t R, int64_t Hkv)
+int wide_parts(int64_t B, int64_t G, int64_t R, int64_t Hkv, int64_t width)
 {
-    return wide_prefix(B, G, R) ? (int)std::min<int64_t>(kMaxParts, 2 * kWideWorkgroups / (prefix_tiles(B, G, R, 64 * kWide) * Hkv) + 3) : 0;
+    return wide_prefix(B, G, R, Hkv, width) ? (int)std::min<int64_t>(kMaxParts, 2 * kWideWorkgroups / (prefix_tiles(B, G, R, 64 * kWide) * Hkv) + 3) : 0;
 }
-
 // Whether the own tokens have a launch of their own, behind the prefixes' and in place of the join, with registers and LDS for three workgroups on a
-// compute unit, not two.  Side by side with a prefix they fill what it leaves, so few gain nothing: 64 sequences of 32 / 8 heads with 300 tokens behind
-// 4096 27.6 us in two launches side by side and joined, 29.7 one behind the other; 200 of 40 / 8 with 100 behind 1000 36.1 and 32.7; 512 of 32 / 8 with
-// 300 behind 100 64.4 and 52.2; 300 of 32 / 8 with 100 behind 8000 in three groups 96 and 103, 200 of 64 / 8 with 100 behind 16000 190 and 195.  Without prefixes there is the one launch: 64 of 32 / 8 with 300 tokens
-// 11.5 us joined, 7.6 so.
-bool own_launch(int64_t B, int64_t G, int64_t Hkv, int own_parts) { return own_parts == 1 && (!G || B * Hkv > 1000); }
+// compute unit, not two.  Side by side with a prefix they fill what it leaves, so few gain nothing, nor do those beside prefixes that may be long for
+// the wide form: 64 sequences of 32 / 8 heads with 300 tokens behind 4096 27.6 us in one launch and joined, 29.7 one behind the other; 200 of 40 / 8
+// with 100 behind 1000 36.1 and 32.7; 512 of 32 / 8 with 300 behind 100 64.4 and 52.2; 300 of 32 / 8 with 100 behind 8000 in three groups 96 and 103,
+// 200 of 64 / 8 with 100 behind 16000 190 and 195.  Without prefixes there is the one launch: 64 of 32 / 8 with 300 tokens 11.5 us joined, 7.6 so.
+bool own_launch(int64_t B, int64_t G, int64_t Hkv, int own_parts, bool wide) { return own_parts == 1 && !wide && (!G || B * Hkv > 1000); }
 
 }  // namespace
 
 size_t shared_decode_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t width, int64_t G)
 {
-    const int64_t slots = std::max(prefix_parts(B, G, H / Hkv, Hkv, width), wide_parts(B, G, H / Hkv, Hkv)) + parts_for(B * Hkv, width);
+    const int64_t slots = std::max(prefix_parts(B, G, H / Hkv, Hkv, width), wide_parts(B, G, H / Hkv, Hkv, width)) + parts_for(B * Hkv, width);
     return (size_t)(B * H * slots) * kPartial * sizeof(float);
 }
 
@@ -1012,15 +1010,15 @@ hipError_t launch_shared_decode(const void* q, int64_t q_stride, const uint8_t* 
     p.parts = static_cast<float*>(workspace);
     p.out = static_cast<__half*>(out);
     p.pages = (uint32_t)pages; p.width = (int)width; p.B = (int)B; p.G = (int)G; p.Hkv = (int)Hkv; p.R = (int)(H / Hkv);
-    const bool wide = wide_prefix(B, G, p.R);
+    const bool wide = wide_prefix(B, G, p.R, Hkv, width);
     p.prefix_parts = prefix_parts(B, G, p.R, Hkv, width);
-    p.wide_parts = wide_parts(B, G, p.R, Hkv);
+    p.wide_parts = wide_parts(B, G, p.R, Hkv, width);
     p.prefix_slots = std::max(p.prefix_parts, p.wide_parts);
     p.own_parts = parts_for(B * Hkv, width);
     p.prefix_workgroups = kWideWorkgroups;
     p.ratio_magic = (uint32_t)((((uint64_t)1 << 32) + p.R - 1) / p.R);
     const int64_t prefix_blocks = std::max<int64_t>(wide ? kWideWorkgroups : 0, prefix_tiles(B, G, p.R, kPrefixColumns) * Hkv * p.prefix_parts);
-    const bool own = own_launch(B, G, Hkv, p.own_parts);
+    const bool own = own_launch(B, G, Hkv, p.own_parts, wide);
     const int64_t blocks = prefix_blocks + (own ? 0 : B * Hkv * p.own_parts), joins = (B * H + 3) / 4;
     if (blocks >= (int64_t)1 << 24 || B * Hkv >= (int64_t)1 << 24 || joins >= (int64_t)1 << 24) return hipErrorInvalidValue;    // 2^32 threads
     if (wide && prefix_tiles(B, G, p.R, 64 * kWide) * Hkv * width >= (int64_t)1 << 31) return hipErrorInvalidValue;  // units of work, counted in 32 bits
@@ -1032,7 +1030,7 @@ hipError_t launch_shared_decode(const void* q, int64_t q_stride, const uint8_t* 
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (own) {
-        auto* rest = PK == 2 ? (wide ? shared_own_kernel<2, kWide> : shared_own_kernel<2, 0>) : (wide ? shared_own_kernel<1, kWide> : shared_own_kernel<1, 0>);
+        auto* rest = PK == 2 ? shared_own_kernel<2> : shared_own_kernel<1>;
         rest<<<(unsigned)(B * Hkv), 64 * kWaves, 0, s>>>(p);
         return hipGetLastError();
     }

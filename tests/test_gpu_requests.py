@@ -216,6 +216,22 @@ def test_shared_of_sequences_that_fill_the_chip(B, H, Hkv, groups):
         assert _same(s.call(q), out)
 
 
+@pytest.mark.parametrize("B,H,Hkv,prefix,cu", [(256, 32, 2, 2300, [0, 256, 0, 256, 3, 256]), (1200, 8, 1, 700, [9, 1100, 5, 1200, 0, 1 << 30]),
+                                               (6, 8, 2, 200, [0, 6, 0, 6, 0, 6, 0, 6]), (300, 32, 4, 130, [0, 300] * 50)])
+def test_shared_groups_that_overlap_touch_nothing_else(B, H, Hkv, prefix, cu):
+    """Their results are unspecified, but nothing outside them and the workspace is written, and a call of proper groups is as it was."""
+    s = _Batch([(0, B, prefix)], [prefix + b % 9 for b in range(B)], Hkv, 171)
+    q = wl.make_queries(B, H, D, 173, DEV)
+    want = s.call(q)
+    need = api.kv4_shared_attention_workspace_bytes(B, H, Hkv, s.width, len(cu) - 1)
+    held, ws = torch.full((B + 2, H, D), 7.0, dtype=torch.float16, device=DEV), torch.full((need + 4096,), 0x55, dtype=torch.uint8, device=DEV)
+    before = s.pool.clone()
+    api.kv4_shared_attention_decode(q, s.pool, s.table, _ints(s.lens), _ints(cu), _ints([prefix] * (len(cu) - 1)), Hkv, out=held[1:-1], workspace=ws[:need])
+    torch.cuda.synchronize()
+    assert (held[0] == 7).all() and (held[-1] == 7).all() and (ws[need:] == 0x55).all() and torch.equal(s.pool, before)
+    assert _same(s.call(q), want)
+
+
 def test_shared_many_sequences_limits_and_a_graph_of_other_lengths():
     """One captured call whose prefix grows and shrinks on the device past what changes how the waves share it; what lies behind a sequence's
     length, an infinity or pages that hold none of its tokens, is not in its result."""
