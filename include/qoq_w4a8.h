@@ -340,7 +340,9 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
  *   the order of sums.  The first sequence may itself be empty, its entries have to name the prefix's pages all the same.
  *     group_cu     [groups + 1] INT32, device, ascending; sequences in front of the first and behind the last share nothing
  *     prefix_lens  [groups] INT32, device, clamped to [0, 64 width]; a sequence that is shorter sees its seq_lens[b] tokens of it
- *     groups = 0: the pointers may be NULL.  Descending or overlapping groups give unspecified results and touch nothing else.
+ *     groups = 0: the pointers may be NULL.  Bounds that descend give unspecified results and touch nothing else.
+ *   Sums are FP32; weight times value scale is rounded once, to 2^-11 of itself, or (scores within 5e6) 2^-33 of the largest weight times
+ *   the largest scale of what the sequence sees where that is more.
  *   workspace  required, qoq_kv4_shared_attention_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant on entry and exit.
  * qoq_lora_add: out[m] = base[m] + scales[a] (x[m] A_a^T) B_a^T for the rows m of adapter a, out[m] = base[m] for those of none.
  *   base [M, N], x [M, K], out [M, N] FP16 with row strides in elements (multiples of 8), so that they may be slices of a fused projection's;
@@ -362,7 +364,8 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
  *   workspace  NULL, or qoq_token_logprobs_workspace_bytes(...) bytes (0: none is needed), 16-byte aligned, contents irrelevant on entry and exit;
  *              without one a row is not shared by several workgroups.
  * Limits: groups <= 1048576; rank % 8 == 0, rank <= 512, N % 8 == 0, K % 8 == 0, N and K <= 4194304, adapters <= 4096, M <= 1048576 (adapters);
- * V <= 16777216, M <= 16777216 (logits; 2^24 workgroups or more: QOQ_ERR_HIP); the rest as for the paged decode.  Errors as above. */
+ * V <= 16777216, M <= 16777216 (logits); the rest as for the paged decode.  2^24 workgroups or more, or 2^31 pages of prefixes by tiles of 128 query
+ * heads: QOQ_ERR_HIP.  Errors as above. */
 typedef enum { QOQ_FP16 = 0, QOQ_FP32 = 1 } qoq_dtype;
 size_t qoq_kv4_shared_attention_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t width, int64_t groups);
 int qoq_kv4_shared_attention_decode(const void* q_fp16, int64_t q_stride, const void* pool, int64_t pages, const int32_t* block_table,

@@ -11,6 +11,10 @@
 // its range of tokens; a second one joins those of each head.  Where the sequences alone fill the chip, the first launch is the prefixes' and the
 // second that of the own tokens, which joins.  The arithmetic of a chunk and the weights' reference are those of the
 // paged decode kernel (qoq_kv4_paged.hip).
+//
+// A prefix of many columns is bound by the vector unit beside the matrix unit: 200 sequences of 64 / 8 heads with 100 tokens behind 16000 take 190 us, 0.55
+// PFLOP/s, in which the matrix unit is busy for a quarter of the cycles and the vector unit for 0.45 (exp2, weights, FP16).  Short ones are bound
+// by the chain of trips to memory: 4 sequences with 30 tokens behind 1000 10.7 us, 7.7 + 3 for the join by a profiler.
 #include <algorithm>
 
 #include "qoq_gemm_common.h"
@@ -403,7 +407,8 @@ __device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float
 // A page goes through LDS in the order of the matrix instructions' operands, [fragment][lane] of 16 bytes, a quarter of it unpacked by each
 // wave, the next page while this one is used.
 constexpr int kPageFragments = 32;                       // of 1 KB: keys [tile][word], values [chunk][u][j]
-// Binades that the reference is set above what the largest weight needs, so that it seldom has to follow: each time costs half a chunk's arithmetic
+// Binades that the reference is set above what the largest weight needs, so that it seldom has to follow: each time costs half a chunk's arithmetic.
+// Weight times scale is FP16: as many binades less of its range are left below the largest (2^-33 of it, not 2^-39, is its smallest step's half).
 constexpr float kSpare = 6.f;
 struct WidePage {
     uint4 fragment[kPageFragments][64];
