@@ -40,7 +40,7 @@ def _same(a, b):
 class _Batch:
     """Sequences with their own copies of nothing: whole pages of a prefix are shared, the page in which it ends is the first member's."""
 
-    def __init__(self, groups, lens, Hkv, seed, width=None, spare=2):
+    def __init__(self, groups, lens, Hkv, seed, width=None, spare=2, values=None):
         # groups: (first, behind the last, prefix); lens: tokens of every sequence in all
         self.lens, self.Hkv, self.B = lens, Hkv, len(lens)
         self.cu = [g[0] for g in groups] + [groups[-1][1]] if groups else [0]
@@ -67,6 +67,7 @@ class _Batch:
         cu = np.concatenate(([0], np.cumsum(rows)))
         M = int(cu[-1])
         k, v = _heads(max(M, 1), Hkv, seed), _heads(max(M, 1), Hkv, seed + 1, True)
+        v = values(v) if values else v
         self.table = table.to(DEV)
         self.pool = torch.full((self.pages * Hkv * 8704,), 0xFF, dtype=torch.uint8, device=DEV)    # NaN parameters where nothing is written
         api.kv4_paged_append(self.pool, k[:M].contiguous(), v[:M].contiguous(), self.table, _ints(cu.tolist()), _ints(starts))
@@ -214,6 +215,33 @@ def test_shared_of_sequences_that_fill_the_chip(B, H, Hkv, groups):
     _check_some(s, out, q, lens, pick, groups)
     for _ in range(3):
         assert _same(s.call(q), out)
+
+
+@pytest.mark.parametrize("B,H,Hkv,prefix", [(256, 32, 2, 2300), (5, 8, 2, 300), (300, 16, 4, 130)])
+@pytest.mark.parametrize("size", [2.0 ** -16, 2.0 ** -8, 1.0, 2.0 ** 7, 2.0 ** 14])
+@pytest.mark.parametrize("heavy", [False, True])
+def test_shared_values_of_any_size(B, H, Hkv, prefix, size, heavy):
+    """Values up to `size`; heavy: every 50th token's 256 times the others'.  A product of weight and scale is off by 2^-33 of the largest scale at most where that
+    is more than 2^-11 of itself, and a value is at most 15 scales and the weights' sum at least one: L 2^-33 15 s, with 15 s the range of the largest value
+    and zero or the least, at most twice its size (of a half's subnormal steps one more, 15 2^-24 / 2)."""
+    def values(v):
+        v = v.float() / v.abs().max().float() * size
+        if heavy:
+            v[torch.arange(len(v), device=DEV) % 50 != 7] /= 256
+        return v.half()
+    groups = [(0, B, prefix)]
+    lens = [prefix + (b * 3) % 40 if b % 5 else prefix - b for b in range(B)]
+    s = _Batch(groups, lens, Hkv, 181, values=values)
+    q = wl.make_queries(B, H, D, 183, DEV)
+    out = s.call(q)
+    pick = [0, 1, B // 2, B - 1]
+    qd, got = q.cpu().numpy().astype(np.float64), out.cpu().numpy().astype(np.float64)
+    read = lambda i, t: s.read(0 if t < prefix else pick[i], t)
+    for i, (ref, spread, k) in enumerate(requests.shared_attention(qd[pick], read, [lens[b] for b in pick], [0], [])):
+        b, L = pick[i], len(k)
+        e = max([float((np.abs(k[:, h // (H // Hkv)]) @ np.abs(qd[b, h])).max()) for h in range(H)] if L else [0.0]) * 130 * 2.0 ** -24 / np.sqrt(128.0)
+        tol = 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2 * e + 2.0 ** -20 + (L + 160) * 2.0 ** -24) * spread + L * 2.0 ** -33 * 2 * size + 2.0 ** -25
+        assert (np.abs(got[b] - ref) <= tol).all(), (b, float((np.abs(got[b] - ref) / tol).max()))
 
 
 @pytest.mark.parametrize("B,H,Hkv,prefix,cu", [(256, 32, 2, 2300, [0, 256, 0, 256, 3, 256]), (1200, 8, 1, 700, [9, 1100, 5, 1200, 0, 1 << 30]),
@@ -529,6 +557,50 @@ def test_lora_graph_with_its_plan_and_streams():
                 got.append(api.lora_add(base, x, a, b, plan, scales=scales, workspace=space))
     torch.cuda.synchronize()
     assert all(_same(g, want[0][0]) for g in got)
+
+
+@pytest.mark.parametrize("M,N,K,rank,adapters", [(20, 264, 4096, 8, 3), (37, 136, 4096, 64, 5), (300, 200, 2056, 32, 20), (7, 72, 1000, 200, 2), (9, 64, 8, 136, 2), (700, 136, 1032, 40, 4)])
+def test_lora_workspace_of_any_contents_and_graphs_that_share_it(M, N, K, rank, adapters):
+    """Sums joined by the second product and by a launch between, for few rows and many, one chunk of ranks and several."""
+    base, x, a, b, scales = _lora_inputs(M, N, K, rank, adapters, 300 + M)
+    rows = [(m * 5) % (adapters + 1) for m in range(M)]
+    plan = api.lora_plan(_ints(rows), adapters)
+    need = api.lora_workspace_bytes(M, N, K, rank, adapters)
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device=DEV)
+    out = api.lora_add(base, x, a, b, plan, scales=scales, workspace=ws[:need])
+    _check_lora(out, base, x, a, b, rows, scales, list(range(0, M, 11)) + [M - 1])
+    assert (ws[need:] == 0xFF).all()
+    half = torch.zeros_like(out)
+    other = api.lora_add(half, x, a, b, plan)                               # another base, without scales
+    outs, graphs = [torch.empty_like(out), torch.empty_like(out)], []
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for o, args in zip(outs, ((base, scales), (half, None))):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            api.lora_add(args[0], x, a, b, plan, scales=args[1], out=o, workspace=ws[:need])
+        graphs.append(graph)
+    for _ in range(3):
+        ws.fill_(0xFF)
+        for o, graph in zip(outs, graphs):
+            o.fill_(7.0)
+            graph.replay()
+        torch.cuda.synchronize()
+        assert _same(outs[0], out) and _same(outs[1], other)
+        assert _same(api.lora_add(base, x, a, b, plan, scales=scales), out)
+    with pytest.raises(api.QoqError):
+        api.lora_add(base, x, a, b, plan, workspace=ws[:need - 16])
+
+
+def test_calls_on_nothing():
+    got = api.token_logprobs(torch.empty((0, 100), dtype=torch.float16, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV), top=5)
+    assert [tuple(t.shape) for t in got] == [(0,), (0,), (0,), (0, 5), (0, 5)]
+    with pytest.raises(api.QoqError):
+        api.token_logprobs(torch.zeros((2, 4), dtype=torch.float16, device=DEV), top=5)
+    none = torch.empty(0, dtype=torch.int32, device=DEV)
+    out = api.kv4_shared_attention_decode(torch.empty((0, 8, D), dtype=torch.float16, device=DEV), torch.zeros(2 * 2 * 8704, dtype=torch.uint8, device=DEV),
+                                          torch.empty((0, 3), dtype=torch.int32, device=DEV), none, _ints([0]), none, 2)
+    assert out.shape == (0, 8, D)
 
 
 def test_lora_binding_refuses():
