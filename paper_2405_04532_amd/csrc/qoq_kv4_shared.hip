@@ -35,10 +35,12 @@ constexpr int kPrefixColumns = 16 * kColumnTiles;
 constexpr int kWide = 2;                                 // the same where a prefix's columns are many and a workgroup's waves have columns of their own
 constexpr int kWideWorkgroups = 512;                     // that share the prefixes then: two on a compute unit
 constexpr int kLeastRun = 4;                             // pages of a run
-// Units of the wide form (a page for 128 columns) from which it is taken.  Its pages go through LDS one after the other and a run's first costs three:
-// 64 sequences of 32 / 8 heads behind 2000 tokens 33.4 us, 19.5 with tokens shared by the waves, behind 8000 (2000 units) 36.8 and 35.1, behind 16000 49.6
-// and 57.6; 151 of 40 / 8 behind 2000 (1536 units) 41.0 and 35.7, behind 4000 47.7 and 54.8.  Only the device knows the prefixes' lengths.
-constexpr int kWideUnits = 2200;
+// Units of the wide form (a page for 128 columns) from which it is taken, where no column of a tile is empty: about 24 us and 6.5 ns a unit, and about 15 and
+// 10.5 ns for each 128 columns where waves share the tokens (its pages go through LDS one after the other, and a run's first costs three).  64
+// sequences of 32 / 8 heads behind 8000 tokens (2000 units) 36.8 and 35.1 us, behind 16000 49.6 and 57.6; 151 of 40 / 8 behind 2000 (1536) 41.0 and 35.7,
+// behind 4000 47.7 and 54.8; five groups of 13 of 28 / 4 behind 14485 (4540, of which 0.29 empty) 49.2 and 45.0, four of 17 of 32 / 8 behind 16000 (8000, 0.47)
+// 65.5 and 53.7.  Only the device knows the prefixes' lengths.
+constexpr int kWideUnits = 2250;
 
 struct SharedArgs {
     const uint8_t* pool;
@@ -664,6 +666,7 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& p, const Work& k, 
 // equal runs of `run` units, of which none covers a tile in more parts than there are slots.
 struct Units {
     int all, run;
+    bool wide;                                           // worth their form
     int before;                                          // units of the groups in front of the one looked for
     int first, columns, tokens, pages, tiles;            // that group
 };
@@ -673,6 +676,7 @@ struct Units {
 template <int TILE>
 struct GroupLanes {
     int first, last, tokens, columns, pages, tiles, units, upto;
+    int lost;                                            // units' worth of columns that are none
     int reached;                                         // the largest bound in front of these groups
     __device__ __forceinline__ void load(const SharedArgs& p, int g0)
     {
@@ -694,6 +698,7 @@ struct GroupLanes {
         pages = tiles ? (tokens + kPageTokens - 1) / kPageTokens : 0;
         units = tiles * p.Hkv * pages;
         upto = upto_lane(units);
+        lost = (int)((int64_t)(p.Hkv * pages) * (tiles * TILE - columns) / TILE);
     }
     __device__ __forceinline__ void pick(Units& f, unsigned long long who, int before) const
     {
@@ -712,7 +717,7 @@ __device__ __forceinline__ void count_units(const SharedArgs& p, GroupLanes<TILE
 {
     f.all = 0;
     f.tokens = 0;
-    int longest = 0;
+    int longest = 0, lost = 0;
     for (int g0 = 0; g0 < p.G; g0 += 64) {
         g.load(p, g0);
         if (b >= 0 && !f.tokens) {
@@ -721,7 +726,9 @@ __device__ __forceinline__ void count_units(const SharedArgs& p, GroupLanes<TILE
         }
         f.all += __builtin_amdgcn_readlane(g.upto, 63);
         longest = max(longest, largest_of_lanes(g.pages));
+        lost += __builtin_amdgcn_readlane(upto_lane(g.lost), 63);
     }
+    f.wide = 8 * (int64_t)f.all - 21 * (int64_t)lost >= 8 * kWideUnits;      // (10.5 (all - lost) - 6.5 all >= 4 kWideUnits)
     f.run = max(max((f.all + p.prefix_workgroups - 1) / p.prefix_workgroups, min(kLeastRun, max(longest, 1))), (longest + p.wide_parts - 3) / (p.wide_parts - 2));
 }
 template <int TILE>
@@ -803,7 +810,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
             Units f;
             GroupLanes<kTile> g;
             count_units<kTile>(p, g, f, -1);
-            if (f.all < kWideUnits) {
+            if (!f.wide) {
                 if (!narrow_work(p, k)) return;
                 attend<kColumnTiles, 1, true>(p, k, s_part);
                 return;
@@ -920,7 +927,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
         GroupLanes<64 * WIDE> g;
         count_units<64 * WIDE>(p, g, f, b);
         P = f.tokens;
-        if (P && L && f.all < kWideUnits) {
+        if (P && L && !f.wide) {
             n_prefix = attending((P + kChunk - 1) / kChunk, p.prefix_parts);
         } else if (P && L) {
             const int h = (int)(row - (int64_t)b * H), hk = by_ratio(p, h), tile = ((b - f.first) * p.R + h - hk * p.R) / (64 * WIDE);
@@ -971,10 +978,10 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
 }
 
 int64_t prefix_tiles(int64_t B, int64_t G, int64_t R, int64_t columns) { return G ? B * R / columns + G : 0; }
-// Whether prefixes may take the wide form: half a tile of columns to a group, and room in the block table for that many units.
+// Whether prefixes may take the wide form: enough columns to a group, and room in the block table for that many units.
 bool wide_prefix(int64_t B, int64_t G, int64_t R, int64_t Hkv, int64_t width)
 {
-    return G && B * R / G >= 64 && prefix_tiles(B, G, R, 64 * kWide) * Hkv * width >= kWideUnits;
+    return G && B * R / G >= 80 && prefix_tiles(B, G, R, 64 * kWide) * Hkv * width >= kWideUnits;
 }
 // Workgroups that stand by for each tile of columns of a prefix and KV head, and for each sequence and KV head: two to a compute unit.
 int parts_for(int64_t items, int64_t width)

@@ -179,7 +179,7 @@ def _check_some(s, out, q, lens, pick, bounds):
 
 @pytest.mark.parametrize("H,Hkv,groups,B", [
     (32, 2, [(0, 256, 2176)], 256), (32, 2, [(0, 256, 2177)], 256), (32, 2, [(0, 255, 2300)], 256),     # 34, 35 and 36 pages for 64 tiles of 128 columns
-    (9, 1, [(1, 600, 3361)], 601),                                                                      # heads that do not divide a tile
+    (9, 1, [(1, 600, 3361)], 601), (9, 1, [(1, 600, 3700)], 601),                                       # heads that do not divide a tile
     (32, 8, [(2, 120, 2500), (120, 121, 100), (121, 290, 2943), (290, 299, 0)], 300)])
 def test_shared_of_many_sequences_behind_long_prefixes(H, Hkv, groups, B):
     of = {b: p for a, e, p in groups for b in range(a, e)}
