@@ -12,7 +12,8 @@
 //
 // Bound by memory where rows are many: 4096 rows of 64 ranks beside 28672 x 8192 take 171 us, 33 in the first launch (2.0 TB/s: one workgroup to a
 // compute unit) and 136 in the second (470 MB in and out, 3.5 TB/s; 127 without base, 134 without the stores).  Few rows are launches: 64 of 16
-// ranks beside 6144 x 4096 8.4 us, 3.9 + 4.9 by a profiler.
+// ranks beside 6144 x 4096 8.4 us, 3.9 + 4.9 by a profiler.  (In one launch, every workgroup forming h by itself, one row of 4096 x 4096 and 16 ranks took 7.9 us,
+// 7.0 in two: a compute unit needs 5 us for its 128 KB of A.)
 #include <hip/hip_fp16.h>
 
 #include <algorithm>
