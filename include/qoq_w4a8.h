@@ -348,7 +348,8 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
  *   base [M, N], x [M, K], out [M, N] FP16 with row strides in elements (multiples of 8), so that they may be slices of a fused projection's;
  *   out may be base (with its stride), but not overlap base, x, a or b otherwise.  a [adapters, rank, K], b [adapters, N, rank] FP16 contiguous;
  *   scales [adapters] FP32, or NULL: ones.  An adapter of a smaller rank is padded with zeros.  Sums are FP32; x A^T enters the
- *   second product to 2^-22 of itself, or 2^-39 of the largest of its 64 ranks where that is more; one rounding at the end.
+ *   second product to 2^-22 of itself, or 2^-39 of the largest of its 64 ranks where that is more; one rounding at the end.  What is not finite in x, a or b enters
+ *   the results that the definition has it in, as the infinity or NaN that it gives.
  *   plan  of qoq_lora_plan for the same M and adapters: which rows are whose, worked out once and used by every projection of a step (and
  *         by calls on other streams that are ordered behind it).  A plan of another M or number of adapters, or none: nothing is written.
  *   workspace  required, qoq_lora_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant on entry and exit.

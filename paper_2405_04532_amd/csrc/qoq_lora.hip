@@ -7,8 +7,8 @@
 //
 // The first launch forms h = x A^T, tile by tile, K cut over workgroups.  h enters the second product as pairs of FP16 numbers hi + lo of h
 // scaled by a power of two for each row (and 64 ranks): within 2^-22 of h, or 2^-39 of the row's largest; hi B^T + lo B^T is one product whose k
-// runs over the pairs, B's columns taken twice.  Where few sums meet, the launch of the second product adds the slices of K up and forms the
-// pairs itself; else that is a launch between.  (Joined by the last workgroup of a tile, past the caches, a slice of 4096 x 64 sums took 3 us.)
+// runs over the pairs, B's columns taken twice (and, where that gives NaN, done again with hi alone: an infinity of B).  Where few sums meet, the
+// launch of the second product adds the slices of K up and forms the pairs itself; else that is a launch between.  (Joined by the last workgroup of a tile, past the caches, a slice of 4096 x 64 sums took 3 us.)
 //
 // Bound by memory where rows are many: 4096 rows of 64 ranks beside 28672 x 8192 take 171 us, 33 in the first launch (2.0 TB/s: one workgroup to a
 // compute unit) and 136 in the second (470 MB in and out, 3.5 TB/s; 127 without base, 134 without the stores).  Few rows are launches: 64 of 16
@@ -17,6 +17,7 @@
 #include <hip/hip_fp16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "qoq_internal.h"
 #include "qoq_kv4_common.h"
@@ -104,6 +105,12 @@ struct ShrinkArgs {
 __device__ __forceinline__ int shift_of(float most) { return most > 0.f ? min(140 - (int)(__float_as_uint(most) >> 23), 100) : 0; }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 __device__ __forceinline__ float finite_size(float v) { return fabsf(v) < __builtin_inff() ? fabsf(v) : 0.f; }
+// (a number below half of the smallest step keeps that step and its sign, which the low part takes back: an infinity of B that meets it is one, not 0 times that)
+__device__ __forceinline__ _Float16 high_part(float y)
+{
+    const _Float16 hi = (_Float16)y;
+    return hi == (_Float16)0.f && y != 0.f ? __builtin_bit_cast(_Float16, (unsigned short)((__float_as_uint(y) >> 16 & 0x8000u) | 1u)) : hi;
+}
 __device__ __forceinline__ _Float16 low_part(float y, _Float16 hi)
 {
     const float back = (float)hi;
@@ -248,7 +255,7 @@ __global__ __launch_bounds__(256) void lora_pair_kernel(PairArgs p)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const float y = v[e] * power_of_two(shift);
-        hi[e] = (_Float16)y;
+        hi[e] = high_part(y);
         lo[e] = low_part(y, hi[e]);
     }
     _Float16* to = reinterpret_cast<_Float16*>(p.h) + (int64_t)place * 2 * p.rank + 2 * first + rank;
@@ -328,7 +335,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(WIDE ? 1 : 2
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float y = v[s][e] * power_of_two(shift);
-                        const _Float16 hi = (_Float16)y;
+                        const _Float16 hi = high_part(y);
                         o[e] = pair < ranks ? hi : low_part(y, hi);
                         if (!FULL && pair >= 2 * ranks) o[e] = (_Float16)0.f;
                     }
@@ -348,6 +355,52 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(WIDE ? 1 : 2
     };
     if (t.x >= 0 && !WIDE) load_h(0);
     const __half* b = p.b + (int64_t)max(t.x, 0) * p.N * p.rank;
+    // two neighbouring channels of `base` and the products: words k of the lane's eight channels e
+    auto added = [](uint32_t base, const f4 (&sum)[4], int e, int k) __attribute__((always_inline)) {
+        const h2 o = __builtin_bit_cast(h2, base);
+        return (h2){(_Float16)((float)o.x + sum[2 * e + k / 2][2 * (k & 1)]), (_Float16)((float)o.y + sum[2 * e + k / 2][2 * (k & 1) + 1])};
+    };
+    // h B^T of 64 channels from n0 on; HIGH: of the pairs' high parts alone
+    auto products = [&](auto high, int n0, f4 (&sum)[CT][4]) __attribute__((always_inline)) {
+        constexpr bool HIGH = decltype(high)::value;
+#pragma unroll 1
+        for (int z = 0; z < (WIDE ? p.chunks : 1); ++z) {
+            if (WIDE) load_h(z);
+            const int ranks = min(p.rank - z * kRankChunk, kRankChunk);
+            uint4 w[STEPS][4];
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                if constexpr (FULL && STEPS % 2 == 0 && !HIGH) {          // (16 STEPS ranks: the second half of the steps takes B as the first)
+                    if (s >= STEPS / 2) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[s][j] = w[s - STEPS / 2][j];
+                        continue;
+                    }
+                }
+                const int pair = s * 32 + kb * 8, rank = pair < ranks ? pair : (FULL ? pair : min(pair, 2 * ranks - 8)) - ranks;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int row = min(n0 + (j >> 1) * 32 + (r16 >> 2) * 8 + (j & 1) * 4 + (r16 & 3), p.N - 1);
+                    w[s][j] = *reinterpret_cast<const uint4*>(b + (int64_t)row * p.rank + z * kRankChunk + rank);
+                    if (HIGH ? pair >= ranks : !FULL && pair >= 2 * ranks) w[s][j] = make_uint4(0, 0, 0, 0);
+                }
+            }
+            f4 acc[CT][4];
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c)
+                        acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, w[s][j]), __builtin_bit_cast(h8, hv[c][s]), s ? acc[c][j] : (f4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) sum[c][j][x] = !WIDE || z == 0 ? acc[c][j][x] * scale[c] : fmaf(acc[c][j][x], scale[c], sum[c][j][x]);
+        }
+    };
 #pragma unroll 1
     for (int i = 0; i < p.blocks; ++i) {
         const int n0 = (i * gridDim.x + blockIdx.x) * 64;            // neighbouring workgroups go through neighbouring channels together
@@ -361,59 +414,51 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(WIDE ? 1 : 2
 #pragma unroll
             for (int e = 0; e < 2; ++e) bv[c][e] = *reinterpret_cast<const uint4*>(from[c] + min(n + 32 * e, p.N - 8));
         f4 sum[CT][4];
+        h2 any = {(_Float16)0.f, (_Float16)0.f};         // NaN where a result is
         if (t.x >= 0) {
-#pragma unroll 1
-            for (int z = 0; z < (WIDE ? p.chunks : 1); ++z) {
-                if (WIDE) load_h(z);
-                const int ranks = min(p.rank - z * kRankChunk, kRankChunk);
-                uint4 w[STEPS][4];
+            products(std::false_type(), n0, sum);
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s) {
-                    if constexpr (FULL && STEPS % 2 == 0) {               // (16 STEPS ranks: the second half of the steps takes B as the first)
-                        if (s >= STEPS / 2) {
+            for (int c = 0; c < CT; ++c)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) w[s][j] = w[s - STEPS / 2][j];
-                            continue;
-                        }
+                for (int e = 0; e < 2; ++e) {
+                    uint32_t v[4] = {bv[c][e].x, bv[c][e].y, bv[c][e].z, bv[c][e].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const h2 y = added(v[k], sum[c], e, k);
+                        any = __builtin_elementwise_maximum(any, y);
+                        v[k] = __builtin_bit_cast(uint32_t, y);
                     }
-                    const int pair = s * 32 + kb * 8, rank = pair < ranks ? pair : (FULL ? pair : min(pair, 2 * ranks - 8)) - ranks;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int row = min(n0 + (j >> 1) * 32 + (r16 >> 2) * 8 + (j & 1) * 4 + (r16 & 3), p.N - 1);
-                        w[s][j] = *reinterpret_cast<const uint4*>(b + (int64_t)row * p.rank + z * kRankChunk + rank);
-                        if (!FULL && pair >= 2 * ranks) w[s][j] = make_uint4(0, 0, 0, 0);
-                    }
+                    bv[c][e] = make_uint4(v[0], v[1], v[2], v[3]);
                 }
-                f4 acc[CT][4];
-#pragma unroll
-                for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int c = 0; c < CT; ++c)
-                            acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, w[s][j]), __builtin_bit_cast(h8, hv[c][s]), s ? acc[c][j] : (f4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+            // An infinity of B meets both parts of a pair, of which the low one may be 0 or of the other sign: NaN, where h B is the high part's infinity.
+            if (__builtin_amdgcn_ballot_w64(any.x != any.x || any.y != any.y) != 0) {
+                int again = n0;                          // (operands are requested again, not kept until here)
+                asm volatile("" : "+s"(again));
+                products(std::true_type(), again, sum);
 #pragma unroll
                 for (int c = 0; c < CT; ++c)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int e = 0; e < 2; ++e) {
+                        const uint4 base = *reinterpret_cast<const uint4*>(from[c] + min(again + kb * 8 + 32 * e, p.N - 8));
+                        const uint32_t old[4] = {base.x, base.y, base.z, base.w};
+                        uint32_t v[4] = {bv[c][e].x, bv[c][e].y, bv[c][e].z, bv[c][e].w};
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) sum[c][j][x] = !WIDE || z == 0 ? acc[c][j][x] * scale[c] : fmaf(acc[c][j][x], scale[c], sum[c][j][x]);
+                        for (int k = 0; k < 4; ++k) {
+                            h2 y = __builtin_bit_cast(h2, v[k]);
+                            const h2 by_high = added(old[k], sum[c], e, k);
+                            y.x = y.x != y.x ? by_high.x : y.x;
+                            y.y = y.y != y.y ? by_high.y : y.y;
+                            v[k] = __builtin_bit_cast(uint32_t, y);
+                        }
+                        bv[c][e] = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
             }
         }
 #pragma unroll
         for (int c = 0; c < CT; ++c)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t old[4] = {bv[c][e].x, bv[c][e].y, bv[c][e].z, bv[c][e].w};
-                uint32_t now[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const h2 o = __builtin_bit_cast(h2, old[k]);
-                    const float y0 = (float)o.x + sum[c][2 * e + k / 2][2 * (k & 1)], y1 = (float)o.y + sum[c][2 * e + k / 2][2 * (k & 1) + 1];
-                    now[k] = t.x >= 0 ? __builtin_bit_cast(uint32_t, (h2){(_Float16)y0, (_Float16)y1}) : old[k];
-                }
-                if (c * 16 + r16 < t.z && n + 32 * e < p.N) *reinterpret_cast<uint4*>(to[c] + n + 32 * e) = make_uint4(now[0], now[1], now[2], now[3]);
-            }
+            for (int e = 0; e < 2; ++e)
+                if (c * 16 + r16 < t.z && n + 32 * e < p.N) *reinterpret_cast<uint4*>(to[c] + n + 32 * e) = bv[c][e];
     }
 }
 

@@ -509,6 +509,35 @@ def test_lora_infinities_and_large_numbers(M):
     _check_lora(api.lora_add(base, tiny, a, b, plan, scales=scales), base, tiny, a, b, rows, scales, others[::5])
 
 
+@pytest.mark.parametrize("M,rank", [(20, 8), (20, 16), (37, 24), (37, 32), (37, 48), (37, 64), (20, 136), (300, 32), (530, 8), (530, 40), (530, 64), (600, 200)])
+def test_lora_infinities_and_nan_in_b(M, rank):
+    """Of a channel whose B holds an infinity, a row's result is the infinity that the definition gives (NaN where 0 or both signs meet it), also
+    where x A^T is far below the row's other ranks; the other channels are untouched, in place as well."""
+    N, K, inf = 200, 264, float("inf")
+    base, x, a, b, scales = _lora_inputs(M, N, K, rank, 2, 900 + rank)
+    x[5] = 0
+    a[0, 0] *= 500.0
+    a[0, 1] = 0
+    a[0, 1, 0] = 2.0 ** -24                                                 # 2^-24 x beside some 10^4
+    x[::2, 0] = x[::2, 0].clamp(min=2.0 ** -8, max=2.0 ** -6)
+    rows = [m % 3 for m in range(M)]
+    plan = api.lora_plan(_ints(rows), 2)
+    clean = api.lora_add(base, x, a, b, plan, scales=scales)
+    b[0, 3, 1], b[0, 70, rank - 1], b[0, 131, 0], b[1, 131, 5] = inf, -inf, inf, -inf
+    b[1, 199, 0] = float("nan")
+    b[1, 64, 2], b[1, 64, 3], b[0, 65, 4], b[0, 65, rank // 2] = inf, -inf, inf, inf
+    out = api.lora_add(base, x, a, b, plan, scales=scales)
+    f = lambda t: t.cpu().numpy().astype(np.float64)      # noqa: E731
+    with np.errstate(invalid="ignore"):
+        ref, _ = requests.lora(f(base), f(x), f(a), f(b), [n if n < 2 else -1 for n in rows], f(scales))
+    got, was, bad = f(out), f(clean), ~np.isfinite(ref)
+    assert np.isinf(ref).any() and np.isnan(ref).any() and bad.sum() > 6 * M // 4
+    assert ((got == ref) | (np.isnan(got) & np.isnan(ref)))[bad].all(), np.argwhere(bad & ~((got == ref) | (np.isnan(got) & np.isnan(ref))))[:5]
+    assert (got == was)[~bad].all()
+    api.lora_add(base, x, a, b, plan, scales=scales, out=base)
+    assert _same(base, out)
+
+
 def test_lora_graph_with_its_plan_and_streams():
     """Plan and two projections in one graph, replayed with other adapters and activations in the same tensors; overlapping calls."""
     M, K, rank, adapters = 48, 512, 16, 6
