@@ -101,8 +101,8 @@ struct ShrinkArgs {
     int M, adapters, K, rank, slice;                     // slice: elements of K, a multiple of 128
 };
 
-// 2^shift that brings a row's largest number to 2^13 .. 2^14, with room for the others in FP16's range
-__device__ __forceinline__ int shift_of(float most) { return most > 0.f ? min(140 - (int)(__float_as_uint(most) >> 23), 100) : 0; }
+// 2^shift that brings a row's largest number to 2^14 .. 2^15, the last whole binade of FP16: half of its smallest step, 2^-25, is 2^-39 of that at most
+__device__ __forceinline__ int shift_of(float most) { return most > 0.f ? min(141 - (int)(__float_as_uint(most) >> 23), 100) : 0; }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 __device__ __forceinline__ float finite_size(float v) { return fabsf(v) < __builtin_inff() ? fabsf(v) : 0.f; }
 // (a number below half of the smallest step keeps that step and its sign, which the low part takes back: an infinity of B that meets it is one, not 0 times that)

@@ -538,6 +538,25 @@ def test_lora_infinities_and_nan_in_b(M, rank):
     assert _same(base, out)
 
 
+@pytest.mark.parametrize("M,rank", [(16, 8), (16, 72), (520, 8), (520, 64)])
+@pytest.mark.parametrize("largest", [1.0, 1.0009765625, 1.9990234375])
+def test_lora_small_middle_products_beside_large_ones(M, rank, largest):
+    """Middle products of c 2^-41 beside one of `largest`, each brought to its own channel 2^39 times: off by 2^-22 of itself or 2^-39 of the largest,
+    and the result's rounding (each is a single product, so nothing else is rounded)."""
+    base = torch.zeros((M, 64), dtype=torch.float16, device=DEV)
+    x, a, b = torch.zeros((M, 8), device=DEV), torch.zeros((1, rank, 8), device=DEV), torch.zeros((1, 64, rank), device=DEV)
+    x[:, 0], x[:, 1] = largest, 2.0 ** -20
+    a[0, 0, 0] = 1.0
+    c = torch.zeros(64, device=DEV)
+    for n in range(1, min(rank, 64)):
+        c[n] = n % 15 + 1
+        a[0, n, 1], b[0, n, n] = float(c[n]) * 2.0 ** -21, 1.0
+    out = api.lora_add(base, x.half(), a.half(), b.half(), api.lora_plan(_ints([0] * M), 1), scales=torch.tensor([2.0 ** 39], device=DEV))
+    want = c.double() / 4
+    tol = 2.0 ** -22 * want + largest + 2.0 ** -11 * (want + largest)
+    assert ((out.double() - want).abs() <= tol).all(), float(((out.double() - want).abs() / tol).max())
+
+
 def test_lora_graph_with_its_plan_and_streams():
     """Plan and two projections in one graph, replayed with other adapters and activations in the same tensors; overlapping calls."""
     M, K, rank, adapters = 48, 512, 16, 6
