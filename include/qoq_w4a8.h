@@ -359,7 +359,7 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
  *     logprob[m] = x[t] - log sum_j exp(x[j]),  t = tokens[m];   entropy[m] = -sum_j p_j log p_j
  *     rank[m]    = 1 + the number of tokens in front of t in the order of the logits, equal ones by index
  *     top_ids, top_logprobs [M, top]: the first `top` (at most 32, at most V) in that order
- *   Sums are FP32, held relative to the row's largest.  Logits of minus infinity (a masked vocabulary) have probability 0 and logprob minus
+ *   Sums are FP32, held relative to the row's largest, long ones FP64 (no chain of more than 132 additions of FP32).  Logits of minus infinity (a masked vocabulary) have probability 0 and logprob minus
  *   infinity.  A token outside [0, V): logprob NaN, rank 0.  A row that holds a NaN or plus infinity, or minus infinity only: all of its
  *   results NaN, rank 0, top_ids -1.  tokens may be NULL with logprob and rank; logprob, rank and entropy may be NULL.
  *   workspace  NULL, or qoq_token_logprobs_workspace_bytes(...) bytes (0: none is needed), 16-byte aligned, contents irrelevant on entry and exit;

@@ -800,6 +800,31 @@ def test_logprobs_many_rows_and_the_longest():
         _check_logprobs(api.token_logprobs(x, _ints([12345678]), 32, workspace=ws), x, [12345678], 32)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("M,V", [(2, 1 << 24), (3, 1 << 20), (2, 300001), (1100, 128256)])
+def test_logprobs_of_long_rows_of_near_equal_logits(dtype, M, V):
+    """A workgroup to a row, whose sums are of many terms alike, above the reference that the first ones set: the bound has no term that grows with V
+    (8 additions of FP32 within a vector, 32 of vectors, 64 of those, and 28 at most across lanes and waves, 132 in all; the others in FP64)."""
+    g = torch.Generator(device=DEV).manual_seed(V)
+    x = torch.empty((M, V), dtype=dtype, device=DEV)
+    for m in range(M):
+        x[m] = (torch.rand(V, generator=g, device=DEV) * 1.4 + 1.3).to(dtype) if m % 2 == 0 else 2.6875 + 0.0625 * (m % 3 - 1)
+    x[:, :256 * 32] = 0
+    tokens = _ints([V - 1 - m for m in range(M)])
+    lp, _, ent, ids, tops = api.token_logprobs(x, tokens, top=1)
+    for m in range(M):
+        d = x[m].double()
+        d = d - d.max()
+        e = d.exp()
+        lse = float(e.sum().log())
+        dist = float((e * -d).sum() / e.sum())
+        dT = 2.0 ** -23 + 2.0 ** -24 * (1.1 * dist + 6) + 132 * 2.0 ** -24
+        want = float(d[V - 1 - m]) - lse
+        assert abs(float(lp[m]) - want) <= dT + 2.0 ** -24 * abs(want), (m, float(lp[m]) - want, dT)
+        assert abs(float(tops[m, 0]) + lse) <= dT + 2.0 ** -24 * lse, (m, float(tops[m, 0]) + lse, dT)
+        assert abs(float(ent[m]) - (lse + dist)) <= dT * (2 + 2 * (1.45 * dist + 8)) + 2.0 ** -24 * (lse + dist), (m, float(ent[m]) - lse - dist)
+
+
 def test_logprobs_past_four_gigabytes():
     V = 70001
     x = torch.zeros((32000, V), dtype=torch.float16, device=DEV)            # 4.5 GB: 2.24e9 elements
