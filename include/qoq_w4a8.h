@@ -292,8 +292,8 @@ int qoq_kv4_unpack(const void* cache, int64_t B, int64_t Hkv, int64_t S_max, int
  *   sequence b, (code - z) s rounded once; zeros where it lies on no page.  For a prompt that goes on behind cached tokens.
  * qoq_kv4_paged_attention_decode: qoq_kv4_attention_decode over pages, q [B, H, 128] with a stride, out [B, H, 128] contiguous; of
  *   the seq_lens[b] tokens (clamped to [0, 64 width]) those t with  t >= seq_lens[b] - window  or  t < sinks  are seen; window = 0:
- *   all.  A query that sees nothing gives a zero row.  Weight times value scale is rounded to FP16 relative to the largest there is:
- *   2^-11 of itself, or (scores within 5e6) 2^-39 of the largest weight times the largest scale where that is more.
+ *   all.  A query that sees nothing gives a zero row, one whose scores are all minus infinity NaN.  Weight times value scale is rounded to
+ *   FP16 relative to the largest there is: 2^-11 of itself, or (scores within 5e6) 2^-39 of the largest weight times the largest scale where that is more.
  *   workspace  NULL, or at least qoq_kv4_paged_attention_workspace_bytes(...) bytes (0: none is needed), 16-byte aligned, zero-filled
  *              once with qoq_gemm_workspace_prepare, as for qoq_w4a8_gemm, whose workspace may be the same one: calls of both kinds
  *              and any shapes may take turns in it on one stream; calls that overlap in time need workspaces of their own.

@@ -665,7 +665,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
     const int n4 = R * (kD / 4);                         // results, four elements each
     float* mine = p.parts + ((size_t)bh * ns + split) * R * kPartial;
     auto write_out = [&](int x, float4 num, float den) {
-        const float inv = den > 0.f ? 1.f / den : 1.f;   // nothing seen: zero, as the sums are (NaN stays)
+        float inv = den > 0.f ? 1.f / den : 1.f;         // nothing seen: zero, as the sums are (NaN stays)
+        if (den == 0.f)                                  // tokens seen all the same: their scores are minus infinity, and this is no softmax
+            for (int i = 0; i < n; ++i)
+                if ((uint32_t)pages_of[(i < n_first ? i : i + gap) >> 1] < pages) {
+                    inv = __builtin_nanf("");
+                    break;
+                }
         const h2 a = {(_Float16)(num.x * inv), (_Float16)(num.y * inv)}, c = {(_Float16)(num.z * inv), (_Float16)(num.w * inv)};
         reinterpret_cast<uint2*>(out_bh)[x] = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
     };

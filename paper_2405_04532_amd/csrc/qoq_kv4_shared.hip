@@ -87,6 +87,25 @@ __device__ __forceinline__ int prefix_of(const SharedArgs& p, int b, int lane)
     return 0;
 }
 
+// 1 / the weights' sum of sequence b, of whose L tokens P lie in front of its prefix's end.  Without a weight: a sequence that sees nothing has a zero row,
+// as its sums are; one that does has scores of minus infinity only, and NaN.  (Looked up then: no other call pays for it.)
+__device__ __forceinline__ float inverse_sum(const SharedArgs& p, float den, int b, int L, int P)
+{
+    if (den != 0.f || L == 0) return den > 0.f ? 1.f / den : 1.f;           // (a NaN stays)
+    int first = b;
+    for (int g = 0; P > 0 && g < p.G; ++g)
+        if (p.cu[g] <= b && b < p.cu[g + 1]) {
+            first = max(p.cu[g], 0);
+            break;
+        }
+    const int shared = min(P, L);
+    for (int i = 0; i < L; i = (i / kPageTokens + 1) * kPageTokens) {
+        if (i < shared && (uint32_t)p.table[(int64_t)first * p.width + i / kPageTokens] < p.pages) return __builtin_nanf("");
+        if (min((i / kPageTokens + 1) * kPageTokens, L) > shared && (uint32_t)p.table[(int64_t)b * p.width + i / kPageTokens] < p.pages) return __builtin_nanf("");
+    }
+    return 1.f;
+}
+
 // sums over the lanes up to each, in registers
 __device__ __forceinline__ int upto_lane(int v)
 {
@@ -900,7 +919,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
                 den = fmaf(ml[e].y, f, den);
             }
         }
-        const float inv = den > 0.f ? 1.f / den : 1.f;   // nothing seen: zero, as the sums are (NaN stays)
+        const float inv = inverse_sum(p, den, b, k.hi, P);
         *reinterpret_cast<h4*>(p.out + row * kD + d) = (h4){(_Float16)(num.x * inv), (_Float16)(num.y * inv), (_Float16)(num.z * inv), (_Float16)(num.w * inv)};
     };
     if (k.lo < k.hi) {
@@ -973,7 +992,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
             sum.x = fmaf(a[e].x, g, sum.x); sum.y = fmaf(a[e].y, g, sum.y);
         }
     }
-    const float inv = den > 0.f ? 1.f / den : 1.f;       // nothing seen: zero, as the sums are (NaN stays)
+    const float inv = inverse_sum(p, den, b, L, P);
     reinterpret_cast<h2*>(p.out + row * kD)[lane] = (h2){(_Float16)(sum.x * inv), (_Float16)(sum.y * inv)};
 }
 

@@ -398,6 +398,53 @@ def test_shared_pages_past_four_gigabytes():
     assert (out.float() - want.float()).abs().max() <= 4 * 2.0 ** -11 * want.float().abs().max() + 1e-4
 
 
+def _shared_pool(B, Hkv, prefix, own, seed):
+    """Sequences of prefix (whole pages) + own tokens, keys with a channel (5) that no token has at zero."""
+    width, first = -(-(prefix + own) // PAGE), prefix // PAGE
+    n_own, M = width - first, prefix + B * own
+    table = torch.empty((B, width), dtype=torch.int32)
+    table[:, :first] = torch.arange(first)
+    table[:, first:] = first + torch.arange(B * n_own).view(B, n_own)
+    table = table.to(DEV)
+    k, v = _heads(M, Hkv, seed), _heads(M, Hkv, seed + 1, True)
+    k[..., 5] = k.abs().amax(-1).clamp(min=1.0)
+    pool = torch.full(((first + B * n_own) * Hkv * 8704,), 0xFF, dtype=torch.uint8, device=DEV)
+    starts = [0] + [prefix] * (B - 1)
+    cu = [0] + [prefix + (b + 1) * own for b in range(B)]
+    api.kv4_paged_append(pool, k, v, table, _ints(cu), _ints(starts))
+    return pool, table
+
+
+@pytest.mark.parametrize("B,H,Hkv,prefix,own", [(6, 8, 2, 192, 50), (3, 16, 1, 4096, 300), (300, 32, 4, 128, 40), (256, 32, 2, 2304, 30)])
+def test_shared_queries_whose_scores_are_all_minus_infinity(B, H, Hkv, prefix, own):
+    """A softmax of nothing but minus infinity is none: NaN, as in prompt attention, in that query's row alone; a sequence without tokens, or
+    whose pages are none, has a zero row whatever its query is.  With and without groups, and in the call that has none."""
+    pool, table = _shared_pool(B, Hkv, prefix, own, 201)
+    lens = [prefix + own - b % 7 for b in range(B)]
+    lens[1], lens[2] = prefix - 3, 0                                        # inside the prefix; nothing
+    q = wl.make_queries(B, H, D, 203, DEV)
+    bad = q.clone()
+    hit = torch.zeros((B, H), dtype=torch.bool, device=DEV)
+    for b, h in ((0, 0), (0, H - 1), (1, 1), (2, 0), (B - 1, 2), (B // 2, H // 2)):
+        bad[b, h, 5] = -float("inf")
+        hit[b, h] = lens[b] > 0
+    cu, pl, ln = _ints([0, B]), _ints([prefix]), _ints(lens)
+    none = torch.empty(0, dtype=torch.int32, device=DEV)
+    ws = api.new_workspace(api.kv4_paged_attention_workspace_bytes(B, H, Hkv, table.shape[1]), DEV)
+    for call in (lambda t: api.kv4_shared_attention_decode(t, pool, table, ln, cu, pl, Hkv),
+                 lambda t: api.kv4_shared_attention_decode(t, pool, table, ln, _ints([0]), none, Hkv),
+                 lambda t: api.kv4_paged_attention_decode(t, pool, table, ln, Hkv), lambda t: api.kv4_paged_attention_decode(t, pool, table, ln, Hkv, workspace=ws)):
+        clean, out = call(q), call(bad)
+        assert torch.isfinite(clean).all() and out[hit].isnan().all() and _same(out[~hit], clean[~hit])
+        assert not out[2].any()
+    gone = table.clone()
+    gone[0], gone[B - 1] = -1, 1 << 30
+    keep = [b for b in range(B) if b not in (0, B - 1)]
+    out, clean = (api.kv4_shared_attention_decode(t, pool, gone, ln, _ints([0]), none, Hkv) for t in (bad, q))
+    assert not out[[0, B - 1]].any() and out[hit & (torch.arange(B, device=DEV) % (B - 1) > 0)[:, None]].isnan().all()
+    assert _same(out[keep][~hit[keep]], clean[keep][~hit[keep]])
+
+
 # ------------------------------------------------------------------------------------------------------------------
 # Adapters
 # ------------------------------------------------------------------------------------------------------------------
