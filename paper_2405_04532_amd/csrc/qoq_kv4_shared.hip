@@ -996,7 +996,9 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs p)
     reinterpret_cast<h2*>(p.out + row * kD)[lane] = (h2){(_Float16)(sum.x * inv), (_Float16)(sum.y * inv)};
 }
 
-int64_t prefix_tiles(int64_t B, int64_t G, int64_t R, int64_t columns) { return G ? B * R / columns + G : 0; }
+// Tiles of columns of all prefixes at most: every group may end in a part of one, but no more than B of them hold a sequence (3 sequences in 20000 groups
+// 0.15 ms, with workgroups for a tile of each 44).
+int64_t prefix_tiles(int64_t B, int64_t G, int64_t R, int64_t columns) { return B * R / columns * (G > 0) + std::min(G, B); }
 // Whether prefixes may take the wide form: enough columns to a group, and room in the block table for that many units.
 bool wide_prefix(int64_t B, int64_t G, int64_t R, int64_t Hkv, int64_t width)
 {

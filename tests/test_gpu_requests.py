@@ -445,6 +445,21 @@ def test_shared_queries_whose_scores_are_all_minus_infinity(B, H, Hkv, prefix, o
     assert _same(out[keep][~hit[keep]], clean[keep][~hit[keep]])
 
 
+@pytest.mark.parametrize("B,H,Hkv", [(5, 8, 2), (40, 16, 1)])
+def test_shared_of_more_groups_than_sequences(B, H, Hkv):
+    """Most groups hold no sequence: in front of, between and behind those that do."""
+    G, prefix = 2000, 130
+    held = [(0, 2, prefix), (2, 3, 70), (3, B, 200)]
+    lens = [next(p for a, e, p in held if a <= b < e) + 3 + b for b in range(B)]
+    s = _Batch(held, lens, Hkv, 211)
+    cu, pl = [0] * 700 + [2] * 300 + [3] * 500 + [B] * (G + 1 - 1500), [5] * G
+    pl[699], pl[999], pl[1499] = prefix, 70, 200                            # the last group that begins in front of each bound holds what lies there
+    q = wl.make_queries(B, H, D, 213, DEV)
+    out = api.kv4_shared_attention_decode(q, s.pool, s.table, _ints(lens), _ints(cu), _ints(pl), Hkv)
+    s.check(out, q)
+    assert _same(out, s.call(q)) or (out.float() - s.call(q).float()).abs().max() < 1e-2
+
+
 # ------------------------------------------------------------------------------------------------------------------
 # Adapters
 # ------------------------------------------------------------------------------------------------------------------

@@ -59,6 +59,12 @@ def test_shared_workspace_bytes():
         assert size(B, H, Hkv, width, groups + 1) > 0
 
 
+@pytest.mark.parametrize("B,H,Hkv,width", [(1, 4, 4, 1), (3, 32, 8, 100), (40, 16, 1, 3000), (5, 64, 8, 300)])
+def test_shared_workspace_of_more_groups_than_sequences(B, H, Hkv, width):
+    """No more than B groups hold a sequence, so none beyond them takes workgroups, or their parts."""
+    assert len({api.kv4_shared_attention_workspace_bytes(B, H, Hkv, width, groups) for groups in (B, B + 1, 20 * B, 1 << 20)}) == 1
+
+
 @pytest.mark.parametrize("over,want", [
     (dict(M=-1), SHAPE), (dict(M=(1 << 20) + 1), SHAPE), (dict(adapters=0), SHAPE), (dict(adapters=4097), SHAPE), (dict(plan=None), NULL), (dict(rows=None), NULL),
     (dict(rows=None, M=0), ARCH), (dict(plan="p8"), ALIGN), (dict(rows="p2"), ALIGN), (dict(nbytes=64), WORKSPACE), (dict(), ARCH)])
