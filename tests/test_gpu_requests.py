@@ -460,6 +460,34 @@ def test_shared_of_more_groups_than_sequences(B, H, Hkv):
     assert _same(out, s.call(q)) or (out.float() - s.call(q).float()).abs().max() < 1e-2
 
 
+def test_shared_of_long_prefixes_in_more_groups_than_lanes():
+    """70 groups of 128 columns a KV head behind 5 or 6 pages: the units of work of groups 64 and up are counted behind those of the first 64."""
+    H, Hkv, n, G = 128, 8, 8, 70
+    B = n * G
+    groups = [(g * n, g * n + n, (0 if g == 30 else 321 + g % 64)) for g in range(G)]
+    units = sum(Hkv * -(-p // PAGE) for _, _, p in groups)
+    assert n * (H // Hkv) == 128 and units >= 2250 + 500                    # no column of a tile of 128 is empty: the form of many columns
+    lens = [groups[b // n][2] + 1 + (b * 5) % 20 for b in range(B)]
+    for g in (0, 63, 64, 69):
+        a, p = groups[g][0], groups[g][2]
+        lens[a + 1], lens[a + 2], lens[a + 3] = 0, p // 2, p
+    s = _Batch(groups, lens, Hkv, 221)
+    q = wl.make_queries(B, H, D, 223, DEV)
+    out = s.call(q)
+    _check_some(s, out, q, lens, [g * n + i for g in (0, 63, 64, 69) for i in (0, 1, 2, 3, 7)] + [30 * n, 31 * n, 65 * n + 4], groups)
+    for _ in range(3):
+        assert _same(s.call(q), out)
+    # bounds that descend: nothing else is touched, and the next call is as it was
+    need = api.kv4_shared_attention_workspace_bytes(B, H, Hkv, s.width, G)
+    for cu in ([B - g * n for g in range(G + 1)], [(0 if g % 2 else B) for g in range(G + 1)], [(g * 37 % 71) * n for g in range(G + 1)]):
+        held, ws = torch.full((B + 2, H, D), 7.0, dtype=torch.float16, device=DEV), torch.full((need + 4096,), 0x55, dtype=torch.uint8, device=DEV)
+        before = s.pool.clone()
+        api.kv4_shared_attention_decode(q, s.pool, s.table, _ints(s.lens), _ints(cu), _ints(s.prefix), Hkv, out=held[1:-1], workspace=ws[:need])
+        torch.cuda.synchronize()
+        assert (held[0] == 7).all() and (held[-1] == 7).all() and (ws[need:] == 0x55).all() and torch.equal(s.pool, before)
+    assert _same(s.call(q), out)
+
+
 # ------------------------------------------------------------------------------------------------------------------
 # Adapters
 # ------------------------------------------------------------------------------------------------------------------
