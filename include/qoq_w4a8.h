@@ -293,7 +293,8 @@ int qoq_kv4_unpack(const void* cache, int64_t B, int64_t Hkv, int64_t S_max, int
  * qoq_kv4_paged_attention_decode: qoq_kv4_attention_decode over pages, q [B, H, 128] with a stride, out [B, H, 128] contiguous; of
  *   the seq_lens[b] tokens (clamped to [0, 64 width]) those t with  t >= seq_lens[b] - window  or  t < sinks  are seen; window = 0:
  *   all.  A query that sees nothing gives a zero row, one whose scores are all minus infinity NaN.  Weight times value scale is rounded to
- *   FP16 relative to the largest there is: 2^-11 of itself, or (scores within 5e6) 2^-39 of the largest weight times the largest scale where that is more.
+ *   FP16 relative to the largest there is: 2^-11 of itself, or (scores within 5e6) 2^-39 of the largest weight times the largest scale
+ *   (2^-15 where that is less) where that is more.
  *   workspace  NULL, or at least qoq_kv4_paged_attention_workspace_bytes(...) bytes (0: none is needed), 16-byte aligned, zero-filled
  *              once with qoq_gemm_workspace_prepare, as for qoq_w4a8_gemm, whose workspace may be the same one: calls of both kinds
  *              and any shapes may take turns in it on one stream; calls that overlap in time need workspaces of their own.
@@ -342,7 +343,7 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
  *     prefix_lens  [groups] INT32, device, clamped to [0, 64 width]; a sequence that is shorter sees its seq_lens[b] tokens of it
  *     groups = 0: the pointers may be NULL.  Bounds that descend give unspecified results and touch nothing else.
  *   Sums are FP32; weight times value scale is rounded once, to 2^-11 of itself, or (scores within 5e6) 2^-33 of the largest weight times
- *   the largest scale of what the sequence sees where that is more.
+ *   the largest scale of what the sequence sees (2^-15 where that is less) where that is more.
  *   workspace  required, qoq_kv4_shared_attention_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant on entry and exit.
  * qoq_lora_add: out[m] = base[m] + scales[a] (x[m] A_a^T) B_a^T for the rows m of adapter a, out[m] = base[m] for those of none.
  *   base [M, N], x [M, K], out [M, N] FP16 with row strides in elements (multiples of 8), so that they may be slices of a fused projection's;

@@ -356,7 +356,8 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(const uint8_t* __rest
 // arrive adds them up, in the order of the workgroups whichever arrives when, and leaves the counter at zero.
 //
 // The second product's operand is weight x value scale in FP16: off by 2^-11 of itself, or by 2^-39 of the largest weight x scale where that is
-// more (a lane's largest weight times its largest scale, of four or eight tokens at a time).
+// more (a lane's largest weight times its largest scale, of four or eight tokens at a time, or 2^-15 where that is less: a subnormal scale's exponent
+// no longer tells its size).
 //
 // Bound by memory where there are pairs enough, 64 x 1024 tokens of 32 heads 39 us (5.4 TB/s); else by the trips to memory one after the
 // other: table, page, a wave's chunks, and the join's (parts out, counter, parts in: about 4 us); 8192 tokens of 8 KV heads 10.7 us, 40 tokens 4.0.

@@ -19,7 +19,6 @@
 
 #include "qoq_gemm_common.h"
 #include "qoq_kv4_common.h"
-#include "qoq_workspace.h"
 
 namespace qoq {
 namespace {
@@ -429,7 +428,8 @@ __device__ __forceinline__ void attend(const SharedArgs& p, const Work& k, float
 // wave, the next page while this one is used.
 constexpr int kPageFragments = 32;                       // of 1 KB: keys [tile][word], values [chunk][u][j]
 // Binades that the reference is set above what the largest weight needs, so that it seldom has to follow: each time costs half a chunk's arithmetic.
-// Weight times scale is FP16: as many binades less of its range are left below the largest (2^-33 of it, not 2^-39, is its smallest step's half).
+// Weight times scale is FP16: as many binades less of its range are left below the largest (2^-33 of it, or of a weight
+// beside a scale of 2^-15 where there is none as large, and not 2^-39, is its smallest step's half).
 constexpr float kSpare = 6.f;
 struct WidePage {
     uint4 fragment[kPageFragments][64];
@@ -551,7 +551,6 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& p, const Work& k, 
             uint4 kf[8], vf[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) kf[e] = page.fragment[half * 8 + e][lane];
-            __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_sched_barrier(0);
             f4 d[CT][2];
             float t[CT][8], over[CT];

@@ -227,7 +227,7 @@ __device__ __forceinline__ void put_ranked(const Shared& sh, int found, int n, P
     }
 }
 
-// ln T = k ln 2 + 2 artanh((m - 1) / (m + 1)), T = 2^k m with m in 0.70 .. 1.42: the series to the thirteenth power is good to 1e-13
+// ln T = k ln 2 + 2 artanh((m - 1) / (m + 1)), T = 2^k m with m in 0.70 .. 1.42: the series to the thirteenth power is good to 5e-13
 __device__ __forceinline__ double ln_of(float T)
 {
     const uint32_t u = __float_as_uint(T);

@@ -553,7 +553,7 @@ hipError_t launch_lora_add(const LoraAdd& l, hipStream_t s)
     const int64_t blocks64 = (l.N + 63) / 64;
     // blocks of 64 channels for each wave, which keeps h meanwhile
     const int64_t each = std::max<int64_t>(1, std::min<int64_t>(8, tiles * blocks64 / 8192)), groups = (blocks64 + each - 1) / each;
-    if (tiles >= (int64_t)1 << 22 || tiles * slices * chunks >= (int64_t)1 << 24 || tiles * groups >= (int64_t)1 << 24) return hipErrorInvalidValue;
+    if (tiles * groups >= (int64_t)1 << 24) return hipErrorInvalidValue;    // (tiles and slices are at most 20481 and, with the chunks, 163848)
     const dim3 grid((unsigned)tiles, (unsigned)slices, (unsigned)chunks);
     auto* shrink = big ? (rt == 1 ? lora_shrink_kernel<4, 1> : rt == 2 ? lora_shrink_kernel<4, 2> : lora_shrink_kernel<4, 4>)
                        : (rt == 1 ? lora_shrink_kernel<1, 1> : rt == 2 ? lora_shrink_kernel<1, 2> : lora_shrink_kernel<1, 4>);
