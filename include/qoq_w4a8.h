@@ -344,6 +344,8 @@ int qoq_attention_prefill(const void* q_fp16, int64_t q_stride, const void* k_fp
  *     groups = 0: the pointers may be NULL.  Bounds that descend give unspecified results and touch nothing else.
  *   Sums are FP32; weight times value scale is rounded once, to 2^-11 of itself, or (scores within 5e6) 2^-33 of the largest weight times
  *   the largest scale of what the sequence sees (2^-15 where that is less) where that is more.
+ *   It is worth its second launch where one group's sequences x tokens of the prefix x KV heads come to some 500 000 (up to four query heads to a
+ *   KV head) or 2 000 000 (eight); below that the call without groups is level or up to 5 us ahead, where the tables name the prefix's pages for all.
  *   workspace  required, qoq_kv4_shared_attention_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant on entry and exit.
  * qoq_lora_add: out[m] = base[m] + scales[a] (x[m] A_a^T) B_a^T for the rows m of adapter a, out[m] = base[m] for those of none.
  *   base [M, N], x [M, K], out [M, N] FP16 with row strides in elements (multiples of 8), so that they may be slices of a fused projection's;

@@ -12,9 +12,14 @@
 // second that of the own tokens, which joins.  The arithmetic of a chunk and the weights' reference are those of the
 // paged decode kernel (qoq_kv4_paged.hip).
 //
-// A prefix of many columns is bound by the vector unit beside the matrix unit: 200 sequences of 64 / 8 heads with 100 tokens behind 16000 take 190 us, 0.55
-// PFLOP/s, in which the matrix unit is busy for a quarter of the cycles and the vector unit for 0.45 (exp2, weights, FP16).  Short ones are bound
-// by the chain of trips to memory: 4 sequences with 30 tokens behind 1000 10.7 us, 7.7 + 3 for the join by a profiler.
+// A prefix of many columns is bound by the vector unit beside the matrix unit: 200 sequences of 64 / 8 heads with 100 tokens behind 16000 take 187 us, 0.56
+// PFLOP/s, in which the matrix unit is busy for 0.26 of the cycles and the vector unit for 0.49 (exp2, weights, FP16).  Short ones are bound
+// by the chain of trips to memory: 4 sequences with 30 tokens behind 1000 10.7 us, 7.8 and 3.6 for the join by a profiler.
+//
+// Without groups (every sequence reads its prefix itself, qoq_kv4_paged.hip) these two take 432 and 8.1 us: a second launch costs some 3, and columns cost
+// arithmetic.  In one group the call is ahead from about 500 000 sequences x tokens of the prefix x KV heads on where a KV head has up to four query
+// heads (16 behind 4096 of 32 / 8 heads 15.2 and 17.2, 8 behind 1000 of 32 / 32 10.9 and 12.5; 16 behind 1000 of 32 / 8 11.5 and 10.1), from 2 000 000 on
+// where it has eight (64 behind 4096 of 64 / 8 37.3 and 42.7, behind 1000 21.1 and 15.6).
 #include <algorithm>
 
 #include "qoq_gemm_common.h"
@@ -1019,7 +1024,7 @@ int wide_parts(int64_t B, int64_t G, int64_t R, int64_t Hkv, int64_t width)
 }
 // Whether the own tokens have a launch of their own, behind the prefixes' and in place of the join, with registers and LDS for three workgroups on a
 // compute unit, not two.  Side by side with a prefix they fill what it leaves, so few gain nothing, nor do those beside prefixes that may be long for
-// the wide form: 64 sequences of 32 / 8 heads with 300 tokens behind 4096 27.6 us in one launch and joined, 29.7 one behind the other; 200 of 40 / 8
+// the wide form: 64 sequences of 32 / 8 heads with 300 tokens behind 4096 26.5 us in one launch and joined, 28.5 one behind the other; 200 of 40 / 8
 // with 100 behind 1000 36.1 and 32.7; 512 of 32 / 8 with 300 behind 100 64.4 and 52.2; 300 of 32 / 8 with 100 behind 8000 in three groups 96 and 103,
 // 200 of 64 / 8 with 100 behind 16000 190 and 195.  Without prefixes there is the one launch: 64 of 32 / 8 with 300 tokens 11.5 us joined, 7.6 so.
 bool own_launch(int64_t B, int64_t G, int64_t Hkv, int own_parts, bool wide) { return own_parts == 1 && !wide && (!G || B * Hkv > 1000); }

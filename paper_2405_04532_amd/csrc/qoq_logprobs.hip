@@ -12,9 +12,9 @@
 // registers by ballots, bit by bit; the vectors of the lanes at or above the best wave's are looked through again (they are in the L2), and
 // what is found is ranked by counting.
 //
-// Many rows are bound by memory, a workgroup to each: 4001 of 32000 FP16 48 us without alternatives, 5.3 TB/s, 54 to 57 with the largest (the vector
-// unit is active for nearly all of that).  Few rows are shared by workgroups whose parts a second launch joins, and are bound by the chain of steps: one of 32000 with
-// 5 alternatives 11.4 us, 64 of 128256 with 20 17.2.
+// Many rows are bound by memory, a workgroup to each: 4001 of 32000 FP16 46 us without alternatives, 5.5 TB/s, 54 with the largest where the same logits
+// are read again and again, 58.7 where each pass has others (the vector unit is active for nearly all of that).  Few rows are shared by workgroups
+// whose parts a second launch joins, and are bound by the chain of steps: one of 32000 with 5 alternatives 11.5 us, 64 of 128256 with 20 17.3.
 #include <hip/hip_fp16.h>
 
 #include <algorithm>

@@ -10,9 +10,12 @@
 // runs over the pairs, B's columns taken twice (and, where that gives NaN, done again with hi alone: an infinity of B).  Where few sums meet, the
 // launch of the second product adds the slices of K up and forms the pairs itself; else that is a launch between.  (Joined by the last workgroup of a tile, past the caches, a slice of 4096 x 64 sums took 3 us.)
 //
-// Bound by memory where rows are many: 4096 rows of 64 ranks beside 28672 x 8192 take 171 us, 33 in the first launch (2.0 TB/s: one workgroup to a
-// compute unit) and 136 in the second (470 MB in and out, 3.5 TB/s; 127 without base, 134 without the stores).  Few rows are launches: 64 of 16
-// ranks beside 6144 x 4096 8.4 us, 3.9 + 4.9 by a profiler.  (In one launch, every workgroup forming h by itself, one row of 4096 x 4096 and 16 ranks took 7.9 us,
+// Many rows are bound by the trips to memory that a wave makes one after the other: 4096 rows of 64 ranks beside 28672 x 8192 take 172 us, 34 in the first
+// launch (2.0 TB/s: one workgroup to a compute unit) and 138 in the second (470 MB in and out, 3.4 TB/s).  It is not the bytes that the second waits for (136
+// took 127 without base, 134 without the stores), nor arithmetic (matrix unit 0.10 of the cycles, vector unit 0.13): of two waves to a SIMD, none has the next
+// block's operands in flight while it multiplies and stores.  Few rows are launches: 64 of 16 ranks beside 6144 x 4096 8.5 us, 4.0 + 5.0 by a profiler.  More
+// than 64 ranks: the pairs are read again for every 64 channels, by one wave to a SIMD where rows are many (2048 rows beside 8192 x 8192: 56 ranks 41 us,
+// 128 89, 256 166; 64 rows of 256 ranks beside 6144 x 4096 23.6).  (In one launch, every workgroup forming h by itself, one row of 4096 x 4096 and 16 ranks took 7.9 us,
 // 7.0 in two: a compute unit needs 5 us for its 128 KB of A.)
 #include <hip/hip_fp16.h>
 
